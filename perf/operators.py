@@ -1,0 +1,512 @@
+"""Performance cases of the operators over a bounded cache held in 4 bits.
+
+Every cached K and V row is stored as 4-bit floats (e2m1: 0, .5, 1, 1.5, 2, 3, 4,
+6 and their negatives) with one power-of-two scale per 32 elements:
+
+    E = the smallest integer with max|x| <= 6 * 2^E, within [-119, 125]
+    x^ = 2^E * e2m1(x / 2^E), rounded half to even; scale byte E + 127
+
+(255 for a group with an infinity or NaN, which reads back as NaN).  Two codes a byte, the
+lower half first.  Five operators:
+
+* ``store``: rows are written into the cache, and read back;
+* ``read``: a stretch of cached rows is read back;
+* ``decode``: tokens of generation over a cache (attention, scores, one
+  removal a step where the cache is full);
+* ``long``: one token over a cache that is never cut (outputs only);
+* ``prefill``: a prompt's block over the cached entries and its own rows.
+
+A call's own rows are attended to as given; entries cached before it as they
+read back.  ``run`` in its plain form computes this with elementary torch
+operations in float32.  Rows that a decode step stores come back in what the
+steps behind it make of them; a prefill's and a long decode's are read back.
+"""
+import math
+
+import torch
+
+own = False
+
+_DTYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+_MAX_GEN = 1 << 28      # decode goes on for as long as the program runs
+_E2M1 = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
+
+
+def _case(op, *, name=None, dtype="bf16", b, heads, kv_heads, d=128, n, rows=1, slot0=0, steps=1,
+          full=False, pad_max=0):
+    """n: entries in the cache (store: slots); rows: rows of the call; full: the
+    cache is at its bound, so each decode step removes one entry."""
+    c = dict(op=op, dtype=dtype, b=b, heads=heads, kv_heads=kv_heads, d=d, n=n, rows=rows,
+             slot0=slot0, steps=steps, full=full, pad_max=pad_max)
+    if name:
+        c["name"] = name
+    return c
+
+
+def listed():
+    return [
+        # one generated token's rows for a small batch: latency is what it costs
+        _case("store", name="store-b8-rows1", b=8, heads=32, kv_heads=8, n=768, slot0=700),
+        # a prompt block's rows for an ordinary batch
+        _case("store", name="store-b64-rows256", b=64, heads=32, kv_heads=8, n=768, rows=256,
+              slot0=512),
+        # a float32 multi-head layer with small heads, odd row counts
+        _case("read", name="read-f32-d64-rows333", dtype="f32", b=5, heads=20, kv_heads=20, d=64,
+              n=400, rows=333, slot0=33),
+        # whole caches of a large batch, as a program does that hands a layer on
+        _case("read", name="read-b512-rows512", b=512, heads=32, kv_heads=8, n=768, rows=512),
+        # one user's next tokens through an 8B model's layer shape
+        _case("decode", name="decode-b1-n512", b=1, heads=32, kv_heads=8, n=512, steps=8, full=True),
+        # an ordinary batch
+        _case("decode", name="decode-b64-n512", b=64, heads=32, kv_heads=8, n=512, steps=4,
+              full=True),
+        # throughput serving: the largest decode batch
+        _case("decode", name="decode-b1024-n512", b=1024, heads=32, kv_heads=8, n=512, steps=2,
+              full=True),
+        # float32, multi-head, small heads, odd length, padded on the left, not yet full
+        _case("decode", name="decode-f32-mha-padded-n333", dtype="f32", b=6, heads=12, kv_heads=12,
+              d=64, n=333, steps=4, pad_max=100),
+        # a token over a few whole 8192-token prompts
+        _case("long", name="long-b8-n8192", b=8, heads=32, kv_heads=8, n=8192),
+        # one user's very long prompt
+        _case("long", name="long-b1-n60001", b=1, heads=32, kv_heads=8, n=60001),
+        # a prompt's block of an ordinary batch, the cache at its bound
+        _case("prefill", name="prefill-b64-n512", b=64, heads=32, kv_heads=8, n=512, rows=256),
+        # one user's last, partial block; small heads, two queries per KV head, padded
+        _case("prefill", name="prefill-b3-d64-n201", b=3, heads=16, kv_heads=8, d=64, n=201,
+              rows=77, pad_max=230),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return min(hi, max(lo, int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))))
+
+
+def draw(rng):
+    op = rng.choice(("store", "read", "decode", "decode", "decode", "long", "prefill", "prefill"))
+    while True:
+        group = rng.choice((1, 2, 4, 4))
+        kv = rng.choice((1, 2, 4, 5, 8, 8))
+        shape = dict(dtype=rng.choice(("bf16",) * 4 + ("f32",)), heads=kv * group, kv_heads=kv,
+                     d=rng.choice((64, 128, 128)))
+        if op in ("store", "read"):
+            rows = _log_int(rng, 1, 2048)
+            slot0 = rng.choice((0, rng.randint(1, 700)))
+            case = _case(op, b=_log_int(rng, 1, 512), rows=rows, slot0=slot0,
+                         n=slot0 + rows + rng.choice((0, 1, rng.randint(1, 500))), **shape)
+        elif op == "decode":
+            n = _log_int(rng, 40, 4096)
+            full = rng.random() < 0.7
+            case = _case(op, b=_log_int(rng, 1, 1024), n=n - 8 * (not full), steps=rng.randint(2, 8),
+                         full=full, pad_max=0 if full else rng.choice((0, n // 3)), **shape)
+        elif op == "long":
+            n = _log_int(rng, 4200, 65000)
+            case = _case(op, b=_log_int(rng, 1, 32), n=n, pad_max=rng.choice((0, 0, n // 2)), **shape)
+        else:
+            n, rows = rng.choice((0, _log_int(rng, 1, 2048))), _log_int(rng, 1, 512)
+            case = _case(op, b=_log_int(rng, 1, 128), n=n, rows=rows,
+                         pad_max=rng.choice((0, 0, n + rows // 2)), **shape)
+        w = work(case)
+        slow = 16 if case["dtype"] == "f32" else 1          # float32 matrix instructions' rate
+        if w["bytes"] < 1.3e9 and w["flops"] * slow < 1.7e11 and _plain_bytes(case) < 1.2e10:
+            return case
+
+
+def _units(case):
+    return case["b"] * case["kv_heads"]
+
+
+def _visible(case):
+    """(query, key) pairs of one query head of the call's rows, padding aside."""
+    n, r = case["n"], case["rows"]
+    return r * n + r * (r + 1) // 2
+
+
+def _plain_bytes(case):
+    """The plain form's largest intermediate results."""
+    deq = 8 * _units(case) * case["n"] * case["d"]
+    group = case["heads"] // case["kv_heads"]
+    return deq + 8 * _units(case) * group * _visible(case)
+
+
+def work(case):
+    """Every input read once, every output written once; 4 d flops per visible
+    (query, key) pair.  Padded batches count as unpadded."""
+    d, es = case["d"], 2 if case["dtype"] == "bf16" else 4
+    pair4, pair = 2 * (d // 2 + d // 32), 2 * d * es     # a cached pair, a pair of rows as given
+    u, h, n, r = _units(case), case["b"] * case["heads"], case["n"], case["rows"]
+    if case["op"] == "store":
+        return {"bytes": u * r * (pair + pair4 + pair), "flops": 0}
+    if case["op"] == "read":
+        return {"bytes": u * r * (pair4 + pair), "flops": 0}
+    qo = 2 * d * es
+    if case["op"] == "decode":
+        step = u * (n * (pair4 + 12) + pair + pair4 + 8) + h * qo
+        return {"bytes": case["steps"] * step, "flops": case["steps"] * 4 * d * h * (n + 1)}
+    if case["op"] == "long":
+        return {"bytes": u * (n * pair4 + 2 * pair + pair4 + 8) + h * qo, "flops": 4 * d * h * (n + 1)}
+    return {"bytes": u * (n * (pair4 + 12) + r * (2 * pair + pair4 + 8)) + h * r * qo,
+            "flops": 4 * d * h * _visible(case)}
+
+
+# --------------------------------------------------------------------------
+# the format, in plain operations
+# --------------------------------------------------------------------------
+def _quantise(x):
+    """x [..., d] -> codes uint8 [..., d / 2], scales uint8 [..., d / 32]."""
+    g = x.float().unflatten(-1, (-1, 32))
+    amax = g.abs().amax(dim=-1, keepdim=True)
+    _, e = torch.frexp(amax / 1.5)            # amax / 1.5 = f 2^e with f in [.5, 1)
+    power = torch.ldexp(torch.full_like(amax, 0.5), e)     # 2^(e - 1) <= amax / 1.5
+    e = e - 3 + (amax > 1.5 * power).int()    # 6 2^(e - 3) is 1.5 times that power
+    e = e.clamp(-119, 125)
+    y = torch.ldexp(g, -e)
+    a = y.abs().clamp_max(6.0)
+    step = torch.where(a < 2, 0.5, torch.where(a < 4, 1.0, 2.0))
+    a = torch.round(a / step) * step
+    code = torch.where(a < 2, 2 * a, torch.where(a < 4, a + 2, a / 2 + 4))
+    fine = torch.isfinite(amax)
+    code = torch.where(fine, code, 0.0).to(torch.uint8) | (torch.signbit(y).to(torch.uint8) << 3)
+    scale = torch.where(fine, e + 127, 255).to(torch.uint8).squeeze(-1)
+    code = code.flatten(-2)
+    return code[..., 0::2] | (code[..., 1::2] << 4), scale
+
+
+def _values(codes, scale):
+    """The float32 values that codes [..., d / 2] and scales [..., d / 32] stand for."""
+    c = torch.stack([codes & 15, codes >> 4], dim=-1).flatten(-2)
+    table = torch.tensor(_E2M1 + tuple(-x for x in _E2M1), device=codes.device)
+    x = table[c.int()].unflatten(-1, (-1, 32))
+    s = (scale.int() << 23).view(torch.float32)
+    s = torch.where(scale == 255, float("nan"), s)
+    return (x * s[..., None]).flatten(-2)
+
+
+# --------------------------------------------------------------------------
+# inputs
+# --------------------------------------------------------------------------
+def _generator(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(int(seed))
+    return g
+
+
+def _normal(g, shape, dt):
+    return torch.randn(shape, generator=g, device="cuda", dtype=dt)
+
+
+def _keys(g, shape, dt):
+    """N(0, 1) rows times a lognormal factor per (sample, head, position)."""
+    k = _normal(g, shape, dt)
+    return k.mul_(torch.exp(0.5 * torch.randn(shape[:3] + (1,), generator=g, device="cuda")).to(dt))
+
+
+def _first(case):
+    """The position of the call's first row: a full cache has lost entries."""
+    return 2 * case["n"] + 1000 if case["full"] else case["n"]
+
+
+def _slots(case):
+    return case["n"] if case["op"] in ("store", "read") else case["n"] + max(case["rows"], case["steps"])
+
+
+def _inputs(case, seed):
+    """Rows of the call and the cache before it: codes and scales, scores,
+    positions (a full cache's spread over twice the prompt)."""
+    g, dt = _generator(seed), _DTYPES[case["dtype"]]
+    b, h, hk, d, n = case["b"], case["heads"], case["kv_heads"], case["d"], case["n"]
+    slots, t = _slots(case), max(case["rows"], case["steps"])
+    x = {"q": _normal(g, (b, h, t, d), dt), "kin": _keys(g, (b, hk, t, d), dt),
+         "vin": _normal(g, (b, hk, t, d), dt)}
+    x["k"], x["k_scale"] = _quantise(_keys(g, (b, hk, slots, d), dt))
+    x["v"], x["v_scale"] = _quantise(_normal(g, (b, hk, slots, d), dt))
+    x["pads"] = None
+    if case["pad_max"]:
+        x["pads"] = torch.randint(0, case["pad_max"] + 1, (b,), generator=g, device="cuda",
+                                  dtype=torch.int32)
+    x["pos"] = torch.zeros((b, hk, slots), device="cuda", dtype=torch.int32)
+    x["score"] = torch.zeros((b, hk, slots), device="cuda")
+    first, group = _first(case), h // hk
+    if case["full"]:
+        # increasing positions, one in each of n equal segments; a few old entries
+        # get next to nothing and leave in turn
+        seg = first / n
+        u = torch.rand((b, hk, n), generator=g, device="cuda")
+        i = torch.arange(n, device="cuda")
+        lo, hi = torch.floor(i * seg), torch.floor((i + 1) * seg)
+        pos = torch.minimum(lo + torch.floor(u * (hi - lo)), hi - 1)
+        ave = torch.exp(0.5 * torch.randn((b, hk, n), generator=g, device="cuda"))
+        idle = torch.rand((b, hk, n // 2), generator=g, device="cuda").topk(case["steps"] + 1).indices
+        low = 0.01 * (1.5 ** torch.arange(case["steps"] + 1, device="cuda")).expand(b, hk, -1)
+        ave.scatter_(2, idle, low)
+    else:
+        pos = torch.arange(n, device="cuda").expand(b, hk, n).float()
+        ave = torch.exp(0.5 * torch.randn((b, hk, n), generator=g, device="cuda"))
+    x["pos"][:, :, :n] = pos.int()
+    if case["op"] in ("decode", "prefill"):
+        x["score"][:, :, :n] = ave * group / (n + 1) * (first - pos)
+        if x["pads"] is not None:
+            x["score"][:, :, :n].masked_fill_(pos < x["pads"][:, None, None], 0.0)
+    return x
+
+
+def prepare(case, seed):
+    x = _inputs(case, seed)
+    b, hk, d = case["b"], case["kv_heads"], case["d"]
+    state = {"case": case, "o": torch.zeros_like(x["q"]), "next": _first(case), **x}
+    if case["op"] != "decode":
+        dt = _DTYPES[case["dtype"]]
+        state["ko"] = torch.empty((b, hk, case["rows"], d), device="cuda", dtype=dt)
+        state["vo"] = torch.empty_like(state["ko"])
+    if own:
+        # the layer's cache, filled as the prompt left it, and its context
+        from paper_2412_05693_amd import batchmax
+
+        grows = case["op"] in ("store", "read", "long") or (case["op"] == "decode" and not case["full"])
+        block, kv_max = case["rows"] if case["op"] == "prefill" else 1, _slots(case) if grows else case["n"]
+        last = _first(case) + (case["rows"] if case["op"] == "prefill" else 0)
+        att = batchmax.PDAttentionKV4(
+            b=b, s=max(1, last), kv_max=max(1, kv_max), block=block, max_gen=_MAX_GEN,
+            n_heads=case["heads"], n_kv_heads=hk, head_dim=d, dtype=case["dtype"])
+        n = _slots(case) if case["op"] in ("store", "read") else case["n"]
+        for name in ("k", "v", "k_scale", "v_scale", "score", "pos"):
+            getattr(att, name)[:, :, :n] = x[name][:, :, :n]
+        att.len.fill_(case["n"])
+        if x["pads"] is not None:
+            att.set_left_padding(x["pads"])
+        if case["op"] == "long":
+            att.set_score_accumulation(False)
+        if case["op"] not in ("store", "read"):
+            att.resume(case["n"], _first(case))
+        state["att"] = att
+    return state
+
+
+# --------------------------------------------------------------------------
+# one pass: the package's calls
+# --------------------------------------------------------------------------
+def _run_own(state):
+    case, att = state["case"], state["att"]
+    q, kin, vin, o, n = state["q"], state["kin"], state["vin"], state["o"], case["n"]
+    if case["op"] in ("store", "read"):
+        if case["op"] == "store":
+            att.write_rows(case["slot0"], kin, vin)
+        att.read_rows(case["slot0"], case["rows"], state["ko"], state["vo"])
+        return {"k": state["ko"], "v": state["vo"]}
+    if case["op"] == "decode":
+        if not case["full"]:
+            att.resume(n, n)
+            state["next"] = n
+        for i in range(case["steps"]):
+            att.decode_step(state["next"], q, kin, vin, o, row=i)
+            state["next"] += 1
+        live = att.length
+        return {"o": o, "score": att.score[:, :, :live], "pos": att.pos[:, :, :live]}
+    att.resume(n, n)
+    if case["op"] == "long":
+        att.decode_step(n, q, kin, vin, o)
+        att.read_rows(n, 1, state["ko"], state["vo"])
+        return {"o": o, "k": state["ko"], "v": state["vo"]}
+    att.prefill_block(n, case["rows"], q, kin, vin, o, row=0)
+    att.read_rows(n, case["rows"], state["ko"], state["vo"])
+    return {"o": o, "score": att.score[:, :, :n + case["rows"]], "k": state["ko"], "v": state["vo"]}
+
+
+# --------------------------------------------------------------------------
+# one pass: the plain form
+# --------------------------------------------------------------------------
+def _write(state, at, k, v):
+    """Rows k, v [b, hk, r, d] into the slots `at` on (an integer, or one slot index
+    [b, hk, 1] per unit)."""
+    for name, x in (("k", k), ("v", v)):
+        codes, scale = _quantise(x)
+        for y, z in ((state[name], codes), (state[name + "_scale"], scale)):
+            if isinstance(at, int):
+                y[:, :, at:at + z.shape[2]] = z
+            else:
+                y.scatter_(2, at[..., None].expand(z.shape), z)
+
+
+def _stored(state, at, rows):
+    dt = _DTYPES[state["case"]["dtype"]]
+    return {x: _values(state[x][:, :, at:at + rows], state[x + "_scale"][:, :, at:at + rows]).to(dt)
+            for x in ("k", "v")}
+
+
+def _attend(state, n, q, kin, vin, first):
+    """Rows q [b, h, r, d] at positions first.. over n cached entries and the rows'
+    own -> outputs, probabilities [b, hk, group, r, n + r]."""
+    case = state["case"]
+    b, hk, d, r = case["b"], case["kv_heads"], case["d"], q.shape[2]
+    group = case["heads"] // hk
+    kk = torch.cat([_values(state["k"][:, :, :n], state["k_scale"][:, :, :n]), kin.float()], dim=2)
+    vv = torch.cat([_values(state["v"][:, :, :n], state["v_scale"][:, :, :n]), vin.float()], dim=2)
+    z = torch.matmul(q.float().reshape(b, hk, group * r, d), kk.transpose(2, 3).contiguous())
+    z = z.view(b, hk, group, r, n + r) / math.sqrt(d)
+    rows = torch.arange(r, device="cuda")
+    own_pos = (first + rows).int().expand(b, hk, r)
+    pos = torch.cat([state["pos"][:, :, :n], own_pos], dim=2)
+    gone = torch.arange(n + r, device="cuda") > n + rows[:, None]
+    if state["pads"] is not None:
+        pads = state["pads"][:, None, None]
+        z = z.masked_fill((pos < pads)[:, :, None, None], float("-inf"))
+        gone = gone | ((first + rows)[:, None] < pads)[:, None, None]
+    z = z.masked_fill(gone, float("-inf"))
+    m = z.amax(dim=-1, keepdim=True)
+    p = torch.exp(z - torch.where(torch.isinf(m), 0.0, m))
+    p = p / p.sum(dim=-1, keepdim=True).clamp_min(1e-30)
+    o = torch.matmul(p.view(b, hk, group * r, n + r), vv).view(b, hk * group, r, d)
+    return o.to(q.dtype), p
+
+
+def _step(state, n, i):
+    """One decode step: attention, scores, and the smallest (average, position)
+    leaves if the cache is full."""
+    case, now = state["case"], state["next"]
+    kin, vin = state["kin"][:, :, i:i + 1], state["vin"][:, :, i:i + 1]
+    state["o"][:, :, i:i + 1], p = _attend(state, n, state["q"][:, :, i:i + 1], kin, vin, now)
+    gain = p.sum(dim=(2, 3))
+    score, pos = state["score"], state["pos"]
+    score[:, :, :n] += gain[:, :, :n]
+    at = torch.full_like(pos[:, :, :1], n, dtype=torch.long)
+    if case["full"]:
+        full_pos = torch.cat([pos[:, :, :n], torch.full_like(pos[:, :, :1], now)], dim=2)
+        ave = torch.cat([score[:, :, :n], gain[:, :, n:]], dim=2) / (now + 1 - full_pos).float()
+        least = ave == ave.amin(dim=2, keepdim=True)
+        at = torch.where(least, full_pos, 1 << 30).argmin(dim=2, keepdim=True)
+    # (a full cache's slot n is scratch: the step's own pair may be the one that leaves)
+    score.scatter_(2, at, gain[:, :, n:])
+    pos.scatter_(2, at, torch.full_like(pos[:, :, :1], now))
+    _write(state, at, kin, vin)
+    state["next"] = now + 1
+
+
+def _run_plain(state):
+    case, n, r = state["case"], state["case"]["n"], state["case"]["rows"]
+    q, kin, vin = state["q"], state["kin"], state["vin"]
+    if case["op"] in ("store", "read"):
+        if case["op"] == "store":
+            _write(state, case["slot0"], kin, vin)
+        return _stored(state, case["slot0"], r)
+    if case["op"] == "decode":
+        live = n if case["full"] else n + case["steps"]
+        if not case["full"]:
+            state["next"] = n
+        for i in range(case["steps"]):
+            _step(state, n if case["full"] else n + i, i)
+        return {"o": state["o"], "score": state["score"][:, :, :live], "pos": state["pos"][:, :, :live]}
+    o, p = _attend(state, n, q, kin, vin, n)
+    _write(state, n, kin, vin)
+    if case["op"] == "long":
+        return {"o": o, **_stored(state, n, 1)}
+    gain = p.sum(dim=(2, 3))
+    state["score"][:, :, :n] += gain[:, :, :n]
+    state["score"][:, :, n:n + r] = gain[:, :, n:]
+    return {"o": o, "score": state["score"][:, :, :n + r], **_stored(state, n, r)}
+
+
+def run(state):
+    return _run_own(state) if own else _run_plain(state)
+
+
+# --------------------------------------------------------------------------
+# the same in 64 bits
+# --------------------------------------------------------------------------
+def _nearest(x):
+    """What rows x [..., d] stand for once stored: the nearest of the fifteen values
+    on each group's scale, the even code on a tie."""
+    g = x.double().unflatten(-1, (-1, 32))
+    top = g.abs().amax(dim=-1, keepdim=True)
+    e = torch.ceil(torch.log2(top / 6.0)).clamp(-119, 125)
+    # the logarithm may round across an integer: settle by the definition itself
+    e = torch.where(top <= 6.0 * torch.exp2(e - 1), e - 1, torch.where(top > 6.0 * torch.exp2(e), e + 1, e))
+    e = e.clamp(-119, 125)
+    y = g / torch.exp2(e)
+    a = y.abs().contiguous()
+    grid = torch.tensor(_E2M1, device=x.device, dtype=torch.float64)
+    mid = (grid[1:] + grid[:-1]) / 2
+    lower = torch.bucketize(a, mid, right=False)      # a tie stays with the lower code
+    upper = torch.bucketize(a, mid, right=True)       # ... or goes to the upper one
+    idx = torch.where(lower % 2 == 0, lower, upper)
+    return (torch.sign(y) * grid[idx] * torch.exp2(e)).flatten(-2)
+
+
+def _decoded(codes, scale):
+    lo, hi = (codes % 16).long(), (codes // 16).long()
+    c = torch.stack([lo, hi], dim=-1).flatten(-2)
+    grid = torch.tensor(_E2M1, device=codes.device, dtype=torch.float64)
+    x = torch.where(c >= 8, -1.0, 1.0) * grid[c % 8]
+    return (x.unflatten(-1, (-1, 32)) * torch.exp2(scale.double() - 127)[..., None]).flatten(-2)
+
+
+def _softmax_over(q, kk, vv, seen):
+    """q [u, g, r, d], kk and vv [u, l, d], seen [u, r, l] -> o, probabilities."""
+    u, g, r, d = q.shape
+    z = torch.bmm(q.reshape(u, g * r, d), kk.transpose(1, 2).contiguous()).view(u, g, r, -1) / math.sqrt(d)
+    z = torch.where(seen[:, None], z, -math.inf)
+    m = z.amax(dim=-1, keepdim=True).clamp_min(-1e300)
+    p = torch.where(seen[:, None], torch.exp(z - m), 0.0)
+    p = p / p.sum(dim=-1, keepdim=True).clamp_min(1e-300)
+    return torch.bmm(p.view(u, g * r, -1), vv).view(u, g, r, d), p
+
+
+def _exact_units(case, x, u0, u1):
+    """Units u0..u1 of an attention case -> outputs, scores (None where none are kept)."""
+    b, hk, d, n, r = case["b"], case["kv_heads"], case["d"], case["n"], case["rows"]
+    group, units = case["heads"] // hk, b * hk
+    take = lambda y: y.reshape((units,) + tuple(y.shape[2:]))[u0:u1]       # noqa: E731
+    q = x["q"].view(units, group, -1, d)[u0:u1].double()
+    kin, vin = take(x["kin"]), take(x["vin"])
+    kk = _decoded(take(x["k"][:, :, :n]), take(x["k_scale"][:, :, :n]))
+    vv = _decoded(take(x["v"][:, :, :n]), take(x["v_scale"][:, :, :n]))
+    pos, score = take(x["pos"][:, :, :n]).long(), take(x["score"][:, :, :n]).double()
+    pad = torch.zeros(u1 - u0, device="cuda", dtype=torch.long)
+    if x["pads"] is not None:
+        pad = x["pads"].long().repeat_interleave(hk)[u0:u1]
+    now, out = _first(case), []
+    for i in range(case["steps"]):
+        t = r if case["op"] == "prefill" else 1
+        at = now + torch.arange(t, device="cuda")
+        mine = slice(i, i + t)
+        pos = torch.cat([pos, at.expand(u1 - u0, t)], dim=1)
+        kall = torch.cat([kk, kin[:, mine].double()], dim=1)
+        vall = torch.cat([vv, vin[:, mine].double()], dim=1)
+        seen = (pos[:, None] <= at[:, None]) & (pos[:, None] >= pad[:, None, None])
+        seen = seen & (at[:, None] >= pad[:, None, None])
+        o, p = _softmax_over(q[:, :, mine], kall, vall, seen)
+        out.append(o)
+        score = torch.cat([score, torch.zeros((u1 - u0, t), device="cuda", dtype=torch.float64)], dim=1)
+        score = score + p.sum(dim=(1, 2))
+        kk = torch.cat([kk, _nearest(kin[:, mine])], dim=1)
+        vv = torch.cat([vv, _nearest(vin[:, mine])], dim=1)
+        now += t
+        if case["full"]:
+            order = torch.argsort(pos, dim=1, stable=True)
+            key = (score / (now - pos)).gather(1, order)
+            slot = order.gather(1, key.argmin(dim=1, keepdim=True))
+            for y in (score, pos):
+                y.scatter_(1, slot, y[:, n:].clone())
+            for y in (kk, vv):
+                y.scatter_(1, slot[..., None].expand(-1, -1, d), y[:, n:].clone())
+            score, pos, kk, vv = score[:, :n], pos[:, :n], kk[:, :n], vv[:, :n]
+    return torch.cat(out, dim=2), score
+
+
+def exact(case, seed):
+    x = _inputs(case, seed)
+    b, h, hk, d, n = case["b"], case["heads"], case["kv_heads"], case["d"], case["n"]
+    if case["op"] == "store":
+        return {"k": _nearest(x["kin"]), "v": _nearest(x["vin"])}
+    if case["op"] == "read":
+        s = slice(case["slot0"], case["slot0"] + case["rows"])
+        return {y: _decoded(x[y][:, :, s], x[y + "_scale"][:, :, s]) for y in ("k", "v")}
+    units, rows = b * hk, case["rows"]
+    cost = (h // hk) * rows * (n + rows) + 6 * (n + rows) * d
+    size = max(1, min(units, int(1.5e8 / cost)))
+    parts = [_exact_units(case, x, u, min(units, u + size)) for u in range(0, units, size)]
+    o = torch.cat([p[0] for p in parts]).view(b, h, -1, d)
+    score = torch.cat([p[1] for p in parts]).view(b, hk, -1)
+    if case["op"] == "decode":
+        return {"o": o, "score": score, "pos": None}
+    stored = {"k": _nearest(x["kin"]), "v": _nearest(x["vin"])}
+    return {"o": o, **stored} if case["op"] == "long" else {"o": o, "score": score, **stored}
