@@ -1,0 +1,91 @@
+/*
+ * bm_kv4.h -- the bounded cache held in 4 bits (part of libbatchmax).
+ *
+ * Every K and V row of the cache is stored as 4-bit floats (e2m1: 0, .5, 1,
+ * 1.5, 2, 3, 4, 6 and their negatives) with one power-of-two scale for each
+ * group of 32 consecutive elements (the OCP microscaling format MXFP4): 4.25
+ * bits an element, so the memory of a bfloat16 cache holds 3.76 times the
+ * entries.  Groups lie inside one row, so single entries are written, evicted
+ * and moved without touching their neighbours.
+ *
+ *   E   = the smallest integer with max|x_i| <= 6 * 2^E, within [-119, 125]
+ *   x^  = 2^E * e2m1(x_i / 2^E), rounded to nearest, ties to the even code
+ *
+ * The scale byte is E + 127.  Elements beyond 6 * 2^125 become +-6 * 2^125; a
+ * group with an infinity or a NaN has the scale byte 255 and reads back as 32
+ * NaN.  Every x^ is exact in bfloat16 and in float32, and a row that was read
+ * back and is written again keeps its values.
+ *
+ * A context made by bm_kv4_init or bm_kv4_resume drives such a cache through
+ * the calls of batchmax.h: bm_prefill_block, bm_prefill_block_cut,
+ * bm_evict_compact, bm_decode_step, the bm_set_* calls and bm_destroy, with the
+ * same arguments, checks, order and limits.  A call's own K and V rows are
+ * attended to as given and stored in 4 bits; entries cached before the call
+ * are attended to as they read back.  Scores, positions and lengths are those
+ * of batchmax.h.
+ */
+#ifndef BM_KV4_H
+#define BM_KV4_H
+
+#include "batchmax.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Elements that share one scale. */
+#define BM_KV4_GROUP 32
+
+/* The cache, caller-owned device memory, all C-contiguous.
+ *   k, v              [b, n_kv_heads, cap, head_dim / 2] bytes: element 2i in the
+ *                     lower half of byte i, element 2i + 1 in the upper half;
+ *                     16-byte aligned
+ *   k_scale, v_scale  [b, n_kv_heads, cap, head_dim / 32] bytes; 4-byte aligned
+ *   score, pos, len   as in bm_cache
+ *   work              bm_kv4_workspace_bytes(dims) bytes of scratch, 16-byte
+ *                     aligned; contents need not survive between calls (but
+ *                     for BM_RANK_TOVA's weights, as in bm_cache) */
+typedef struct bm_kv4_cache {
+  void* k;
+  void* v;
+  void* k_scale;
+  void* v_scale;
+  float* score;
+  int32_t* pos;
+  int32_t* len;
+  void* work;
+  size_t work_bytes;
+} bm_kv4_cache;
+
+/* Bytes of bm_kv4_cache.work; 0 if dims are invalid.  They hold
+ * bm_workspace_bytes(dims) and one layer's cached rows in the element type of
+ * dims.dtype, which a prefill block reads back once for all its queries;
+ * layers that run one after another can share it. */
+size_t bm_kv4_workspace_bytes(const bm_dims* dims);
+
+/* bm_init over a 4-bit cache: enqueues the zeroing of len and score. */
+int bm_kv4_init(const bm_dims* dims, const bm_kv4_cache* cache, hipStream_t stream, bm_ctx** out);
+
+/* bm_resume over a 4-bit cache that already holds `len` entries per unit. */
+int bm_kv4_resume(const bm_dims* dims, const bm_kv4_cache* cache, int32_t len, int32_t next_pos,
+                  bm_ctx** out);
+
+/* Store n rows of every unit in slots slot0 .. slot0 + n - 1 of the cache.
+ *   k, v  point at row 0 of [b, n_kv_heads, seq_ld, head_dim] buffers of the
+ *         element type of dims.dtype, 16-byte aligned; seq_ld >= n
+ * Scores, positions and lengths are left as they are, the other slots too.
+ * The cache's work, score, pos and len are not read and may be null.
+ * BM_ERR_CAPACITY if slot0 + n exceeds cap; n = 0 is a no-op. */
+int bm_kv4_write(const bm_dims* dims, const bm_kv4_cache* cache, int32_t slot0, int32_t n,
+                 const void* k, const void* v, int32_t seq_ld, hipStream_t stream);
+
+/* The inverse: slots slot0 .. slot0 + n - 1 of every unit into rows 0 .. n - 1
+ * of k and v.  Rows from n on are left as they are.  k and v must not overlap. */
+int bm_kv4_read(const bm_dims* dims, const bm_kv4_cache* cache, int32_t slot0, int32_t n, void* k,
+                void* v, int32_t seq_ld, hipStream_t stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* BM_KV4_H */

@@ -60,6 +60,16 @@ class bm_cache(ctypes.Structure):
                 ("work_bytes", ctypes.c_size_t)]
 
 
+class bm_kv4_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("score", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("len", ctypes.c_void_p), ("work", ctypes.c_void_p),
+                ("work_bytes", ctypes.c_size_t)]
+
+
+BM_KV4_GROUP = 32       # elements that share one scale of a 4-bit row
+
+
 def _load() -> ctypes.CDLL:
     # torch ships its own HIP runtime under the same soname as ROCm's; load it
     # first so this library binds to that single runtime instead of a second copy
@@ -72,6 +82,7 @@ def _load() -> ctypes.CDLL:
     lib = ctypes.CDLL(LIB_PATH)
     P, I32, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
     dims_p, cache_p = ctypes.POINTER(bm_dims), ctypes.POINTER(bm_cache)
+    kv4_p = ctypes.POINTER(bm_kv4_cache)
     sig = {
         "bm_abi_version": (ctypes.c_int, []),
         "bm_last_error": (ctypes.c_char_p, []),
@@ -92,6 +103,11 @@ def _load() -> ctypes.CDLL:
         "bm_set_left_padding": (ctypes.c_int, [P, P]),
         "bm_set_split_event": (ctypes.c_int, [P, P]),
         "bm_decode_step": (ctypes.c_int, [P, I32, P, P, P, P, I32, P]),
+        "bm_kv4_workspace_bytes": (SZ, [dims_p]),
+        "bm_kv4_init": (ctypes.c_int, [dims_p, kv4_p, P, ctypes.POINTER(P)]),
+        "bm_kv4_resume": (ctypes.c_int, [dims_p, kv4_p, I32, I32, ctypes.POINTER(P)]),
+        "bm_kv4_write": (ctypes.c_int, [dims_p, kv4_p, I32, I32, P, P, I32, P]),
+        "bm_kv4_read": (ctypes.c_int, [dims_p, kv4_p, I32, I32, P, P, I32, P]),
         "bm_ctx_len": (I32, [P]),
         "bm_ctx_next_pos": (I32, [P]),
         "bm_destroy": (None, [P]),
@@ -117,6 +133,7 @@ EXPORTED = ("bm_abi_version", "bm_last_error", "bm_cache_slots", "bm_workspace_b
             "bm_set_decode_removal", "bm_set_rank_rule", "bm_set_decode_bound",
             "bm_set_score_accumulation", "bm_set_left_padding", "bm_set_split_event",
             "bm_decode_step", "bm_ctx_len", "bm_ctx_next_pos", "bm_destroy", "bm_synth_qkv",
+            "bm_kv4_workspace_bytes", "bm_kv4_init", "bm_kv4_resume", "bm_kv4_write", "bm_kv4_read",
             "bm_philox4x32_10", "bm_probe_stream_read", "bm_probe_mfma",
             "bm_prefill_timeline", "bm_prefill_tile_workgroups")
 
@@ -216,6 +233,33 @@ def bm_decode_step(ctx: int, pos: int, q: int, k: int, v: int, o: int, seq_ld: i
     _check(_lib.bm_decode_step(ctx, pos, q, k, v, o, seq_ld, stream))
 
 
+def bm_kv4_workspace_bytes(dims: bm_dims) -> int:
+    return _lib.bm_kv4_workspace_bytes(ctypes.byref(dims))
+
+
+def bm_kv4_init(dims: bm_dims, cache: bm_kv4_cache, stream: int) -> int:
+    out = ctypes.c_void_p()
+    _check(_lib.bm_kv4_init(ctypes.byref(dims), ctypes.byref(cache), stream, ctypes.byref(out)))
+    return out.value
+
+
+def bm_kv4_resume(dims: bm_dims, cache: bm_kv4_cache, length: int, next_pos: int) -> int:
+    out = ctypes.c_void_p()
+    _check(_lib.bm_kv4_resume(ctypes.byref(dims), ctypes.byref(cache), length, next_pos,
+                              ctypes.byref(out)))
+    return out.value
+
+
+def bm_kv4_write(dims: bm_dims, cache: bm_kv4_cache, slot0: int, n: int, k: int, v: int,
+                 seq_ld: int, stream: int) -> None:
+    _check(_lib.bm_kv4_write(ctypes.byref(dims), ctypes.byref(cache), slot0, n, k, v, seq_ld, stream))
+
+
+def bm_kv4_read(dims: bm_dims, cache: bm_kv4_cache, slot0: int, n: int, k: int, v: int,
+                seq_ld: int, stream: int) -> None:
+    _check(_lib.bm_kv4_read(ctypes.byref(dims), ctypes.byref(cache), slot0, n, k, v, seq_ld, stream))
+
+
 def bm_ctx_len(ctx: int) -> int:
     return _lib.bm_ctx_len(ctx)
 
@@ -302,34 +346,29 @@ class PDAttention:
         self.cap = bm_cache_slots(self.dims)
         self.group = n_heads // n_kv_heads
         U = b * n_kv_heads
-        self.work_bytes = bm_workspace_bytes(self.dims)
+        self.work_bytes = self._workspace_bytes(self.dims)
         self.static_workspace = static_workspace
         if static_workspace and buffers is not None:
             raise ValueError("static_workspace takes no caller buffers")
+        want = self._buffers()
         if buffers is None:
-            self.k = torch.empty((b, n_kv_heads, self.cap, head_dim), dtype=self.tdtype, device=self.device)
-            self.v = torch.empty_like(self.k)
-            self.score = torch.empty((b, n_kv_heads, self.cap), dtype=torch.float32, device=self.device)
-            self.pos = torch.zeros((b, n_kv_heads, self.cap), dtype=torch.int32, device=self.device)
-            self.len = torch.empty((b, n_kv_heads), dtype=torch.int32, device=self.device)
+            for nm, (shape, dt) in want.items():
+                # (positions start defined: resume() may count entries that a caller never wrote)
+                make = torch.zeros if nm == "pos" else torch.empty
+                setattr(self, nm, make(shape, dtype=dt, device=self.device))
             self.work = (None if static_workspace else
                          torch.empty(self.work_bytes, dtype=torch.uint8, device=self.device))
         else:
             # caller-provided views (for example slices of one arena); shapes checked
-            self.k, self.v, self.score, self.pos, self.len, self.work = buffers
-            want = {"k": (b, n_kv_heads, self.cap, head_dim), "v": (b, n_kv_heads, self.cap, head_dim),
-                    "score": (b, n_kv_heads, self.cap), "pos": (b, n_kv_heads, self.cap),
-                    "len": (b, n_kv_heads)}
-            for nm, shp in want.items():
+            for nm, x in zip((*want, "work"), buffers, strict=True):
+                setattr(self, nm, x)
+            for nm, (shp, _) in want.items():
                 x = getattr(self, nm)
                 if tuple(x.shape) != shp or not x.is_contiguous() or x.device != self.device:
                     raise ValueError(f"buffer {nm}: need a contiguous {shp} tensor on {self.device}")
             if self.work.numel() * self.work.element_size() < self.work_bytes:
                 raise ValueError("work buffer is smaller than bm_workspace_bytes")
-        self.cache = bm_cache(self.k.data_ptr(), self.v.data_ptr(), self.score.data_ptr(),
-                              self.pos.data_ptr(), self.len.data_ptr(),
-                              0 if self.work is None else self.work.data_ptr(),
-                              0 if self.work is None else self.work_bytes)
+        self.cache = self._cache()
         self.units = U
         # for every call's checks and stream: the current stream of a device index as an
         # integer, without the stream object that torch.cuda.current_stream makes
@@ -343,6 +382,31 @@ class PDAttention:
         self._settings = {}
         if init:
             self.reset()
+
+    # -- the cache ----------------------------------------------------------------
+    def _buffers(self) -> dict:
+        """Shape and element type of every tensor of the cache, in the order of ``buffers``."""
+        t, d = self.torch, self.dims
+        unit = (d.b, d.n_kv_heads)
+        row = (*unit, self.cap, d.head_dim)
+        return {"k": (row, self.tdtype), "v": (row, self.tdtype),
+                "score": (row[:3], t.float32), "pos": (row[:3], t.int32), "len": (unit, t.int32)}
+
+    def _work_ptr(self):
+        return (0, 0) if self.work is None else (self.work.data_ptr(), self.work_bytes)
+
+    def _cache(self):
+        return bm_cache(self.k.data_ptr(), self.v.data_ptr(), self.score.data_ptr(),
+                        self.pos.data_ptr(), self.len.data_ptr(), *self._work_ptr())
+
+    _workspace_bytes = staticmethod(bm_workspace_bytes)
+
+    def _new_context(self) -> int:
+        init = bm_init_static_workspace if self.static_workspace else bm_init
+        return init(self.dims, self.cache, self._stream())
+
+    def _resumed_context(self, length, next_pos) -> int:
+        return bm_resume(self.dims, self.cache, length, next_pos)
 
     # -- helpers ----------------------------------------------------------------
     def _stream(self) -> int:
@@ -402,8 +466,7 @@ class PDAttention:
         if self.ctx is not None:
             bm_destroy(self.ctx)
             self.ctx = None
-        init = bm_init_static_workspace if self.static_workspace else bm_init
-        self.ctx = init(self.dims, self.cache, self._stream())
+        self.ctx = self._new_context()
         self._apply_settings()
 
     def resume(self, length: int, next_pos: int) -> None:
@@ -412,7 +475,7 @@ class PDAttention:
         if self.ctx is not None:
             bm_destroy(self.ctx)
             self.ctx = None
-        self.ctx = bm_resume(self.dims, self.cache, length, next_pos)
+        self.ctx = self._resumed_context(length, next_pos)
         self._apply_settings()
 
     def _block_args(self, t0, n_tok, q, k, v, o, row):
@@ -557,6 +620,70 @@ class PDAttention:
             pass
 
 
+class PDAttentionKV4(PDAttention):
+    """PDAttention over a cache held in 4 bits (include/bm_kv4.h), every call included:
+    a call's own K and V rows are attended to as given and stored in 4 bits,
+    earlier entries as they read back.
+
+    ``k``, ``v`` hold codes, uint8 ``[b, n_kv_heads, cap, d / 2]``, ``k_scale``, ``v_scale``
+    their scale bytes, uint8 ``[b, n_kv_heads, cap, d / 32]``.  ``buffers``: those four, then
+    score, pos, len and work.  ``write_rows`` and ``read_rows`` convert rows of the
+    configured dtype to and from slots.
+    """
+
+    def __init__(self, *, static_workspace=False, **kw):
+        if static_workspace:
+            raise ValueError("a 4-bit cache needs a caller-allocated workspace")
+        super().__init__(**kw)
+
+    def _buffers(self) -> dict:
+        t, d = self.torch, self.dims
+        plain = super()._buffers()
+        slots = plain["score"][0]
+        code, scale = (*slots, d.head_dim // 2), (*slots, d.head_dim // BM_KV4_GROUP)
+        return {"k": (code, t.uint8), "v": (code, t.uint8), "k_scale": (scale, t.uint8),
+                "v_scale": (scale, t.uint8), **{x: plain[x] for x in ("score", "pos", "len")}}
+
+    def _cache(self):
+        return bm_kv4_cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
+                            self.v_scale.data_ptr(), self.score.data_ptr(), self.pos.data_ptr(),
+                            self.len.data_ptr(), *self._work_ptr())
+
+    _workspace_bytes = staticmethod(bm_kv4_workspace_bytes)
+
+    def _new_context(self) -> int:
+        return bm_kv4_init(self.dims, self.cache, self._stream())
+
+    def _resumed_context(self, length, next_pos) -> int:
+        return bm_kv4_resume(self.dims, self.cache, length, next_pos)
+
+    def _rows(self, k, v):
+        for x, nm in ((k, "k"), (v, "v")):
+            self._check_tensor(x, self.dims.n_kv_heads, nm)
+        if k.shape[2] != v.shape[2]:
+            raise ValueError("k and v need the same number of rows")
+        return k.shape[2]
+
+    def write_rows(self, slot0, k, v) -> None:
+        """Store every row of k, v ``[b, n_kv_heads, n, d]`` in slots slot0 .. slot0 + n - 1 of
+        its unit; scores, positions and lengths are left as they are."""
+        n = self._rows(k, v)
+        bm_kv4_write(self.dims, self.cache, slot0, n, k.data_ptr(), v.data_ptr(), n, self._stream())
+
+    def read_rows(self, slot0, n, k=None, v=None):
+        """Slots slot0 .. slot0 + n - 1 of every unit as k, v ``[b, n_kv_heads, n, d]`` of the
+        configured dtype (new tensors unless given), which are returned."""
+        t, d = self.torch, self.dims
+        if k is None:
+            k = t.empty((d.b, d.n_kv_heads, n, d.head_dim), dtype=self.tdtype, device=self.device)
+        if v is None:
+            v = t.empty_like(k)
+        if self._rows(k, v) != n:
+            raise ValueError(f"k and v need {n} rows")
+        bm_kv4_read(self.dims, self.cache, slot0, n, k.data_ptr(), v.data_ptr(), n, self._stream())
+        return k, v
+
+
 # ---------------------------------------------------------------------------
 # synthetic inputs of the layer stack (bm_synth.h)
 # ---------------------------------------------------------------------------
@@ -593,22 +720,34 @@ def _align(n: int, a: int = 256) -> int:
     return (n + a - 1) // a * a
 
 
-def stack_layer_bytes(*, b, kv_max, block, n_kv_heads, head_dim, dtype) -> int:
-    """Device bytes of one layer's cache (K, V, score, pos, len), 256-byte aligned."""
+def _row_planes(head_dim, dtype, kv_bits) -> tuple:
+    """Bytes of an entry's K row and, held in 4 bits, of its scales."""
+    if kv_bits == 16:
+        return (head_dim * (4 if dtype in ("f32", BM_F32) else 2),)
+    if kv_bits == 4:
+        return (head_dim // 2, head_dim // BM_KV4_GROUP)
+    raise ValueError("kv_bits is 16 (rows of the element type) or 4")
+
+
+def stack_layer_bytes(*, b, kv_max, block, n_kv_heads, head_dim, dtype, kv_bits=16) -> int:
+    """Device bytes of one layer's cache (K, V and their scales, score, pos, len),
+    256-byte aligned."""
     cap = kv_max + block
-    es = 4 if dtype in ("f32", BM_F32) else 2
     rows = b * n_kv_heads * cap
-    return (2 * _align(rows * head_dim * es) + 2 * _align(rows * 4) + _align(b * n_kv_heads * 4))
+    planes = _row_planes(head_dim, dtype, kv_bits)
+    return (sum(2 * _align(rows * x) for x in planes) + 2 * _align(rows * 4)
+            + _align(b * n_kv_heads * 4))
 
 
 class PDStack:
     """``n_layers`` independent bounded caches (the attention layers of one
     model, each with its own scores and evictions) carved from one device
     arena, sharing one workspace (its contents never outlive a call).  Layer
-    ``l`` is driven through ``self.layers[l]``, a ``PDAttention``."""
+    ``l`` is driven through ``self.layers[l]``, a ``PDAttention`` (``kv_bits`` 4: a
+    ``PDAttentionKV4``)."""
 
     def __init__(self, *, n_layers, b, s, kv_max, block, max_gen, n_heads, n_kv_heads, head_dim,
-                 dtype="bf16", sm_scale=0.0, device="cuda"):
+                 dtype="bf16", sm_scale=0.0, device="cuda", kv_bits=16):
         import torch
 
         dims = make_dims(b=b, s=s, kv_max=kv_max, block=block, max_gen=max_gen, n_heads=n_heads,
@@ -618,11 +757,11 @@ class PDStack:
         if dev.type == "cuda" and dev.index is None:
             dev = torch.device("cuda", torch.cuda.current_device())
         tdt = torch.float32 if dims.dtype == BM_F32 else torch.bfloat16
-        es = 4 if dims.dtype == BM_F32 else 2
         cap = kv_max + block
         per_layer = stack_layer_bytes(b=b, kv_max=kv_max, block=block, n_kv_heads=n_kv_heads,
-                                      head_dim=head_dim, dtype=dims.dtype)
-        work_bytes = bm_workspace_bytes(dims)
+                                      head_dim=head_dim, dtype=dims.dtype, kv_bits=kv_bits)
+        layer_type = PDAttentionKV4 if kv_bits == 4 else PDAttention
+        work_bytes = layer_type._workspace_bytes(dims)
         self.arena_bytes = n_layers * per_layer + _align(work_bytes)
         self.arena = torch.empty(self.arena_bytes, dtype=torch.uint8, device=dev)
         work = self.arena[n_layers * per_layer:n_layers * per_layer + work_bytes]
@@ -637,16 +776,19 @@ class PDStack:
                 off += _align(nbytes)
                 return x
 
-            kk = take(rows * head_dim * es, tdt, (b, n_kv_heads, cap, head_dim))
-            vv = take(rows * head_dim * es, tdt, (b, n_kv_heads, cap, head_dim))
+            kv = []
+            for row in _row_planes(head_dim, dims.dtype, kv_bits):
+                dt = torch.uint8 if kv_bits == 4 else tdt
+                shape = (b, n_kv_heads, cap, row // dt.itemsize)
+                kv += [take(rows * row, dt, shape), take(rows * row, dt, shape)]
             sc = take(rows * 4, torch.float32, (b, n_kv_heads, cap))
             ps = take(rows * 4, torch.int32, (b, n_kv_heads, cap))
             ln = take(b * n_kv_heads * 4, torch.int32, (b, n_kv_heads))
-            self.layers.append(PDAttention(b=b, s=s, kv_max=kv_max, block=block, max_gen=max_gen,
-                                           n_heads=n_heads, n_kv_heads=n_kv_heads,
-                                           head_dim=head_dim, dtype=dtype, sm_scale=sm_scale,
-                                           device=dev, init=False,
-                                           buffers=(kk, vv, sc, ps, ln, work)))
+            self.layers.append(layer_type(b=b, s=s, kv_max=kv_max, block=block, max_gen=max_gen,
+                                          n_heads=n_heads, n_kv_heads=n_kv_heads,
+                                          head_dim=head_dim, dtype=dtype, sm_scale=sm_scale,
+                                          device=dev, init=False,
+                                          buffers=(*kv, sc, ps, ln, work)))
         self.n_layers = n_layers
         self.device = dev
 
@@ -660,7 +802,7 @@ class PDStack:
 
 
 def stack_bytes(*, b, n_layers, s, kv_max, block, max_gen, n_heads, n_kv_heads, head_dim,
-                dtype) -> int:
+                dtype, kv_bits=16) -> int:
     """Device bytes a P&D run of the layer stack needs at batch b: every layer's
     bounded cache, the shared workspace, and the reusable input/output buffers
     of one prefill block and one decode row."""
@@ -668,8 +810,8 @@ def stack_bytes(*, b, n_layers, s, kv_max, block, max_gen, n_heads, n_kv_heads, 
     dims = make_dims(b=b, s=s, kv_max=kv_max, block=block, max_gen=max_gen, n_heads=n_heads,
                      n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=dtype)
     caches = n_layers * stack_layer_bytes(b=b, kv_max=kv_max, block=block, n_kv_heads=n_kv_heads,
-                                          head_dim=head_dim, dtype=dtype)
-    work = _align(bm_workspace_bytes(dims))
+                                          head_dim=head_dim, dtype=dtype, kv_bits=kv_bits)
+    work = _align(bm_kv4_workspace_bytes(dims) if kv_bits == 4 else bm_workspace_bytes(dims))
     rows = block + 1
     io = rows * b * (2 * n_heads + 2 * n_kv_heads) * head_dim * es
     return caches + work + io

@@ -32,6 +32,11 @@ struct bm_ctx {
   bool scores_valid;  // no block has run without accumulation
   const int32_t* pad; // device [b] left pad tokens per sample, or null
   hipEvent_t split;   // recorded between a block's attention and its score/cut launches, or null
+  // a cache held in 4 bits (bm_kv4.h): cache.k and cache.v are codes, these their scales,
+  // and a prefill block reads the cached rows back into the workspace at these offsets
+  void* k_scale;      // null: rows of dims.dtype
+  void* v_scale;
+  size_t rows_k_off, rows_v_off;
 };
 
 namespace {
@@ -149,7 +154,8 @@ BM_EXPORT size_t bm_workspace_bytes(const bm_dims* dims) {
 
 namespace {
 
-int make_ctx(const bm_dims* dims, const bm_cache* cache, bm_ctx** out) {
+// work_need: bytes of workspace the context's calls use
+int make_ctx(const bm_dims* dims, const bm_cache* cache, size_t work_need, bm_ctx** out) {
   int st = check_dims(dims);
   if (st != BM_OK) return st;
   if (!cache || !out) return fail(BM_ERR_INVALID_ARG, "cache or out is null");
@@ -159,9 +165,8 @@ int make_ctx(const bm_dims* dims, const bm_cache* cache, bm_ctx** out) {
     return fail(BM_ERR_INVALID_ARG, "k, v and work must be 16-byte aligned");
   if (((uintptr_t)cache->score | (uintptr_t)cache->pos | (uintptr_t)cache->len) & 3)
     return fail(BM_ERR_INVALID_ARG, "score, pos and len must be 4-byte aligned");
-  const bm::Layout lay = bm::workspace_layout(*dims);
-  if (cache->work_bytes < lay.total)
-    return fail(BM_ERR_INVALID_ARG, "work_bytes %zu < required %zu", cache->work_bytes, lay.total);
+  if (cache->work_bytes < work_need)
+    return fail(BM_ERR_INVALID_ARG, "work_bytes %zu < required %zu", cache->work_bytes, work_need);
   bm_ctx* c = new (std::nothrow) bm_ctx;
   if (!c) return fail(BM_ERR_INVALID_ARG, "out of host memory");
   c->dims = *dims;
@@ -171,7 +176,7 @@ int make_ctx(const bm_dims* dims, const bm_cache* cache, bm_ctx** out) {
   c->units = dims->b * dims->n_kv_heads;
   c->elem_bytes = dims->dtype == BM_BF16 ? 2 : 4;
   c->sm_scale = eff_scale(*dims);
-  c->lay = lay;
+  c->lay = bm::workspace_layout(*dims);
   c->len = 0;
   c->next_pos = 0;
   c->last_pos = -1;
@@ -182,6 +187,8 @@ int make_ctx(const bm_dims* dims, const bm_cache* cache, bm_ctx** out) {
   c->scores_valid = true;
   c->pad = nullptr;
   c->split = nullptr;
+  c->k_scale = c->v_scale = nullptr;
+  c->rows_k_off = c->rows_v_off = 0;
   *out = c;
   return BM_OK;
 }
@@ -190,20 +197,48 @@ char* work_at(const bm_ctx* c, size_t off) { return static_cast<char*>(c->cache.
 
 }  // namespace
 
-BM_EXPORT int bm_init(const bm_dims* dims, const bm_cache* cache, hipStream_t stream,
-                      bm_ctx** out) {
-  if (out) *out = nullptr;
-  bm_ctx* c = nullptr;
-  const int st = make_ctx(dims, cache, &c);
-  if (st != BM_OK) return st;
+namespace {
+
+// Enqueue the zeroing of a new context's cache, or drop the context.
+int start(bm_ctx* c, hipStream_t stream, bm_ctx** out) {
   const size_t n_score = (size_t)c->units * c->cap;
-  const hipError_t e = bm::launch_reset(cache->score, cache->len, n_score, (size_t)c->units, stream);
+  const hipError_t e =
+      bm::launch_reset(c->cache.score, c->cache.len, n_score, (size_t)c->units, stream);
   if (e != hipSuccess) {
     delete c;
     return hip_fail(e, "reset launch");
   }
   *out = c;
   return ok();
+}
+
+// Put a new context at `len` entries and position next_pos, or drop it.
+int place(bm_ctx* c, int32_t len, int32_t next_pos, bm_ctx** out) {
+  if (len < 0 || len > c->cap || next_pos < 0 || next_pos > c->dims.s + c->dims.max_gen ||
+      len > next_pos) {
+    delete c;
+    return fail(BM_ERR_INVALID_ARG, "resume state len=%d next_pos=%d is not reachable", len,
+                next_pos);
+  }
+  c->len = len;
+  c->next_pos = next_pos;
+  c->last_pos = next_pos - 1;
+  *out = c;
+  return ok();
+}
+
+size_t plain_work_bytes(const bm_dims* d) {
+  return check_dims(d) == BM_OK ? bm::workspace_layout(*d).total : 0;
+}
+
+}  // namespace
+
+BM_EXPORT int bm_init(const bm_dims* dims, const bm_cache* cache, hipStream_t stream,
+                      bm_ctx** out) {
+  if (out) *out = nullptr;
+  bm_ctx* c = nullptr;
+  const int st = make_ctx(dims, cache, plain_work_bytes(dims), out ? &c : nullptr);
+  return st == BM_OK ? start(c, stream, out) : st;
 }
 
 // ---------------------------------------------------------------------------
@@ -268,19 +303,136 @@ BM_EXPORT int bm_resume(const bm_dims* dims, const bm_cache* cache, int32_t len,
                         int32_t next_pos, bm_ctx** out) {
   if (out) *out = nullptr;
   bm_ctx* c = nullptr;
-  const int st = make_ctx(dims, cache, &c);
+  const int st = make_ctx(dims, cache, plain_work_bytes(dims), out ? &c : nullptr);
+  return st == BM_OK ? place(c, len, next_pos, out) : st;
+}
+
+// ---------------------------------------------------------------------------
+// a cache held in 4 bits (bm_kv4.h)
+// ---------------------------------------------------------------------------
+namespace {
+
+// The workspace of a 4-bit context: that of batchmax.h, then one layer's cached rows in
+// the element type.  Returns the bytes; the rows' offsets in *k_off and *v_off.
+size_t kv4_layout(const bm_dims& d, size_t* k_off, size_t* v_off) {
+  const size_t base = align256(bm::workspace_layout(d).total);
+  const size_t rows = align256((size_t)d.b * d.n_kv_heads * ((size_t)d.kv_max + d.block) *
+                               d.head_dim * (d.dtype == BM_BF16 ? 2 : 4));
+  *k_off = base;
+  *v_off = base + rows;
+  return base + 2 * rows;
+}
+
+int kv4_ctx(const bm_dims* dims, const bm_kv4_cache* cache, bm_ctx** out) {
+  const int st = check_dims(dims);
   if (st != BM_OK) return st;
-  if (len < 0 || len > c->cap || next_pos < 0 || next_pos > dims->s + dims->max_gen ||
-      len > next_pos) {
-    delete c;
-    return fail(BM_ERR_INVALID_ARG, "resume state len=%d next_pos=%d is not reachable", len,
-                next_pos);
-  }
-  c->len = len;
-  c->next_pos = next_pos;
-  c->last_pos = next_pos - 1;
-  *out = c;
+  if (!cache) return fail(BM_ERR_INVALID_ARG, "cache or out is null");
+  if (!cache->k_scale || !cache->v_scale)
+    return fail(BM_ERR_INVALID_ARG, "a cache pointer is null");
+  if (((uintptr_t)cache->k_scale | (uintptr_t)cache->v_scale) & 3)
+    return fail(BM_ERR_INVALID_ARG, "k_scale and v_scale must be 4-byte aligned");
+  const bm_cache plain = {cache->k,   cache->v,    cache->score,     cache->pos,
+                          cache->len, cache->work, cache->work_bytes};
+  size_t k_off, v_off;
+  const int made = make_ctx(dims, &plain, kv4_layout(*dims, &k_off, &v_off), out);
+  if (made != BM_OK) return made;
+  (*out)->k_scale = cache->k_scale;
+  (*out)->v_scale = cache->v_scale;
+  (*out)->rows_k_off = k_off;
+  (*out)->rows_v_off = v_off;
+  return BM_OK;
+}
+
+// Rows between buffers of the element type and slots of a 4-bit cache.
+int kv4_rows(const bm_dims* dims, const bm_kv4_cache* cache, int32_t slot0, int32_t n,
+             const void* k, const void* v, int32_t seq_ld, bool write, hipStream_t stream) {
+  const int st = check_dims(dims);
+  if (st != BM_OK) return st;
+  if (!cache) return fail(BM_ERR_INVALID_ARG, "cache is null");
+  if (!cache->k || !cache->v || !cache->k_scale || !cache->v_scale)
+    return fail(BM_ERR_INVALID_ARG, "a cache pointer is null");
+  if (((uintptr_t)cache->k | (uintptr_t)cache->v) & 15)
+    return fail(BM_ERR_INVALID_ARG, "the cache's k and v must be 16-byte aligned");
+  if (((uintptr_t)cache->k_scale | (uintptr_t)cache->v_scale) & 3)
+    return fail(BM_ERR_INVALID_ARG, "k_scale and v_scale must be 4-byte aligned");
+  if (slot0 < 0 || n < 0) return fail(BM_ERR_INVALID_ARG, "slot0=%d n=%d", slot0, n);
+  if ((int64_t)slot0 + n > (int64_t)dims->kv_max + dims->block)
+    return fail(BM_ERR_CAPACITY, "slots [%d, %lld) exceed cap %d", slot0, (long long)slot0 + n,
+                dims->kv_max + dims->block);
+  if (n == 0) return ok();
+  if (!k || !v) return fail(BM_ERR_INVALID_ARG, "k or v is null");
+  if (((uintptr_t)k | (uintptr_t)v) & 15)
+    return fail(BM_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
+  if (seq_ld < n) return fail(BM_ERR_INVALID_ARG, "seq_ld %d < n %d", seq_ld, n);
+  bm::Kv4RowsArgs a;
+  a.k = k;
+  a.v = v;
+  a.kq = cache->k;
+  a.vq = cache->v;
+  a.ks = cache->k_scale;
+  a.vs = cache->v_scale;
+  a.seq_ld = seq_ld;
+  a.units = dims->b * dims->n_kv_heads;
+  a.cap = dims->kv_max + dims->block;
+  a.slot0 = slot0;
+  a.n = n;
+  const hipError_t e = bm::launch_kv4_rows(a, write, dims->dtype, dims->head_dim, stream);
+  if (e != hipSuccess) return hip_fail(e, write ? "4-bit write launch" : "4-bit read launch");
   return ok();
+}
+
+// The same on a context's cache, unchecked.
+hipError_t ctx_rows(const bm_ctx* ctx, int slot0, int n, const void* k, const void* v,
+                    int64_t seq_ld, bool write, hipStream_t stream) {
+  bm::Kv4RowsArgs a;
+  a.k = k;
+  a.v = v;
+  a.kq = ctx->cache.k;
+  a.vq = ctx->cache.v;
+  a.ks = ctx->k_scale;
+  a.vs = ctx->v_scale;
+  a.seq_ld = seq_ld;
+  a.units = ctx->units;
+  a.cap = ctx->cap;
+  a.slot0 = slot0;
+  a.n = n;
+  return bm::launch_kv4_rows(a, write, ctx->dims.dtype, ctx->dims.head_dim, stream);
+}
+
+}  // namespace
+
+BM_EXPORT size_t bm_kv4_workspace_bytes(const bm_dims* dims) {
+  if (check_dims(dims) != BM_OK) return 0;
+  size_t k_off, v_off;
+  return kv4_layout(*dims, &k_off, &v_off);
+}
+
+BM_EXPORT int bm_kv4_init(const bm_dims* dims, const bm_kv4_cache* cache, hipStream_t stream,
+                          bm_ctx** out) {
+  if (out) *out = nullptr;
+  bm_ctx* c = nullptr;
+  if (!out) return fail(BM_ERR_INVALID_ARG, "cache or out is null");
+  const int st = kv4_ctx(dims, cache, &c);
+  return st == BM_OK ? start(c, stream, out) : st;
+}
+
+BM_EXPORT int bm_kv4_resume(const bm_dims* dims, const bm_kv4_cache* cache, int32_t len,
+                            int32_t next_pos, bm_ctx** out) {
+  if (out) *out = nullptr;
+  bm_ctx* c = nullptr;
+  if (!out) return fail(BM_ERR_INVALID_ARG, "cache or out is null");
+  const int st = kv4_ctx(dims, cache, &c);
+  return st == BM_OK ? place(c, len, next_pos, out) : st;
+}
+
+BM_EXPORT int bm_kv4_write(const bm_dims* dims, const bm_kv4_cache* cache, int32_t slot0, int32_t n,
+                           const void* k, const void* v, int32_t seq_ld, hipStream_t stream) {
+  return kv4_rows(dims, cache, slot0, n, k, v, seq_ld, true, stream);
+}
+
+BM_EXPORT int bm_kv4_read(const bm_dims* dims, const bm_kv4_cache* cache, int32_t slot0, int32_t n,
+                          void* k, void* v, int32_t seq_ld, hipStream_t stream) {
+  return kv4_rows(dims, cache, slot0, n, k, v, seq_ld, false, stream);
 }
 
 namespace {
@@ -314,8 +466,10 @@ int prefill_args(bm_ctx* ctx, int32_t t0, int32_t n_tok, const void* q, const vo
   a.kin = k;
   a.vin = v;
   a.o = o;
-  a.kc = ctx->cache.k;
-  a.vc = ctx->cache.v;
+  // the rows that the attention reads and appends to: the cache's own, or those that
+  // attend() reads back from 4 bits into the workspace
+  a.kc = ctx->k_scale ? static_cast<void*>(work_at(ctx, ctx->rows_k_off)) : ctx->cache.k;
+  a.vc = ctx->k_scale ? static_cast<void*>(work_at(ctx, ctx->rows_v_off)) : ctx->cache.v;
   a.pos = ctx->cache.pos;
   a.score = ctx->cache.score;
   a.len = ctx->cache.len;
@@ -339,6 +493,25 @@ int prefill_args(bm_ctx* ctx, int32_t t0, int32_t n_tok, const void* q, const vo
   return BM_OK;
 }
 
+// Enqueue a checked block's attention (a 4-bit cache: between the reading of its rows
+// and the storing of the block's) and the caller's event behind it.
+int attend(bm_ctx* ctx, const bm::PrefillArgs& a, hipStream_t stream) {
+  hipError_t e;
+  if (ctx->k_scale && a.len0 > 0) {
+    e = ctx_rows(ctx, 0, a.len0, a.kc, a.vc, ctx->cap, false, stream);
+    if (e != hipSuccess) return hip_fail(e, "4-bit read launch");
+  }
+  e = bm::launch_prefill(a, ctx->dims.dtype, ctx->dims.head_dim, ctx->group, stream);
+  if (e != hipSuccess) return hip_fail(e, "prefill launch");
+  if (ctx->k_scale) {
+    e = ctx_rows(ctx, a.len0, a.n_tok, a.kin, a.vin, a.seq_ld, true, stream);
+    if (e != hipSuccess) return hip_fail(e, "4-bit write launch");
+  }
+  if (ctx->split && (e = hipEventRecord(ctx->split, stream)) != hipSuccess)
+    return hip_fail(e, "split event record");
+  return BM_OK;
+}
+
 void advance(bm_ctx* ctx, int32_t t0, int32_t n_tok) {
   ctx->len += n_tok;
   ctx->next_pos = t0 + n_tok;
@@ -352,13 +525,11 @@ BM_EXPORT int bm_prefill_block(bm_ctx* ctx, int32_t t0, int32_t n_tok, const voi
                                const void* k, const void* v, void* o, int32_t seq_ld,
                                hipStream_t stream) {
   bm::PrefillArgs a;
-  const int st = prefill_args(ctx, t0, n_tok, q, k, v, o, seq_ld, &a);
+  int st = prefill_args(ctx, t0, n_tok, q, k, v, o, seq_ld, &a);
   if (st != BM_OK) return st;
-  hipError_t e = bm::launch_prefill(a, ctx->dims.dtype, ctx->dims.head_dim, ctx->group, stream);
-  if (e != hipSuccess) return hip_fail(e, "prefill launch");
-  if (ctx->split && (e = hipEventRecord(ctx->split, stream)) != hipSuccess)
-    return hip_fail(e, "split event record");
-  e = bm::launch_score_reduce(a, stream);
+  st = attend(ctx, a, stream);
+  if (st != BM_OK) return st;
+  const hipError_t e = bm::launch_score_reduce(a, stream);
   if (e != hipSuccess) return hip_fail(e, "score reduce launch");
   advance(ctx, t0, n_tok);
   return ok();
@@ -375,10 +546,9 @@ BM_EXPORT int bm_prefill_block_cut(bm_ctx* ctx, int32_t t0, int32_t n_tok, const
   if (cuts && (!ctx->scores_valid || !ctx->accumulate) && ctx->rule != BM_RANK_RECENT)
     return fail(BM_ERR_ORDER,
                 "a block ran without score accumulation: only BM_RANK_RECENT can rank this cache");
-  hipError_t e = bm::launch_prefill(a, ctx->dims.dtype, ctx->dims.head_dim, ctx->group, stream);
-  if (e != hipSuccess) return hip_fail(e, "prefill launch");
-  if (ctx->split && (e = hipEventRecord(ctx->split, stream)) != hipSuccess)
-    return hip_fail(e, "split event record");
+  st = attend(ctx, a, stream);
+  if (st != BM_OK) return st;
+  hipError_t e;
   if (n > bm::kMaxCap) {
     // too many entries for the one-workgroup cut: fold, then the two-kernel cut
     e = bm::launch_score_reduce(a, stream);
@@ -408,6 +578,8 @@ BM_EXPORT int bm_prefill_block_cut(bm_ctx* ctx, int32_t t0, int32_t n_tok, const
   c.elem_bytes = ctx->elem_bytes;
   c.rule = ctx->rule;
   c.lastw = reinterpret_cast<float*>(work_at(ctx, ctx->lay.lastw_off));
+  c.ks = ctx->k_scale;
+  c.vs = ctx->v_scale;
   e = bm::launch_fold_cut(a, c, bm::positions_per_wg(ctx->group), stream);
   if (e != hipSuccess) return hip_fail(e, "fold-cut launch");
   advance(ctx, t0, n_tok);
@@ -446,7 +618,7 @@ constexpr int kOneLaunchEntries = 2048;
 constexpr int kOneLaunchUnits = 256;      // a workgroup for every compute unit
 
 bool one_launch_cut(const bm::EvictArgs& a, int max_moves) {
-  const int64_t bytes = (int64_t)max_moves * 2 * a.head_dim * a.elem_bytes;
+  const int64_t bytes = (int64_t)max_moves * 2 * a.row_bytes();
   const bool idle = a.n > kOneLaunchEntries && a.units < kOneLaunchUnits;
   return a.n <= bm::kMaxCap && bytes <= (idle ? kOneLaunchMoveBytes / 2 : kOneLaunchMoveBytes);
 }
@@ -473,6 +645,8 @@ int cut_to(bm_ctx* ctx, int target, int32_t curr_id, hipStream_t stream) {
   a.elem_bytes = ctx->elem_bytes;
   a.rule = ctx->rule;
   a.lastw = reinterpret_cast<float*>(work_at(ctx, ctx->lay.lastw_off));
+  a.ks = ctx->k_scale;
+  a.vs = ctx->v_scale;
   const int n_evict = ctx->len - target;
   const int max_moves = n_evict < target ? n_evict : target;
   hipError_t e;
@@ -553,6 +727,53 @@ BM_EXPORT int bm_set_decode_removal(bm_ctx* ctx, int32_t p) {
   return ok();
 }
 
+namespace {
+
+// A checked decode step over a 4-bit cache; outputs_only: more entries than a scoring
+// step takes, split over key chunks whose partial results go where a prefill block
+// reads the cached rows back (at most 520 bytes for each of 512 rows of 256 or more).
+int kv4_step(bm_ctx* ctx, int32_t pos, const void* q, const void* k, const void* v, void* o,
+             int32_t seq_ld, bool outputs_only, hipStream_t stream) {
+  bm::Kv4DecodeArgs a;
+  a.q = q;
+  a.kin = k;
+  a.vin = v;
+  a.o = o;
+  a.kq = ctx->cache.k;
+  a.vq = ctx->cache.v;
+  a.ks = ctx->k_scale;
+  a.vs = ctx->v_scale;
+  a.score = ctx->cache.score;
+  a.pos = ctx->cache.pos;
+  a.len = ctx->cache.len;
+  a.part = reinterpret_cast<float*>(work_at(ctx, ctx->rows_k_off));
+  a.seq_ld = seq_ld;
+  a.n_heads = ctx->dims.n_heads;
+  a.n_kv_heads = ctx->dims.n_kv_heads;
+  a.cap = ctx->cap;
+  a.len0 = ctx->len;
+  a.kv_max = ctx->kv_dec;
+  a.cur_pos = pos;
+  a.units = ctx->units;
+  a.nsplit = outputs_only ? bm::kv4_long_splits(ctx->len) : 0;
+  a.rule = ctx->rule;
+  a.pad = ctx->pad;
+  a.lastw = ctx->rule == BM_RANK_TOVA ? reinterpret_cast<float*>(work_at(ctx, ctx->lay.lastw_off))
+                                      : nullptr;
+  a.scale_log2 = ctx->sm_scale * 1.4426950408889634f;
+  const hipError_t e =
+      outputs_only
+          ? bm::launch_kv4_long(a, ctx->dims.dtype, ctx->dims.head_dim, ctx->group, stream)
+          : bm::launch_kv4_decode(a, ctx->dims.dtype, ctx->dims.head_dim, ctx->group, stream);
+  if (e != hipSuccess) return hip_fail(e, "4-bit decode launch");
+  if (outputs_only || ctx->len < ctx->kv_dec) ctx->len += 1;
+  ctx->next_pos = pos + 1;
+  ctx->last_pos = pos;
+  return ok();
+}
+
+}  // namespace
+
 BM_EXPORT int bm_decode_step(bm_ctx* ctx, int32_t pos, const void* q, const void* k,
                              const void* v, void* o, int32_t seq_ld, hipStream_t stream) {
   if (!ctx) return fail(BM_ERR_INVALID_ARG, "ctx is null");
@@ -595,6 +816,7 @@ BM_EXPORT int bm_decode_step(bm_ctx* ctx, int32_t pos, const void* q, const void
                   "a decode step over %d > %d entries computes outputs only: it needs score "
                   "accumulation off and no removal",
                   len_att + 1, bm::kMaxDecodeLen);
+    if (ctx->k_scale) return kv4_step(ctx, pos, q, k, v, o, seq_ld, true, stream);
     const int nsplit = bm::long_decode_splits(len_att);
     const size_t need = (size_t)ctx->units * nsplit * ctx->group * (ctx->dims.head_dim + 2);
     const size_t have = (size_t)ctx->units * ctx->lay.npt * ctx->cap;
@@ -634,6 +856,7 @@ BM_EXPORT int bm_decode_step(bm_ctx* ctx, int32_t pos, const void* q, const void
     const int st = cut_to(ctx, target, ctx->last_pos, stream);
     if (st != BM_OK) return st;
   }
+  if (ctx->k_scale) return kv4_step(ctx, pos, q, k, v, o, seq_ld, false, stream);
   bm::DecodeArgs a;
   a.q = q;
   a.kin = k;

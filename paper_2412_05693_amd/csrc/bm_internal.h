@@ -7,6 +7,7 @@
 #include <stdint.h>
 
 #include "batchmax.h"
+#include "bm_kv4.h"
 #include "bm_probe.h"
 #include "bm_synth.h"
 
@@ -91,6 +92,11 @@ struct EvictArgs {
   int cap, n, kv_max, curr_id, units, head_dim, elem_bytes;
   int rule;           // bm_rank_rule
   float* lastw;       // [U, cap] last query's weights (moved with the entries), or null
+  // a cache held in 4 bits: kc and vc are rows of head_dim / 2 bytes (elem_bytes 0), and
+  // every entry has head_dim / 32 scale bytes in each of these
+  void* ks = nullptr;
+  void* vs = nullptr;
+  __host__ __device__ int row_bytes() const { return ks ? head_dim / 2 : head_dim * elem_bytes; }
 };
 
 struct DecodeArgs {
@@ -128,6 +134,40 @@ struct LongDecodeArgs {
   float scale_log2;
 };
 
+// A step over a cache held in 4 bits, scoring or split over key chunks.
+struct Kv4DecodeArgs {
+  const void* q;      // [b, H, seq_ld, D] row of this step
+  const void* kin;    // [b, Hk, seq_ld, D]
+  const void* vin;
+  void* o;
+  void* kq;           // codes [U, cap, D / 2]
+  void* vq;
+  void* ks;           // scales [U, cap, D / 32]
+  void* vs;
+  float* score;
+  int32_t* pos;
+  int32_t* len;
+  float* part;        // [U][nsplit][G][D + 2] chunk partials (o, m, l) of a split step
+  int64_t seq_ld;
+  int n_heads, n_kv_heads, cap, len0, kv_max, cur_pos, units, nsplit;   // kv_max: the decode bound
+  int rule;           // bm_rank_rule
+  const int32_t* pad; // [b] left pad tokens per sample, or null
+  float* lastw;       // [U, cap] this step's weights are written here, or null
+  float scale_log2;
+};
+
+// Rows 0 .. n - 1 of [U, seq_ld, D] buffers to or from slots slot0 .. of a 4-bit cache.
+struct Kv4RowsArgs {
+  const void* k;      // (a read writes through them)
+  const void* v;
+  void* kq;
+  void* vq;
+  void* ks;
+  void* vs;
+  int64_t seq_ld;
+  int units, cap, slot0, n;
+};
+
 struct SynthArgs {
   void* q;
   void* k;
@@ -154,6 +194,13 @@ hipError_t launch_decode(const DecodeArgs& a, int dtype, int head_dim, int group
 int long_decode_splits(int len0);
 hipError_t launch_decode_long(const LongDecodeArgs& a, int dtype, int head_dim, int group,
                               hipStream_t stream);
+hipError_t launch_kv4_decode(const Kv4DecodeArgs& a, int dtype, int head_dim, int group,
+                             hipStream_t stream);
+int kv4_long_splits(int len0);
+hipError_t launch_kv4_long(const Kv4DecodeArgs& a, int dtype, int head_dim, int group,
+                           hipStream_t stream);
+hipError_t launch_kv4_rows(const Kv4RowsArgs& a, bool write, int dtype, int head_dim,
+                           hipStream_t stream);
 hipError_t launch_reset(float* score, int32_t* len, size_t n_score, size_t n_len,
                         hipStream_t stream);
 hipError_t launch_synth_qkv(const SynthArgs& a, hipStream_t stream);

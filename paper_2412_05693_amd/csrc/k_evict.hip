@@ -15,7 +15,8 @@
 // prefix counts, so the pairing is deterministic.
 //
 // K3 (compact_kernel), units x chunks of 32 moves: the i-th source moves into
-// the i-th hole (K row, V row, score, pos), 16-byte coalesced copies.  Sources
+// the i-th hole (K row, V row, score, pos; a 4-bit entry's scales), 16-byte
+// coalesced copies.  Sources
 // and holes are disjoint, so moves never overlap.
 #include "bm_internal.h"
 
@@ -256,6 +257,22 @@ __global__ void __launch_bounds__(256) select_kernel(EvictArgs a) {
   }
 }
 
+// a 4-bit entry's scales (2 or 4 bytes of K's and of V's) from slot s to slot d
+__device__ __forceinline__ void move_scales(const EvictArgs& a, int u, int s, int d) {
+  const int64_t row = (int64_t)u * a.cap;
+  if (a.head_dim == 128) {
+    uint32_t* const ks = static_cast<uint32_t*>(a.ks) + row;
+    uint32_t* const vs = static_cast<uint32_t*>(a.vs) + row;
+    ks[d] = ks[s];
+    vs[d] = vs[s];
+  } else {
+    uint16_t* const ks = static_cast<uint16_t*>(a.ks) + row;
+    uint16_t* const vs = static_cast<uint16_t*>(a.vs) + row;
+    ks[d] = ks[s];
+    vs[d] = vs[s];
+  }
+}
+
 __global__ void __launch_bounds__(256) compact_kernel(EvictArgs a, int nchunks) {
   constexpr int kMoves = 32;
   const int u = blockIdx.x / nchunks;
@@ -265,7 +282,7 @@ __global__ void __launch_bounds__(256) compact_kernel(EvictArgs a, int nchunks) 
   if (m0 >= m) return;
   const int32_t* holes = a.holes + (int64_t)u * a.cap;
   const int32_t* srcs = a.srcs + (int64_t)u * a.cap;
-  const int row_bytes = a.head_dim * a.elem_bytes;
+  const int row_bytes = a.row_bytes();
   const int cpr = row_bytes / 16;
   char* kc = static_cast<char*>(a.kc) + (int64_t)u * a.cap * row_bytes;
   char* vc = static_cast<char*>(a.vc) + (int64_t)u * a.cap * row_bytes;
@@ -288,6 +305,7 @@ __global__ void __launch_bounds__(256) compact_kernel(EvictArgs a, int nchunks) 
       a.score[(int64_t)u * a.cap + d] = a.score[(int64_t)u * a.cap + s];
       a.pos[(int64_t)u * a.cap + d] = a.pos[(int64_t)u * a.cap + s];
       if (a.rule == BM_RANK_TOVA) a.lastw[(int64_t)u * a.cap + d] = a.lastw[(int64_t)u * a.cap + s];
+      if (a.ks) move_scales(a, u, s, d);
     }
   }
 }
@@ -430,8 +448,8 @@ __global__ void __launch_bounds__(256) fold_cut_kernel(PrefillArgs pa, EvictArgs
 
   // 3. the moves: the i-th source into the i-th hole (disjoint slot ranges)
   const int m = min(min(hbase, sbase), list_len);
-  const int row_bytes = a.head_dim * a.elem_bytes;
-  const int lg = 31 - __clz(row_bytes / 16);   // 8, 16 or 32 chunks of 16 bytes per row
+  const int row_bytes = a.row_bytes();
+  const int lg = 31 - __clz(row_bytes / 16);   // 8, 16 or 32 chunks of 16 bytes per row (4 bits: 2 or 4)
   char* kc = static_cast<char*>(a.kc) + (int64_t)u * a.cap * row_bytes;
   char* vc = static_cast<char*>(a.vc) + (int64_t)u * a.cap * row_bytes;
   // four loads in flight per thread: a chunk's store would otherwise wait for its
@@ -462,6 +480,7 @@ __global__ void __launch_bounds__(256) fold_cut_kernel(PrefillArgs pa, EvictArgs
     score[dj] = FOLD ? sc[sj] : score[sj];
     pos[dj] = FOLD ? ps[sj] : pos[sj];
     if (last) last[dj] = FOLD ? lw[sj] : last[sj];
+    if (a.ks) move_scales(a, u, sj, dj);
   }
   if (tid == 0) a.len[u] = a.kv_max;
 }

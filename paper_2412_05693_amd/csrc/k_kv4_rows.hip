@@ -1,0 +1,148 @@
+// K8: rows into and out of a cache held in 4 bits (include/bm_kv4.h).
+//
+// A lane owns eight consecutive elements of a row, a quad of lanes one group of
+// 32 and its scale; it moves the K row's and the V row's eight elements of the
+// same slot.  HBM-bound: 16 (float32: 32) bytes in for 4.25 bytes out, or the
+// reverse, each read and written once.
+#include "bm_internal.h"
+#include "bm_kv4_dev.h"
+
+namespace bm {
+namespace {
+
+using kv4::u32x4;
+
+constexpr int kIters = 4;   // row pairs a lane moves, loads of all of them in flight
+
+// Item i of a launch is row i % n of unit i / n.  A workgroup's first item is split
+// with one 64-bit division, the rest with 32-bit ones (n <= 65536).
+template <int D>
+struct Items {
+  static constexpr int kLanes = D / 8;              // lanes per row
+  static constexpr int kRows = 256 / kLanes;        // rows a workgroup moves at a time
+  int64_t u0, left;
+  uint32_t r0, n;
+  int lane, first;
+  __device__ __forceinline__ Items(const Kv4RowsArgs& a) {
+    const int64_t i0 = (int64_t)blockIdx.x * (kRows * kIters);
+    u0 = i0 / a.n;
+    r0 = (uint32_t)(i0 - u0 * a.n);
+    n = (uint32_t)a.n;
+    left = (int64_t)a.units * a.n - i0;
+    lane = threadIdx.x % kLanes;
+    first = threadIdx.x / kLanes;
+  }
+  // unit and row of the lane's k-th item; false past the last (the unit and row are
+  // then those of the workgroup's first item, so that a load stays in bounds)
+  __device__ __forceinline__ bool at(int k, int64_t* u, uint32_t* r) const {
+    const uint32_t off = (uint32_t)(first + k * kRows);
+    const bool live = off < left;
+    const uint32_t t = r0 + (live ? off : 0);
+    const uint32_t q = t / n;
+    *u = u0 + q;
+    *r = t - q * n;
+    return live;
+  }
+};
+
+template <bool BF16, int D>
+__global__ void __launch_bounds__(256) kv4_write_kernel(Kv4RowsArgs a) {
+  constexpr int EB = BF16 ? 2 : 4;
+  const Items<D> it(a);
+  float x[kIters][2][8];
+  int64_t slot[kIters];
+  bool live[kIters];
+#pragma unroll
+  for (int k = 0; k < kIters; ++k) {
+    int64_t u;
+    uint32_t r;
+    live[k] = it.at(k, &u, &r);
+    slot[k] = u * a.cap + a.slot0 + r;
+    const int64_t src = ((u * a.seq_ld + r) * D + it.lane * 8) * EB;
+    kv4::load8<BF16>(static_cast<const char*>(a.k) + src, x[k][0]);
+    kv4::load8<BF16>(static_cast<const char*>(a.v) + src, x[k][1]);
+  }
+#pragma unroll
+  for (int k = 0; k < kIters; ++k) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      uint32_t byte;
+      const uint32_t c = kv4::quantise8(x[k][w], &byte);
+      if (live[k]) {
+        uint8_t* code = static_cast<uint8_t*>(w ? a.vq : a.kq) + slot[k] * (D / 2) + it.lane * 4;
+        *reinterpret_cast<uint32_t*>(code) = c;
+        if ((it.lane & 3) == 0)
+          (static_cast<uint8_t*>(w ? a.vs : a.ks))[slot[k] * (D / 32) + it.lane / 4] = (uint8_t)byte;
+      }
+    }
+  }
+}
+
+template <bool BF16, int D>
+__global__ void __launch_bounds__(256) kv4_read_kernel(Kv4RowsArgs a) {
+  constexpr int EB = BF16 ? 2 : 4;
+  const Items<D> it(a);
+  uint32_t c[kIters][2], s[kIters][2];
+  int64_t dst[kIters];
+  bool live[kIters];
+#pragma unroll
+  for (int k = 0; k < kIters; ++k) {
+    int64_t u;
+    uint32_t r;
+    live[k] = it.at(k, &u, &r);
+    const int64_t slot = u * a.cap + a.slot0 + r;
+    dst[k] = ((u * a.seq_ld + r) * D + it.lane * 8) * EB;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const uint8_t* code = static_cast<const uint8_t*>(w ? a.vq : a.kq) + slot * (D / 2) + it.lane * 4;
+      c[k][w] = *reinterpret_cast<const uint32_t*>(code);
+      s[k][w] = (static_cast<const uint8_t*>(w ? a.vs : a.ks))[slot * (D / 32) + it.lane / 4];
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kIters; ++k) {
+    if (!live[k]) continue;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      u32x4* p = reinterpret_cast<u32x4*>(const_cast<char*>(static_cast<const char*>(w ? a.v : a.k)) + dst[k]);
+      const u32x4 x = kv4::bf16x8_of(c[k][w], kv4::scale_of(s[k][w]));
+      if constexpr (BF16) {
+        *p = x;
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          u32x4 y;
+          y[0] = x[2 * i] << 16;
+          y[1] = x[2 * i] & 0xFFFF0000u;
+          y[2] = x[2 * i + 1] << 16;
+          y[3] = x[2 * i + 1] & 0xFFFF0000u;
+          p[i] = y;
+        }
+      }
+    }
+  }
+}
+
+template <bool BF16, int D>
+hipError_t launch_t(const Kv4RowsArgs& a, bool write, hipStream_t stream) {
+  constexpr int64_t per = Items<D>::kRows * kIters;
+  const int64_t blocks = ((int64_t)a.units * a.n + per - 1) / per;
+  if (blocks > 0xFFFFFF) return hipErrorInvalidValue;   // 2^32 threads a launch
+  const dim3 grid((unsigned)blocks);
+  if (write)
+    hipLaunchKernelGGL((kv4_write_kernel<BF16, D>), grid, dim3(256), 0, stream, a);
+  else
+    hipLaunchKernelGGL((kv4_read_kernel<BF16, D>), grid, dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv4_rows(const Kv4RowsArgs& a, bool write, int dtype, int head_dim,
+                           hipStream_t stream) {
+  if (dtype == BM_BF16)
+    return head_dim == 128 ? launch_t<true, 128>(a, write, stream) : launch_t<true, 64>(a, write, stream);
+  return head_dim == 128 ? launch_t<false, 128>(a, write, stream) : launch_t<false, 64>(a, write, stream);
+}
+
+}  // namespace bm
