@@ -269,7 +269,10 @@ def prepare(case, seed):
             b=b, s=max(1, last), kv_max=max(1, kv_max), block=block, max_gen=_MAX_GEN,
             n_heads=case["heads"], n_kv_heads=hk, head_dim=d, dtype=case["dtype"])
         n = _slots(case) if case["op"] in ("store", "read") else case["n"]
-        for name in ("k", "v", "k_scale", "v_scale", "score", "pos"):
+        if n:                          # (a row that is read back and written again stays the same)
+            dt = _DTYPES[case["dtype"]]
+            att.write_rows(0, *(_values(x[y][:, :, :n], x[y + "_scale"][:, :, :n]).to(dt) for y in "kv"))
+        for name in ("score", "pos"):
             getattr(att, name)[:, :, :n] = x[name][:, :, :n]
         att.len.fill_(case["n"])
         if x["pads"] is not None:
