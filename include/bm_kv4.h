@@ -36,12 +36,19 @@ extern "C" {
 /* Elements that share one scale. */
 #define BM_KV4_GROUP 32
 
-/* The cache, caller-owned device memory, all C-contiguous.
- *   k, v              [b, n_kv_heads, cap, head_dim / 2] bytes: element 2i in the
- *                     lower half of byte i, element 2i + 1 in the upper half;
- *                     16-byte aligned
- *   k_scale, v_scale  [b, n_kv_heads, cap, head_dim / 32] bytes; 4-byte aligned
- *   score, pos, len   as in bm_cache
+/* The cache, caller-owned device memory, all C-contiguous; slots =
+ * bm_kv4_slots(dims) is cap rounded up to a multiple of 64.  The layouts are what
+ * the attention's lanes load 16 bytes at a time; bm_kv4_write and bm_kv4_read
+ * convert rows, and a program need not know them.
+ *   k        [b, n_kv_heads, slots, head_dim / 2] bytes: element 2i in the lower
+ *            half of byte i, element 2i + 1 in the upper half
+ *   v        [b, n_kv_heads, slots / 4, head_dim / 8, 4] words of 32 bits: eight
+ *            codes each, lowest element first; four slots lie side by side
+ *   k_scale  [b, n_kv_heads, slots / 64, head_dim / 32, 64] bytes: slot 16 t + i
+ *            (t < 4, i < 16) of the 64 at byte 4 i + t
+ *   v_scale  the same with slot 16 t + 4 h + r (t, h, r < 4) at 16 h + 4 t + r
+ *   (these four 16-byte aligned)
+ *   score, pos, len   as in bm_cache, of cap slots
  *   work              bm_kv4_workspace_bytes(dims) bytes of scratch, 16-byte
  *                     aligned; contents need not survive between calls (but
  *                     for BM_RANK_TOVA's weights, as in bm_cache) */
@@ -56,6 +63,9 @@ typedef struct bm_kv4_cache {
   void* work;
   size_t work_bytes;
 } bm_kv4_cache;
+
+/* Slots a unit has in the planes of a 4-bit cache; -1 if dims are invalid. */
+int32_t bm_kv4_slots(const bm_dims* dims);
 
 /* Bytes of bm_kv4_cache.work; 0 if dims are invalid.  They hold
  * bm_workspace_bytes(dims) and one layer's cached rows in the element type of

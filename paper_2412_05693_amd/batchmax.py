@@ -103,6 +103,7 @@ def _load() -> ctypes.CDLL:
         "bm_set_left_padding": (ctypes.c_int, [P, P]),
         "bm_set_split_event": (ctypes.c_int, [P, P]),
         "bm_decode_step": (ctypes.c_int, [P, I32, P, P, P, P, I32, P]),
+        "bm_kv4_slots": (I32, [dims_p]),
         "bm_kv4_workspace_bytes": (SZ, [dims_p]),
         "bm_kv4_init": (ctypes.c_int, [dims_p, kv4_p, P, ctypes.POINTER(P)]),
         "bm_kv4_resume": (ctypes.c_int, [dims_p, kv4_p, I32, I32, ctypes.POINTER(P)]),
@@ -133,7 +134,7 @@ EXPORTED = ("bm_abi_version", "bm_last_error", "bm_cache_slots", "bm_workspace_b
             "bm_set_decode_removal", "bm_set_rank_rule", "bm_set_decode_bound",
             "bm_set_score_accumulation", "bm_set_left_padding", "bm_set_split_event",
             "bm_decode_step", "bm_ctx_len", "bm_ctx_next_pos", "bm_destroy", "bm_synth_qkv",
-            "bm_kv4_workspace_bytes", "bm_kv4_init", "bm_kv4_resume", "bm_kv4_write", "bm_kv4_read",
+            "bm_kv4_slots", "bm_kv4_workspace_bytes", "bm_kv4_init", "bm_kv4_resume", "bm_kv4_write", "bm_kv4_read",
             "bm_philox4x32_10", "bm_probe_stream_read", "bm_probe_mfma",
             "bm_prefill_timeline", "bm_prefill_tile_workgroups")
 
@@ -231,6 +232,10 @@ def bm_set_split_event(ctx: int, event: int) -> None:
 def bm_decode_step(ctx: int, pos: int, q: int, k: int, v: int, o: int, seq_ld: int,
                    stream: int) -> None:
     _check(_lib.bm_decode_step(ctx, pos, q, k, v, o, seq_ld, stream))
+
+
+def bm_kv4_slots(dims: bm_dims) -> int:
+    return _lib.bm_kv4_slots(ctypes.byref(dims))
 
 
 def bm_kv4_workspace_bytes(dims: bm_dims) -> int:
@@ -625,10 +630,10 @@ class PDAttentionKV4(PDAttention):
     a call's own K and V rows are attended to as given and stored in 4 bits,
     earlier entries as they read back.
 
-    ``k``, ``v`` hold codes, uint8 ``[b, n_kv_heads, cap, d / 2]``, ``k_scale``, ``v_scale``
-    their scale bytes, uint8 ``[b, n_kv_heads, cap, d / 32]``.  ``buffers``: those four, then
-    score, pos, len and work.  ``write_rows`` and ``read_rows`` convert rows of the
-    configured dtype to and from slots.
+    ``k``, ``v`` hold the codes, uint8 ``[b, n_kv_heads, slots, d / 2]``, ``k_scale``, ``v_scale``
+    the scale bytes, uint8 ``[b, n_kv_heads, slots, d / 32]``, in the library's own order of
+    bytes within a unit.  ``buffers``: those four, then score, pos, len and work.
+    ``write_rows`` and ``read_rows`` convert rows of the configured dtype to and from slots.
     """
 
     def __init__(self, *, static_workspace=False, **kw):
@@ -639,7 +644,7 @@ class PDAttentionKV4(PDAttention):
     def _buffers(self) -> dict:
         t, d = self.torch, self.dims
         plain = super()._buffers()
-        slots = plain["score"][0]
+        slots = (d.b, d.n_kv_heads, bm_kv4_slots(d))
         code, scale = (*slots, d.head_dim // 2), (*slots, d.head_dim // BM_KV4_GROUP)
         return {"k": (code, t.uint8), "v": (code, t.uint8), "k_scale": (scale, t.uint8),
                 "v_scale": (scale, t.uint8), **{x: plain[x] for x in ("score", "pos", "len")}}
@@ -720,12 +725,13 @@ def _align(n: int, a: int = 256) -> int:
     return (n + a - 1) // a * a
 
 
-def _row_planes(head_dim, dtype, kv_bits) -> tuple:
-    """Bytes of an entry's K row and, held in 4 bits, of its scales."""
+def _row_planes(cap, head_dim, dtype, kv_bits) -> tuple:
+    """Slots of a unit in the planes of K (and of V), and the bytes of a slot in each: K's
+    rows and, held in 4 bits, their scales."""
     if kv_bits == 16:
-        return (head_dim * (4 if dtype in ("f32", BM_F32) else 2),)
+        return cap, (head_dim * (4 if dtype in ("f32", BM_F32) else 2),)
     if kv_bits == 4:
-        return (head_dim // 2, head_dim // BM_KV4_GROUP)
+        return _align(cap, 64), (head_dim // 2, head_dim // BM_KV4_GROUP)
     raise ValueError("kv_bits is 16 (rows of the element type) or 4")
 
 
@@ -733,10 +739,10 @@ def stack_layer_bytes(*, b, kv_max, block, n_kv_heads, head_dim, dtype, kv_bits=
     """Device bytes of one layer's cache (K, V and their scales, score, pos, len),
     256-byte aligned."""
     cap = kv_max + block
-    rows = b * n_kv_heads * cap
-    planes = _row_planes(head_dim, dtype, kv_bits)
-    return (sum(2 * _align(rows * x) for x in planes) + 2 * _align(rows * 4)
-            + _align(b * n_kv_heads * 4))
+    units = b * n_kv_heads
+    slots, planes = _row_planes(cap, head_dim, dtype, kv_bits)
+    return (sum(2 * _align(units * slots * x) for x in planes) + 2 * _align(units * cap * 4)
+            + _align(units * 4))
 
 
 class PDStack:
@@ -777,10 +783,11 @@ class PDStack:
                 return x
 
             kv = []
-            for row in _row_planes(head_dim, dims.dtype, kv_bits):
+            slots, planes = _row_planes(cap, head_dim, dims.dtype, kv_bits)
+            for row in planes:
                 dt = torch.uint8 if kv_bits == 4 else tdt
-                shape = (b, n_kv_heads, cap, row // dt.itemsize)
-                kv += [take(rows * row, dt, shape), take(rows * row, dt, shape)]
+                shape, size = (b, n_kv_heads, slots, row // dt.itemsize), b * n_kv_heads * slots * row
+                kv += [take(size, dt, shape), take(size, dt, shape)]
             sc = take(rows * 4, torch.float32, (b, n_kv_heads, cap))
             ps = take(rows * 4, torch.int32, (b, n_kv_heads, cap))
             ln = take(b * n_kv_heads * 4, torch.int32, (b, n_kv_heads))

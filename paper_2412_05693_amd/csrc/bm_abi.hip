@@ -329,8 +329,8 @@ int kv4_ctx(const bm_dims* dims, const bm_kv4_cache* cache, bm_ctx** out) {
   if (!cache) return fail(BM_ERR_INVALID_ARG, "cache or out is null");
   if (!cache->k_scale || !cache->v_scale)
     return fail(BM_ERR_INVALID_ARG, "a cache pointer is null");
-  if (((uintptr_t)cache->k_scale | (uintptr_t)cache->v_scale) & 3)
-    return fail(BM_ERR_INVALID_ARG, "k_scale and v_scale must be 4-byte aligned");
+  if (((uintptr_t)cache->k_scale | (uintptr_t)cache->v_scale) & 15)
+    return fail(BM_ERR_INVALID_ARG, "k_scale and v_scale must be 16-byte aligned");
   const bm_cache plain = {cache->k,   cache->v,    cache->score,     cache->pos,
                           cache->len, cache->work, cache->work_bytes};
   size_t k_off, v_off;
@@ -353,8 +353,8 @@ int kv4_rows(const bm_dims* dims, const bm_kv4_cache* cache, int32_t slot0, int3
     return fail(BM_ERR_INVALID_ARG, "a cache pointer is null");
   if (((uintptr_t)cache->k | (uintptr_t)cache->v) & 15)
     return fail(BM_ERR_INVALID_ARG, "the cache's k and v must be 16-byte aligned");
-  if (((uintptr_t)cache->k_scale | (uintptr_t)cache->v_scale) & 3)
-    return fail(BM_ERR_INVALID_ARG, "k_scale and v_scale must be 4-byte aligned");
+  if (((uintptr_t)cache->k_scale | (uintptr_t)cache->v_scale) & 15)
+    return fail(BM_ERR_INVALID_ARG, "k_scale and v_scale must be 16-byte aligned");
   if (slot0 < 0 || n < 0) return fail(BM_ERR_INVALID_ARG, "slot0=%d n=%d", slot0, n);
   if ((int64_t)slot0 + n > (int64_t)dims->kv_max + dims->block)
     return fail(BM_ERR_CAPACITY, "slots [%d, %lld) exceed cap %d", slot0, (long long)slot0 + n,
@@ -373,7 +373,7 @@ int kv4_rows(const bm_dims* dims, const bm_kv4_cache* cache, int32_t slot0, int3
   a.vs = cache->v_scale;
   a.seq_ld = seq_ld;
   a.units = dims->b * dims->n_kv_heads;
-  a.cap = dims->kv_max + dims->block;
+  a.slots = bm::kv4_slots(dims->kv_max + dims->block);
   a.slot0 = slot0;
   a.n = n;
   const hipError_t e = bm::launch_kv4_rows(a, write, dims->dtype, dims->head_dim, stream);
@@ -393,13 +393,17 @@ hipError_t ctx_rows(const bm_ctx* ctx, int slot0, int n, const void* k, const vo
   a.vs = ctx->v_scale;
   a.seq_ld = seq_ld;
   a.units = ctx->units;
-  a.cap = ctx->cap;
+  a.slots = bm::kv4_slots(ctx->cap);
   a.slot0 = slot0;
   a.n = n;
   return bm::launch_kv4_rows(a, write, ctx->dims.dtype, ctx->dims.head_dim, stream);
 }
 
 }  // namespace
+
+BM_EXPORT int32_t bm_kv4_slots(const bm_dims* dims) {
+  return check_dims(dims) == BM_OK ? bm::kv4_slots(dims->kv_max + dims->block) : -1;
+}
 
 BM_EXPORT size_t bm_kv4_workspace_bytes(const bm_dims* dims) {
   if (check_dims(dims) != BM_OK) return 0;
@@ -580,6 +584,7 @@ BM_EXPORT int bm_prefill_block_cut(bm_ctx* ctx, int32_t t0, int32_t n_tok, const
   c.lastw = reinterpret_cast<float*>(work_at(ctx, ctx->lay.lastw_off));
   c.ks = ctx->k_scale;
   c.vs = ctx->v_scale;
+  c.slots = bm::kv4_slots(ctx->cap);
   e = bm::launch_fold_cut(a, c, bm::positions_per_wg(ctx->group), stream);
   if (e != hipSuccess) return hip_fail(e, "fold-cut launch");
   advance(ctx, t0, n_tok);
@@ -647,6 +652,7 @@ int cut_to(bm_ctx* ctx, int target, int32_t curr_id, hipStream_t stream) {
   a.lastw = reinterpret_cast<float*>(work_at(ctx, ctx->lay.lastw_off));
   a.ks = ctx->k_scale;
   a.vs = ctx->v_scale;
+  a.slots = bm::kv4_slots(ctx->cap);
   const int n_evict = ctx->len - target;
   const int max_moves = n_evict < target ? n_evict : target;
   hipError_t e;
@@ -747,6 +753,7 @@ int kv4_step(bm_ctx* ctx, int32_t pos, const void* q, const void* k, const void*
   a.pos = ctx->cache.pos;
   a.len = ctx->cache.len;
   a.part = reinterpret_cast<float*>(work_at(ctx, ctx->rows_k_off));
+  a.slots = bm::kv4_slots(ctx->cap);
   a.seq_ld = seq_ld;
   a.n_heads = ctx->dims.n_heads;
   a.n_kv_heads = ctx->dims.n_kv_heads;

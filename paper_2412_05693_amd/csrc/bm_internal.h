@@ -45,6 +45,9 @@ __device__ __forceinline__ uint64_t rank_key(int rule, float score, float last, 
   return ((uint64_t)__float_as_uint(k) << 32) | (uint32_t)pos;
 }
 
+// slots a unit has in the planes of a 4-bit cache
+inline int kv4_slots(int cap) { return (cap + 63) & ~63; }
+
 inline int positions_per_wg(int group) { return kWaves * kRowsPerWave / group; }
 
 // Workspace carve-up (all offsets 256-byte aligned).
@@ -92,11 +95,12 @@ struct EvictArgs {
   int cap, n, kv_max, curr_id, units, head_dim, elem_bytes;
   int rule;           // bm_rank_rule
   float* lastw;       // [U, cap] last query's weights (moved with the entries), or null
-  // a cache held in 4 bits: kc and vc are rows of head_dim / 2 bytes (elem_bytes 0), and
-  // every entry has head_dim / 32 scale bytes in each of these
+  // a cache held in 4 bits: kc and vc are its code planes, these its scales, all of
+  // `slots` slots a unit (bm_kv4.h)
   void* ks = nullptr;
   void* vs = nullptr;
-  __host__ __device__ int row_bytes() const { return ks ? head_dim / 2 : head_dim * elem_bytes; }
+  int slots = 0;
+  int row_bytes() const { return ks ? head_dim / 2 : head_dim * elem_bytes; }
 };
 
 struct DecodeArgs {
@@ -140,16 +144,16 @@ struct Kv4DecodeArgs {
   const void* kin;    // [b, Hk, seq_ld, D]
   const void* vin;
   void* o;
-  void* kq;           // codes [U, cap, D / 2]
+  void* kq;           // the planes of bm_kv4.h, `slots` slots a unit
   void* vq;
-  void* ks;           // scales [U, cap, D / 32]
+  void* ks;
   void* vs;
-  float* score;
+  float* score;       // [U, cap]
   int32_t* pos;
   int32_t* len;
-  float* part;        // [U][nsplit][G][D + 2] chunk partials (o, m, l) of a split step
+  float* part;        // [U][nsplit][G][D] partial outputs of a split step, then their [..][2] (m, l)
   int64_t seq_ld;
-  int n_heads, n_kv_heads, cap, len0, kv_max, cur_pos, units, nsplit;   // kv_max: the decode bound
+  int n_heads, n_kv_heads, cap, slots, len0, kv_max, cur_pos, units, nsplit;   // kv_max: the decode bound
   int rule;           // bm_rank_rule
   const int32_t* pad; // [b] left pad tokens per sample, or null
   float* lastw;       // [U, cap] this step's weights are written here, or null
@@ -165,7 +169,7 @@ struct Kv4RowsArgs {
   void* ks;
   void* vs;
   int64_t seq_ld;
-  int units, cap, slot0, n;
+  int units, slots, slot0, n;
 };
 
 struct SynthArgs {

@@ -17,10 +17,30 @@ typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 
-constexpr int kGroup = 32;
+// Planes of a unit (include/bm_kv4.h): K rows in order; V's words of eight codes with four
+// slots side by side; the scales of 64 slots side by side, in the order of a lane's slots.
+template <int D>
+__device__ __forceinline__ uint32_t k_word(uint32_t slot, uint32_t octet) {
+  return slot * (D / 8) + octet;
+}
+template <int D>
+__device__ __forceinline__ uint32_t v_word(uint32_t slot, uint32_t octet) {
+  return (slot >> 2) * (D / 2) + octet * 4 + (slot & 3);
+}
+template <int D>
+__device__ __forceinline__ uint32_t k_scale_at(uint32_t slot, uint32_t group) {
+  return (slot >> 6) * (2 * D) + group * 64 + (slot & 15) * 4 + ((slot >> 4) & 3);
+}
+template <int D>
+__device__ __forceinline__ uint32_t v_scale_at(uint32_t slot, uint32_t group) {
+  return (slot >> 6) * (2 * D) + group * 64 + ((slot >> 2) & 3) * 16 + ((slot >> 4) & 3) * 4 + (slot & 3);
+}
 
 // 2^E as a float from its scale byte (255: an infinity, which converts to NaN)
 __device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// the scale in byte b of a word
+__device__ __forceinline__ float scale_in(uint32_t word, int b) { return scale_of((word >> (8 * b)) & 0xFFu); }
 
 // Scale byte of a group whose largest element has the float bits `top` (sign
 // cleared): the exponent of the smallest power of two with top <= 6 2^E = 1.5
@@ -68,6 +88,19 @@ __device__ __forceinline__ void load8(const void* p, float (&x)[8]) {
       x[i] = __uint_as_float(w0[i]);
       x[4 + i] = __uint_as_float(w1[i]);
     }
+  }
+}
+
+// Lane `octet` of D / 8 stores its part of a row that a quad per group has quantised: the
+// row of slot `slot` of the unit whose planes begin at slot base0 (V's if `values`).
+template <int D>
+__device__ __forceinline__ void store_row(void* codes, void* scales, bool values, int64_t base0,
+                                          uint32_t slot, uint32_t octet, uint32_t code, uint32_t byte) {
+  const uint32_t at = values ? v_word<D>(slot, octet) : k_word<D>(slot, octet);
+  (static_cast<uint32_t*>(codes) + base0 * (D / 8))[at] = code;
+  if ((octet & 3) == 0) {
+    const uint32_t g = octet / 4, s = values ? v_scale_at<D>(slot, g) : k_scale_at<D>(slot, g);
+    (static_cast<uint8_t*>(scales) + base0 * (D / 32))[s] = (uint8_t)byte;
   }
 }
 

@@ -15,10 +15,11 @@
 // prefix counts, so the pairing is deterministic.
 //
 // K3 (compact_kernel), units x chunks of 32 moves: the i-th source moves into
-// the i-th hole (K row, V row, score, pos; a 4-bit entry's scales), 16-byte
-// coalesced copies.  Sources
+// the i-th hole (K row, V row, score, pos), 16-byte coalesced copies (a cache held
+// in 4 bits: move_4bit).  Sources
 // and holes are disjoint, so moves never overlap.
 #include "bm_internal.h"
+#include "bm_kv4_dev.h"
 
 namespace bm {
 namespace {
@@ -257,22 +258,46 @@ __global__ void __launch_bounds__(256) select_kernel(EvictArgs a) {
   }
 }
 
-// a 4-bit entry's scales (2 or 4 bytes of K's and of V's) from slot s to slot d
-__device__ __forceinline__ void move_scales(const EvictArgs& a, int u, int s, int d) {
-  const int64_t row = (int64_t)u * a.cap;
-  if (a.head_dim == 128) {
-    uint32_t* const ks = static_cast<uint32_t*>(a.ks) + row;
-    uint32_t* const vs = static_cast<uint32_t*>(a.vs) + row;
-    ks[d] = ks[s];
-    vs[d] = vs[s];
-  } else {
-    uint16_t* const ks = static_cast<uint16_t*>(a.ks) + row;
-    uint16_t* const vs = static_cast<uint16_t*>(a.vs) + row;
-    ks[d] = ks[s];
-    vs[d] = vs[s];
+// Rows that moves m0 .. m1 - 1 of a unit's list take from a slot to another in a cache held
+// in 4 bits, by the 256 threads of a workgroup: items of 4 bytes, D / 8 of K's and of V's
+// codes per move, then D / 32 scale bytes of each.
+template <int D>
+__device__ __forceinline__ void move_4bit(const EvictArgs& a, int u, int m0, int m1, const int32_t* holes,
+                                          const int32_t* srcs) {
+  constexpr int UM = 4;                      // loads in flight per thread
+  constexpr int W = D / 8, S = D / 32;
+  uint32_t* const kc = static_cast<uint32_t*>(a.kc) + (int64_t)u * a.slots * W;
+  uint32_t* const vc = static_cast<uint32_t*>(a.vc) + (int64_t)u * a.slots * W;
+  uint8_t* const ks = static_cast<uint8_t*>(a.ks) + (int64_t)u * a.slots * S;
+  uint8_t* const vs = static_cast<uint8_t*>(a.vs) + (int64_t)u * a.slots * S;
+  const int words = (m1 - m0) * 2 * W;
+  for (int c0 = threadIdx.x; c0 < words; c0 += 256 * UM) {
+    uint32_t x[UM];
+    uint32_t* to[UM];
+#pragma unroll
+    for (int i = 0; i < UM; ++i) {
+      const int c = min(c0 + 256 * i, words - 1);
+      const int mv = m0 + c / (2 * W), o = c % W;
+      const bool values = (c / W) & 1;
+      uint32_t* const base = values ? vc : kc;
+      x[i] = base[values ? kv4::v_word<D>(srcs[mv], o) : kv4::k_word<D>(srcs[mv], o)];
+      to[i] = base + (values ? kv4::v_word<D>(holes[mv], o) : kv4::k_word<D>(holes[mv], o));
+    }
+#pragma unroll
+    for (int i = 0; i < UM; ++i)
+      if (c0 + 256 * i < words) *to[i] = x[i];
+  }
+  for (int c = threadIdx.x; c < (m1 - m0) * 2 * S; c += 256) {
+    const int mv = m0 + c / (2 * S), g = c % S;
+    if ((c / S) & 1)
+      vs[kv4::v_scale_at<D>(holes[mv], g)] = vs[kv4::v_scale_at<D>(srcs[mv], g)];
+    else
+      ks[kv4::k_scale_at<D>(holes[mv], g)] = ks[kv4::k_scale_at<D>(srcs[mv], g)];
   }
 }
 
+// Q4: head_dim of a cache held in 4 bits, else 0
+template <int Q4>
 __global__ void __launch_bounds__(256) compact_kernel(EvictArgs a, int nchunks) {
   constexpr int kMoves = 32;
   const int u = blockIdx.x / nchunks;
@@ -282,11 +307,12 @@ __global__ void __launch_bounds__(256) compact_kernel(EvictArgs a, int nchunks) 
   if (m0 >= m) return;
   const int32_t* holes = a.holes + (int64_t)u * a.cap;
   const int32_t* srcs = a.srcs + (int64_t)u * a.cap;
-  const int row_bytes = a.row_bytes();
+  if constexpr (Q4 != 0) move_4bit<Q4>(a, u, m0, min(m, m0 + kMoves), holes, srcs);
+  const int row_bytes = a.head_dim * a.elem_bytes;
   const int cpr = row_bytes / 16;
   char* kc = static_cast<char*>(a.kc) + (int64_t)u * a.cap * row_bytes;
   char* vc = static_cast<char*>(a.vc) + (int64_t)u * a.cap * row_bytes;
-  const int total = kMoves * 2 * cpr;
+  const int total = Q4 ? 0 : kMoves * 2 * cpr;
   for (int c = threadIdx.x; c < total; c += 256) {
     const int mv = c / (2 * cpr);
     const int rem = c - mv * 2 * cpr;
@@ -305,7 +331,6 @@ __global__ void __launch_bounds__(256) compact_kernel(EvictArgs a, int nchunks) 
       a.score[(int64_t)u * a.cap + d] = a.score[(int64_t)u * a.cap + s];
       a.pos[(int64_t)u * a.cap + d] = a.pos[(int64_t)u * a.cap + s];
       if (a.rule == BM_RANK_TOVA) a.lastw[(int64_t)u * a.cap + d] = a.lastw[(int64_t)u * a.cap + s];
-      if (a.ks) move_scales(a, u, s, d);
     }
   }
 }
@@ -325,7 +350,8 @@ __host__ __device__ __forceinline__ int most_moves(const EvictArgs& a) {
 // reads the moved entries' scores, positions and weights again: arrays of all n
 // entries (82 KB at 4096) left a compute unit one workgroup, and the launch took
 // twice the time of select and compaction (4096 entries to 4064, 2048 units: 107 us).
-template <int KP, bool FOLD>
+// Q4: head_dim of a cache held in 4 bits, else 0.
+template <int KP, bool FOLD, int Q4>
 __global__ void __launch_bounds__(256) fold_cut_kernel(PrefillArgs pa, EvictArgs a,
                                                         int pt_positions) {
   __shared__ uint32_t hist[512];
@@ -448,8 +474,9 @@ __global__ void __launch_bounds__(256) fold_cut_kernel(PrefillArgs pa, EvictArgs
 
   // 3. the moves: the i-th source into the i-th hole (disjoint slot ranges)
   const int m = min(min(hbase, sbase), list_len);
-  const int row_bytes = a.row_bytes();
-  const int lg = 31 - __clz(row_bytes / 16);   // 8, 16 or 32 chunks of 16 bytes per row (4 bits: 2 or 4)
+  if constexpr (Q4 != 0) move_4bit<Q4>(a, u, 0, m, holes, srcs);
+  const int row_bytes = a.head_dim * a.elem_bytes;
+  const int lg = 31 - __clz(row_bytes / 16);   // 8, 16 or 32 chunks of 16 bytes per row
   char* kc = static_cast<char*>(a.kc) + (int64_t)u * a.cap * row_bytes;
   char* vc = static_cast<char*>(a.vc) + (int64_t)u * a.cap * row_bytes;
   // four loads in flight per thread: a chunk's store would otherwise wait for its
@@ -458,7 +485,7 @@ __global__ void __launch_bounds__(256) fold_cut_kernel(PrefillArgs pa, EvictArgs
   // same for every thread) and addresses are formed with shifts.  (An array of HIP's
   // uint4, a structure, would be kept in scratch memory.)
   constexpr int UM = 4;
-  const int chunks = m << (lg + 1);
+  const int chunks = Q4 ? 0 : m << (lg + 1);
   for (int b0 = 0; b0 < chunks; b0 += 256 * UM) {
     u32x4 x[UM];
     char* to[UM];
@@ -480,7 +507,6 @@ __global__ void __launch_bounds__(256) fold_cut_kernel(PrefillArgs pa, EvictArgs
     score[dj] = FOLD ? sc[sj] : score[sj];
     pos[dj] = FOLD ? ps[sj] : pos[sj];
     if (last) last[dj] = FOLD ? lw[sj] : last[sj];
-    if (a.ks) move_scales(a, u, sj, dj);
   }
   if (tid == 0) a.len[u] = a.kv_max;
 }
@@ -489,19 +515,26 @@ __global__ void __launch_bounds__(256) fold_cut_kernel(PrefillArgs pa, EvictArgs
 
 namespace {
 
-template <bool FOLD>
-hipError_t launch_cut_t(const PrefillArgs& pa, const EvictArgs& a, int pt_positions, hipStream_t stream) {
-  if (a.n > kMaxCap) return hipErrorInvalidValue;
+template <bool FOLD, int Q4>
+hipError_t launch_cut_q(const PrefillArgs& pa, const EvictArgs& a, int pt_positions, hipStream_t stream) {
   const size_t lds = sizeof(int32_t) * (FOLD ? 5 * (size_t)((a.n + 3) & ~3) : 2 * (size_t)most_moves(a));
   const dim3 grid((unsigned)a.units);
   if (a.n <= 256 * 3)
-    hipLaunchKernelGGL((fold_cut_kernel<3, FOLD>), grid, dim3(256), lds, stream, pa, a, pt_positions);
+    hipLaunchKernelGGL((fold_cut_kernel<3, FOLD, Q4>), grid, dim3(256), lds, stream, pa, a, pt_positions);
   else if (a.n <= 256 * 4)
-    hipLaunchKernelGGL((fold_cut_kernel<4, FOLD>), grid, dim3(256), lds, stream, pa, a, pt_positions);
+    hipLaunchKernelGGL((fold_cut_kernel<4, FOLD, Q4>), grid, dim3(256), lds, stream, pa, a, pt_positions);
   else
-    hipLaunchKernelGGL((fold_cut_kernel<kMaxPer, FOLD>), grid, dim3(256), lds, stream, pa, a,
+    hipLaunchKernelGGL((fold_cut_kernel<kMaxPer, FOLD, Q4>), grid, dim3(256), lds, stream, pa, a,
                        pt_positions);
   return hipGetLastError();
+}
+
+template <bool FOLD>
+hipError_t launch_cut_t(const PrefillArgs& pa, const EvictArgs& a, int pt_positions, hipStream_t stream) {
+  if (a.n > kMaxCap) return hipErrorInvalidValue;
+  if (!a.ks) return launch_cut_q<FOLD, 0>(pa, a, pt_positions, stream);
+  return a.head_dim == 128 ? launch_cut_q<FOLD, 128>(pa, a, pt_positions, stream)
+                           : launch_cut_q<FOLD, 64>(pa, a, pt_positions, stream);
 }
 
 }  // namespace
@@ -530,8 +563,13 @@ hipError_t launch_select(const EvictArgs& a, hipStream_t stream) {
 hipError_t launch_compact(const EvictArgs& a, int max_moves, hipStream_t stream) {
   if (max_moves <= 0) return hipSuccess;
   const int nchunks = (max_moves + 31) / 32;
-  hipLaunchKernelGGL(compact_kernel, dim3((unsigned)(a.units * nchunks)), dim3(256), 0, stream,
-                     a, nchunks);
+  const dim3 grid((unsigned)(a.units * nchunks));
+  if (!a.ks)
+    hipLaunchKernelGGL(compact_kernel<0>, grid, dim3(256), 0, stream, a, nchunks);
+  else if (a.head_dim == 128)
+    hipLaunchKernelGGL(compact_kernel<128>, grid, dim3(256), 0, stream, a, nchunks);
+  else
+    hipLaunchKernelGGL(compact_kernel<64>, grid, dim3(256), 0, stream, a, nchunks);
   return hipGetLastError();
 }
 

@@ -3,10 +3,14 @@
 // update, ranking, one removal, in-place write -- with the cached rows as 4-bit
 // floats (bm_kv4_attn.h) and the step's pair quantised into the slot it gets.
 //
-// One workgroup per unit; its waves take chunks of 64 cached slots in turn, each
-// with its own running maximum and sum; logits stay in LDS, because the scores
-// need every entry's probability under the whole unit's normaliser.  The step's own
-// pair (as given, float32 products) joins where the waves' outputs do.
+// One workgroup per unit:
+//   1. logits of all cached entries into LDS, a wave at a time on 64 slots;
+//   2. the exact softmax: sums per head, then every entry's probabilities, scores
+//      and ranking; the probabilities stay in LDS as the parts that the next
+//      product takes;
+//   3. outputs: 64 slots a wave, chunk c into stream c % kStreams, the streams' sums
+//      added in order; the step's own pair (as given, float32) joins at the end.
+// The next chunk's rows are on their way while one is computed.
 #include <type_traits>
 
 #include "bm_internal.h"
@@ -17,8 +21,24 @@
 namespace bm {
 namespace {
 
+using kv4::f32x4;
 using kv4::kChunk;
 using kv4::kNegInf;
+using kv4::u32x4;
+
+// rows of scores and positions begin anywhere
+typedef float f32x4u __attribute__((ext_vector_type(4), aligned(4)));
+typedef int32_t i32x4u __attribute__((ext_vector_type(4), aligned(4)));
+
+// Chunks of 64 slots are spread over so many partial output sums whatever the number of
+// waves, so that a launch can choose it and a sample's results stay the same bits.
+constexpr int kStreams = 4;
+
+constexpr int kRing = 2;                   // chunks of K, and of V, in registers
+
+// words of a head's plane of logits: 16 more than slots, so that the 16 words that a wave
+// takes of each of four heads spread over all banks
+__host__ __device__ __forceinline__ int plane_words(int nz) { return nz + 16; }
 
 // a probability: rounded once, never fused into the sum that uses it
 __device__ __forceinline__ float prob(float z, float m, float inv) {
@@ -26,125 +46,234 @@ __device__ __forceinline__ float prob(float z, float m, float inv) {
   return __builtin_amdgcn_exp2f(z - m) * inv;
 }
 
-template <bool BF16, int D, int G, int NW>
-__global__ void __launch_bounds__(64 * NW) kv4_decode_kernel(Kv4DecodeArgs a) {
+template <bool BF16, int D, int G, int NW, bool NT>
+__global__ void __launch_bounds__(64 * NW, BF16 ? 3 : 2) kv4_decode_kernel(Kv4DecodeArgs a) {
   using E = typename std::conditional<BF16, uint16_t, float>::type;
-  using Attn = kv4::Attn<BF16, D, G>;
-  constexpr int NT = 64 * NW;
-  constexpr int RB = Attn::RB, SB = Attn::SB;
-  constexpr int ZP = G < 2 ? 2 : G;       // planes of z: scores and weights end up in two of them
-  extern __shared__ float dsm[];
-  __shared__ float s_m[NW][G], s_l[NW][G], s_own[G];
+  using Attn = kv4::Attn<BF16, D, G, NT>;
+  constexpr int NTH = 64 * NW;
+  constexpr int RB = Attn::RB, SB = Attn::SB, DT = Attn::DT;
+  static_assert(NW <= kStreams, "a wave has whole streams");
+  extern __shared__ __attribute__((aligned(16))) float dsm[];
+  __shared__ float s_m[NW][G], s_own[G];
   __shared__ uint64_t s_wkey[NW];
   __shared__ int s_wslot[NW];
 
   const int u = blockIdx.x;
   const int bi = u / a.n_kv_heads, hk = u - bi * a.n_kv_heads;
-  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int tid = threadIdx.x, w = NW == 1 ? 0 : __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int n = a.len0;
   const int nz = (n + kChunk - 1) & ~(kChunk - 1);
-  float* z = dsm;                          // [ZP][nz] logits, by kv4::z_place
-  float* red = z + ZP * nz;                // [NW][G][D] partial outputs
-  const int64_t row0 = (int64_t)u * a.cap;
-  const kv4::Planes pl = {static_cast<const uint8_t*>(a.kq) + row0 * RB,
-                          static_cast<const uint8_t*>(a.ks) + row0 * SB,
-                          static_cast<const uint8_t*>(a.vq) + row0 * RB,
-                          static_cast<const uint8_t*>(a.vs) + row0 * SB, a.pos + row0};
+  const int chunks = nz / kChunk;
+  const int zs = plane_words(nz);
+  float* z = dsm;                          // [G][zs] logits, then probabilities
+  float* red = z + G * zs;                 // [kStreams][G][kRed] partial outputs (NW > 1)
+  const int64_t row0 = (int64_t)u * a.cap, slot0 = (int64_t)u * a.slots;
+  const kv4::Planes pl = {static_cast<const uint8_t*>(a.kq) + slot0 * RB,
+                          static_cast<const uint8_t*>(a.ks) + slot0 * SB,
+                          static_cast<const uint8_t*>(a.vq) + slot0 * RB,
+                          static_cast<const uint8_t*>(a.vs) + slot0 * SB, a.pos + row0};
   float* score = a.score + row0;
   int32_t* pos = a.pos + row0;
+  float* lw = a.lastw ? a.lastw + row0 : nullptr;
   const int64_t plane = ((int64_t)bi * a.n_kv_heads + hk) * a.seq_ld;
   const E* knew = static_cast<const E*>(a.kin) + plane * D;
   const E* vnew = static_cast<const E*>(a.vin) + plane * D;
   const E* qb = static_cast<const E*>(a.q) + ((int64_t)bi * a.n_heads + hk * G) * a.seq_ld * D;
+  E* ob = static_cast<E*>(a.o) + ((int64_t)bi * a.n_heads + hk * G) * a.seq_ld * D;
   const int64_t head_stride = a.seq_ld * D;
   const int pad = a.pad ? max(0, a.pad[bi]) : 0;
+  const Attn at(lane);
+  auto as_float = [](E x) -> float {
+    if constexpr (BF16) return __uint_as_float((uint32_t)x << 16);
+    else return x;
+  };
+  auto rounded = [](float x) -> E {
+    if constexpr (BF16) return __builtin_bit_cast(uint16_t, (__bf16)x);
+    else return x;
+  };
+  // a wave's chunks of V in order: every kStreams-th from its first, then its next stream's
+  auto next_chunk = [&](int c) {
+    if (c + kStreams < chunks) return c + kStreams;
+    return (c % kStreams) + NW < kStreams ? (c % kStreams) + NW : chunks;
+  };
+  auto load_k = [&](int base, typename Attn::KRows& rows) { at.load_k(pl, base, n - base, rows); };
+  auto load_v = [&](int c, typename Attn::VRows& rows) {
+    c = min(c, chunks);
+    at.load_v(pl, c * kChunk, n - c * kChunk, rows);
+  };
+  auto load_quad = [&](int qd, f32x4& sc, i32x4u& ps) {
+    if (4 * qd + 3 < n) {
+      sc = *reinterpret_cast<const f32x4u*>(score + 4 * qd);
+      ps = *reinterpret_cast<const i32x4u*>(pos + 4 * qd);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int j = min(4 * qd + r, max(n - 1, 0));   // slot 0 exists even when empty
+        sc[r] = score[j];
+        ps[r] = pos[j];
+      }
+    }
+  };
 
-  // the step's own pair in 4 bits (D / 8 lanes for each of the two rows)
-  uint32_t code = 0, byte = 0;
-  if (tid < D / 4) {
-    float x[8];
-    kv4::load8<BF16>((tid < D / 8 ? knew : vnew) + (tid % (D / 8)) * 8, x);
-    code = kv4::quantise8(x, &byte);
+  // The first rows of K and V, the queries, the step's own pair and the first scores are
+  // all on their way before any is used.
+  constexpr int kStep = NW * kChunk;
+  constexpr int GW = (G + NW - 1) / NW;    // heads of this wave in what waves share out
+  constexpr int NSP = NW == 1 ? 2 : 1;     // quads of slots per thread loaded ahead
+  typedef E own_t __attribute__((ext_vector_type(D / 64)));
+  typename Attn::Query q;
+  typename Attn::KRows k[kRing];
+  typename Attn::VRows v[kRing];
+#pragma unroll
+  for (int r = 0; r + 1 < kRing; ++r) load_k(w * kChunk + r * kStep, k[r]);
+  at.load_q(qb, head_stride, q);
+  own_t own_q[GW];
+  const own_t own_k = reinterpret_cast<const own_t*>(knew)[lane];
+#pragma unroll
+  for (int x = 0; x < GW; ++x)
+    own_q[x] = reinterpret_cast<const own_t*>(qb + min(w + x * NW, G - 1) * head_stride)[lane];
+  float pair[8] = {};                      // D / 8 lanes for each of the step's two rows
+  if (tid < D / 4) kv4::load8<BF16>((tid < D / 8 ? knew : vnew) + (tid % (D / 8)) * 8, pair);
+  const E v_out = vnew[tid % D];           // (NW > 1: of this thread's outputs)
+  int ahead = w;
+#pragma unroll
+  for (int r = 0; r + 1 < kRing; ++r) {
+    load_v(ahead, v[r]);
+    ahead = next_chunk(ahead);
   }
-  for (int g = w; g < G; g += NW) {
-    const float s = lanes::wave_sum(kv4::dot_part<BF16, D>(qb + g * head_stride, knew, lane));
-    if (lane == 0) s_own[g] = s * a.scale_log2;
-  }
+  f32x4 sp_score[NSP];
+  i32x4u sp_pos[NSP];
+#pragma unroll
+  for (int e = 0; e < NSP; ++e) load_quad(tid + NTH * e, sp_score[e], sp_pos[e]);
 
-  // 1. attention over the cached entries
-  Attn at;
-  at.init(qb, head_stride, lane);
-  for (int base = w * kChunk; base < n; base += NW * kChunk) {
-    at.chunk(pl, base, n, pad, a.scale_log2,
-             [&](int t, const kv4::f32x4& zt) {
-                   if (at.i < G)
-                     *reinterpret_cast<kv4::f32x4*>(z + at.i * nz + base + 16 * t + 4 * at.h) = zt;
-                 });
+  // ---------------- 1. logits ----------------
+  {
+    float m = kNegInf;
+    auto take = [&](const typename Attn::KRows& rows, int base) {
+      typename Attn::Logits zt;
+      at.logits(rows, q, a.scale_log2, n - base, zt);
+      if (pad > 0) at.pads(pl, base, n - base, pad, [&](int e) { zt[e] = kNegInf; });
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const f32x4 x = {zt[4 * t], zt[4 * t + 1], zt[4 * t + 2], zt[4 * t + 3]};
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m = fmaxf(m, x[r]);
+        if (at.i < G) *reinterpret_cast<f32x4*>(z + at.i * zs + base + 16 * t + 4 * at.h) = x;
+      }
+    };
+    for (int base = w * kChunk; base < n;) {
+#pragma unroll
+      for (int r = 0; r < kRing; ++r) {
+        if (base >= n) break;
+        load_k(base + (kRing - 1) * kStep, k[(r + kRing - 1) % kRing]);
+        take(k[r], base);
+        base += kStep;
+      }
+    }
+    m = kv4::xor16_32_max(m);
+    if (lane < G) s_m[w][lane] = m;
+#pragma unroll
+    for (int x = 0; x < GW; ++x) {
+      float s = 0.0f;
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e) s = fmaf(as_float(own_q[x][e]), as_float(own_k[e]), s);
+      s = lanes::wave_sum(s);
+      if (lane == 0 && w + x * NW < G) s_own[w + x * NW] = s * a.scale_log2;
+    }
   }
-  const float l = at.sum();
-  if (lane < G) {
-    s_m[w][lane] = at.m;
-    s_l[w][lane] = l;
-  }
-  if (at.i < G) at.store_o(red + (w * G + at.i) * D);
+  uint32_t byte;
+  const uint32_t code = kv4::quantise8(pair, &byte);
   __syncthreads();
 
-  // the unit's maximum and sum per head, the step's own pair included
-  float mg[G], inv[G], p_own[G];
+  // ---------------- 2. softmax, scores, ranking ----------------
+  // Each wave forms every head's maximum and sum by itself: 64 / G lanes a head.
+  float mg[G], inv[G], p_own[G], w_own = 0.0f;
 #pragma unroll
   for (int g = 0; g < G; ++g) {
     float m = s_own[g];
 #pragma unroll
     for (int i = 0; i < NW; ++i) m = fmaxf(m, s_m[i][g]);
-    const float e = __builtin_amdgcn_exp2f(s_own[g] - m);
-    float sum = e;
-#pragma unroll
-    for (int i = 0; i < NW; ++i) sum += s_l[i][g] * __builtin_amdgcn_exp2f(s_m[i][g] - m);
     mg[g] = m;
-    inv[g] = 1.0f / sum;
-    p_own[g] = e;
   }
-
-  // 2. outputs
-  for (int idx = tid; idx < G * D; idx += NT) {
-    const int g = idx / D, d = idx - g * D;
-    float m = mg[0], r = inv[0], p = p_own[0];
+  {
+    constexpr int L = 64 / G;
+    const int hg = lane / L;
+    float m = mg[0];
 #pragma unroll
-    for (int k = 1; k < G; ++k)
-      if (g == k) m = mg[k], r = inv[k], p = p_own[k];
-    float v;
-    if constexpr (BF16) v = __uint_as_float((uint32_t)vnew[d] << 16);
-    else v = vnew[d];
-    float x = p * v;
+    for (int g = 1; g < G; ++g)
+      if (hg == g) m = mg[g];
+    float s = 0.0f;
+    const float* zh = z + hg * zs;
+#pragma unroll 2
+    for (int qd = lane % L; qd < nz / 4; qd += L) {
+      const f32x4 x = *reinterpret_cast<const f32x4*>(zh + 4 * qd);
+      float e[4];
 #pragma unroll
-    for (int i = 0; i < NW; ++i)
-      x = fmaf(red[(i * G + g) * D + d], __builtin_amdgcn_exp2f(s_m[i][g] - m), x);
-    x *= r;
-    E* o = static_cast<E*>(a.o) + (((int64_t)bi * a.n_heads + hk * G + g) * a.seq_ld) * D + d;
-    if constexpr (BF16) *o = __builtin_bit_cast(uint16_t, (__bf16)x);
-    else *o = x;
+      for (int r = 0; r < 4; ++r) e[r] = __builtin_amdgcn_exp2f(x[r] - m);
+      s += (e[0] + e[1]) + (e[2] + e[3]);
+    }
+    if constexpr (G == 1) s = lanes::wave_sum(s);
+    else s = lanes::group_sum<L>(s);
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+      const float all = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(s), g * L));
+      inv[g] = 1.0f / (all + __builtin_amdgcn_exp2f(s_own[g] - mg[g]));
+    }
   }
-
-  // 3. scores and ranking (entry n is the step's own)
-  float w_own = 0.0f;
+  if constexpr (NW > 1) __syncthreads();   // every wave has read the logits
 #pragma unroll
-  for (int g = 0; g < G; ++g) w_own += prob(s_own[g], mg[g], inv[g]);
+  for (int g = 0; g < G; ++g) {
+    p_own[g] = prob(s_own[g], mg[g], inv[g]);
+    w_own += p_own[g];
+  }
   const bool evict = n + 1 > a.kv_max;
   uint64_t best = ~0ull;
-  int bslot = n;
-  for (int j = tid; j < n; j += NT) {
-    float* zj = z + kv4::z_place(j);
-    float ps = 0.0f;
+  int bslot = n;                           // entry n is the step's own
+  auto rank_quad = [&](int qd, const f32x4& sc, const i32x4u& ps) {
+    float gain[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int g = 0; g < G; ++g) ps += prob(zj[g * nz], mg[g], inv[g]);
-    const float s = score[j] + ps;
-    zj[0] = s;
-    zj[nz] = ps;
-    const uint64_t key = rank_key(a.rule, s, ps, pos[j], a.cur_pos);
-    if (key < best) {
-      best = key;
-      bslot = j;
+    for (int g = 0; g < G; ++g) {
+      u32x4* at_z = reinterpret_cast<u32x4*>(z + g * zs + 4 * qd);
+      const f32x4 x = __builtin_bit_cast(f32x4, *at_z);
+      float p[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        p[r] = prob(x[r], mg[g], inv[g]);
+        gain[r] += p[r];
+      }
+      u32x4 y;
+      if constexpr (BF16) {                // {part 0 of two pairs, part 1 of the same}
+        uint32_t lo[2], hi[2];
+        kv4::split_pair<2>(p[0], p[1], lo);
+        kv4::split_pair<2>(p[2], p[3], hi);
+        y = u32x4{lo[0], hi[0], lo[1], hi[1]};
+      } else {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) y[r] = __float_as_uint(p[r]);
+      }
+      *at_z = y;
     }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int j = 4 * qd + r;
+      if (j >= n) continue;
+      const float s = sc[r] + gain[r];
+      score[j] = s;
+      if (lw) lw[j] = gain[r];
+      const uint64_t key = rank_key(a.rule, s, gain[r], ps[r], a.cur_pos);
+      const bool less = key < best;
+      best = less ? key : best;
+      bslot = less ? j : bslot;
+    }
+  };
+#pragma unroll
+  for (int e = 0; e < NSP; ++e)
+    if (tid + NTH * e < nz / 4) rank_quad(tid + NTH * e, sp_score[e], sp_pos[e]);
+  for (int qd = tid + NTH * NSP; qd < nz / 4; qd += NTH) {
+    f32x4 sc;
+    i32x4u ps;
+    load_quad(qd, sc, ps);
+    rank_quad(qd, sc, ps);
   }
   if (tid == 0) {
     const uint64_t key = rank_key(a.rule, w_own, w_own, a.cur_pos, a.cur_pos);
@@ -153,7 +282,6 @@ __global__ void __launch_bounds__(64 * NW) kv4_decode_kernel(Kv4DecodeArgs a) {
       bslot = n;
     }
   }
-  int dst = n;                             // the slot that receives the step's pair
   if (evict) {
     const uint64_t wmin = lanes::wave_min_u64(best);
     const uint64_t holders = __ballot(best == wmin);
@@ -162,7 +290,94 @@ __global__ void __launch_bounds__(64 * NW) kv4_decode_kernel(Kv4DecodeArgs a) {
       s_wkey[w] = wmin;
       s_wslot[w] = bslot;
     }
+  }
+  __syncthreads();
+
+  // ---------------- 3. outputs ----------------
+  auto add_chunk = [&](typename Attn::VRows& rows, int base, typename Attn::Out& o) {
+    if (pad > 0) at.pads(pl, base, n - base, pad, [&](int e) { Attn::hide_value(rows, e); });
+    at.hide_values_past(rows, n - base);
+    const float* pz = z + min(at.i, G - 1) * zs + base + 4 * at.h;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const u32x4 t0 = *reinterpret_cast<const u32x4*>(pz + 32 * x);
+      const u32x4 t1 = *reinterpret_cast<const u32x4*>(pz + 32 * x + 16);
+      u32x4 pw[Attn::PP];
+      if constexpr (BF16) {
+        pw[0] = u32x4{t0[0], t0[1], t1[0], t1[1]};
+        pw[1] = u32x4{t0[2], t0[3], t1[2], t1[3]};
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const u32x4 t = j < 2 ? t0 : t1;
+          uint32_t part[Attn::PP];
+          kv4::split_pair<Attn::PP>(__uint_as_float(t[2 * (j & 1)]), __uint_as_float(t[2 * (j & 1) + 1]), part);
+#pragma unroll
+          for (int p = 0; p < Attn::PP; ++p) pw[p][j] = part[p];
+        }
+      }
+      at.add_values(rows, x, pw, o);
+    }
+  };
+  typename Attn::Out o, total;             // (total: NW = 1)
+  Attn::clear(total);
+  for (int c = w; c < chunks;) {
+#pragma unroll
+    for (int r = 0; r < kRing; ++r) {
+      if (c >= chunks) break;
+      load_v(ahead, v[(r + kRing - 1) % kRing]);
+      ahead = next_chunk(ahead);
+      if (c < kStreams) Attn::clear(o);    // a stream's first chunk
+      add_chunk(v[r], c * kChunk, o);
+      const int s = c % kStreams;
+      c = next_chunk(c);
+      if (c < chunks && c % kStreams == s) continue;
+      // the stream's last chunk
+      if constexpr (NW == 1) {
+#pragma unroll
+        for (int t = 0; t < DT; ++t) total[t] += o[t];
+      } else {
+        if (at.i < G) at.store_o(o, red + (s * G + at.i) * Attn::kRed);
+      }
+    }
+  }
+  if constexpr (NW == 1) {
+    if (at.i < G) {
+      float p = p_own[0];
+#pragma unroll
+      for (int g = 1; g < G; ++g)
+        if (at.i == g) p = p_own[g];
+      typedef E vec __attribute__((ext_vector_type(DT)));
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int d = DT * (4 * at.h + r);
+        const vec y = *reinterpret_cast<const vec*>(vnew + d);
+        vec x;
+#pragma unroll
+        for (int t = 0; t < DT; ++t) x[t] = rounded(fmaf(p, as_float(y[t]), total[t][r]));
+        *reinterpret_cast<vec*>(ob + at.i * head_stride + d) = x;
+      }
+    }
+  } else {
+    static_assert(NTH % D == 0, "a thread's outputs are one element of several heads");
     __syncthreads();
+    for (int idx = tid; idx < G * D; idx += NTH) {
+      const int g = idx / D, d = idx - g * D;
+      float p = p_own[0];
+#pragma unroll
+      for (int e = 1; e < G; ++e)
+        if (g == e) p = p_own[e];
+      float x = 0.0f;
+#pragma unroll
+      for (int s = 0; s < kStreams; ++s)
+        if (s < chunks) x += red[(s * G + g) * Attn::kRed + Attn::red_word(d)];
+      ob[g * head_stride + d] = rounded(fmaf(p, as_float(v_out), x));
+    }
+  }
+
+  // ---------------- 4. the step's pair ----------------
+  int dst = n;                             // the slot that receives it
+  if (evict) {
     uint64_t k0 = s_wkey[0];
     dst = s_wslot[0];
 #pragma unroll
@@ -172,44 +387,59 @@ __global__ void __launch_bounds__(64 * NW) kv4_decode_kernel(Kv4DecodeArgs a) {
         dst = s_wslot[i];
       }
   }
-
-  // 4. write back: scores (and the step's weights), each by the thread that formed them
-  float* lw = a.lastw ? a.lastw + row0 : nullptr;
-  for (int j = tid; j < n; j += NT) {
-    const float* zj = z + kv4::z_place(j);
-    score[j] = j == dst ? w_own : zj[0];
-    if (lw) lw[j] = j == dst ? w_own : zj[nz];
-  }
   if (tid == 0) a.len[u] = evict ? n : n + 1;
-  // the step's pair, unless it is the one removed (entry n of a full cache)
+  // unless it is the one removed (entry n of a full cache)
   if (evict && dst == n) return;
-  if (tid < D / 4) {
-    const int wh = tid / (D / 8), c = tid - wh * (D / 8);
-    uint8_t* q8 = static_cast<uint8_t*>(wh ? a.vq : a.kq) + (row0 + dst) * RB;
-    *reinterpret_cast<uint32_t*>(q8 + 4 * c) = code;
-    if ((c & 3) == 0) (static_cast<uint8_t*>(wh ? a.vs : a.ks))[(row0 + dst) * SB + c / 4] = (uint8_t)byte;
-  }
-  if (tid == 0) {
+  // its score, by the thread that wrote the slot's before (or the first, behind the last)
+  const int owner = dst < n ? (dst >> 2) % NTH : 0;
+  if (tid == owner) {
+    score[dst] = w_own;
+    if (lw) lw[dst] = w_own;
     pos[dst] = a.cur_pos;
-    if (!evict) {
-      score[n] = w_own;
-      if (lw) lw[n] = w_own;
-    }
+  }
+  if (tid < D / 4) {
+    const int wh = tid / (D / 8), c8 = tid - wh * (D / 8);
+    kv4::store_row<D>(wh ? a.vq : a.kq, wh ? a.vs : a.ks, wh, slot0, dst, c8, code, byte);
   }
 }
 
 template <bool BF16, int D, int G, int NW>
 hipError_t launch_w(const Kv4DecodeArgs& a, hipStream_t stream) {
-  const size_t nz = ((size_t)a.len0 + kChunk - 1) & ~(size_t)(kChunk - 1);
-  const size_t lds = sizeof(float) * ((G < 2 ? 2 : G) * nz + NW * G * D);
-  hipLaunchKernelGGL((kv4_decode_kernel<BF16, D, G, NW>), dim3((unsigned)a.units), dim3(64 * NW),
-                     lds, stream, a);
+  const int nz = (a.len0 + kChunk - 1) & ~(kChunk - 1);
+  const size_t lds = sizeof(float) * ((size_t)G * plane_words(nz) +
+                                      (NW > 1 ? kStreams * G * kv4::Attn<BF16, D, G, false>::kRed : 0));
+  // rows are read once per step: a cache larger than the last-level cache streams past it
+  const size_t bytes = (size_t)a.units * a.len0 * (D + D / 16 + 8);
+  const dim3 grid((unsigned)a.units), block(64 * NW);
+  if (bytes > kLastLevelCacheBytes)
+    hipLaunchKernelGGL((kv4_decode_kernel<BF16, D, G, NW, true>), grid, block, lds, stream, a);
+  else
+    hipLaunchKernelGGL((kv4_decode_kernel<BF16, D, G, NW, false>), grid, block, lds, stream, a);
   return hipGetLastError();
 }
 
+// One wave per unit or four.  One has no partial outputs to join and waits for no other
+// wave, which is fastest once every compute unit has several units; four shorten a unit's
+// chain of loads where it has few, and share the LDS that a long unit's logits fill.
+// us a step with one -> with four, bf16 d=128 G=4 by units (512 entries at 768 units 19.2 ->
+// 18.7, at 896 19.9 -> 22.7):
+//   entries  8             512            1024           2048           8192
+//   64       6.8 -> 6.9    7.9 -> 8.5     8.7 -> 14.0    10.7 -> 21.5   31.8 -> 72.3
+//   128      8.0 -> 7.1    9.1 -> 9.2     10.2 -> 14.8   14.7 -> 24.0   40.4 -> 76.1
+//   512      15.7 -> 8.7   18.6 -> 13.8   20.9 -> 23.5   32.1 -> 39.7   129 -> 150
+//   1024     26.9 -> 11.5  31.3 -> 20.4   34.9 -> 34.4   65.2 -> 72.2   252 -> 249
+//   2048     48.9 -> 17.9  55.0 -> 32.9   70.9 -> 69.9   163 -> 128
+//   4096     93.2 -> 30.4  112 -> 68.1    224 -> 129     447 -> 247
+// (Two waves are between the two, eight slower than four but for 5% at 8 units of 2048
+// entries.  A third chunk of K or V on its way changes nothing: 129 -> 127-145.)
+constexpr int kManyUnits = 768;          // three for every compute unit
+constexpr int kFewEntries = 1024;
+
 template <bool BF16, int D, int G>
 hipError_t launch_t(const Kv4DecodeArgs& a, hipStream_t stream) {
-  return a.len0 > 256 ? launch_w<BF16, D, G, 8>(a, stream) : launch_w<BF16, D, G, 4>(a, stream);
+  if (a.len0 <= kChunk || (a.units > kManyUnits && a.len0 < kFewEntries))
+    return launch_w<BF16, D, G, 1>(a, stream);
+  return launch_w<BF16, D, G, 4>(a, stream);
 }
 
 template <bool BF16, int D>

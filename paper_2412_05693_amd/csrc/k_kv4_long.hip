@@ -1,7 +1,7 @@
 // K10: one decode step over a long cache held in 4 bits, outputs only: K6's step
 // (a cache that is never cut, more entries than a scoring step takes) with the
 // rows as 4-bit floats.  kv4_split_kernel, grid (units, splits): a workgroup's
-// waves attend to kSplit cached slots and leave one partial softmax per head;
+// waves attend to a split of the cached slots and leave one partial softmax per head;
 // kv4_combine_kernel, one workgroup per unit and head, joins them with the step's own
 // pair, writes the outputs and stores that pair in the slot behind the last.
 #include <type_traits>
@@ -16,67 +16,137 @@ namespace {
 
 using kv4::kChunk;
 using kv4::kNegInf;
+using kv4::f32x4;
 
-constexpr int kSplit = 512;              // slots per split workgroup
-constexpr int kMaxSplits = kMaxCapAny / kSplit;
-constexpr int NW = 4;
+// Slots of a split, by the length alone, so that a sample's results are the same bits in
+// any batch.  Each of a split's waves ends with its sums going through LDS, so longer
+// splits are faster once they fill the card (us a step, bf16 d=128 G=4, splits of 512 ->
+// 1024 -> 2048 slots: 64 units of 8192 entries 22.9 -> 21.6 -> 22.9, of 60001 109 -> 97 ->
+// 97, 512 units of 20000 295 -> 274 -> 254) and slower while they do not (8 units of 4200:
+// 9.9 -> 12.4 -> 17.5, of 8192: 10.2 -> 12.6 -> 18.2, of 20000: 12.3 -> 13.3 -> 19.8, of
+// 60001: 21.7 -> 20.3 -> 21.9).
+constexpr int kShortSplit = 512, kLongSplit = 1024, kShortEntries = 16384;
+constexpr int kMaxSplits = kMaxCapAny / kLongSplit;
+static_assert(kShortEntries / kShortSplit <= kMaxSplits, "splits of the shorter kind");
+int split_slots(int n) { return n <= kShortEntries ? kShortSplit : kLongSplit; }
 
-template <bool BF16, int D, int G>
-__global__ void __launch_bounds__(64 * NW) kv4_split_kernel(Kv4DecodeArgs a) {
+constexpr int NW = 4;                    // waves of a split (eight: the same or slower)
+constexpr int kJoin = 256;               // threads that join a head's splits
+
+template <bool BF16, int D, int G, bool NT>
+__global__ void __launch_bounds__(64 * NW, BF16 ? 3 : 2) kv4_split_kernel(Kv4DecodeArgs a, int split) {
   using E = typename std::conditional<BF16, uint16_t, float>::type;
-  using Attn = kv4::Attn<BF16, D, G>;
+  using Attn = kv4::Attn<BF16, D, G, NT>;
   constexpr int RB = Attn::RB, SB = Attn::SB;
-  __shared__ float red[NW][G][D];
+  __shared__ __align__(16) float red[NW][G][Attn::kRed];
   __shared__ float s_m[NW][G], s_l[NW][G];
   const int u = blockIdx.x, c = blockIdx.y;
   const int bi = u / a.n_kv_heads, hk = u - bi * a.n_kv_heads;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int64_t row0 = (int64_t)u * a.cap;
-  const kv4::Planes pl = {static_cast<const uint8_t*>(a.kq) + row0 * RB,
-                          static_cast<const uint8_t*>(a.ks) + row0 * SB,
-                          static_cast<const uint8_t*>(a.vq) + row0 * RB,
-                          static_cast<const uint8_t*>(a.vs) + row0 * SB, a.pos + row0};
+  const kv4::Planes pl = {static_cast<const uint8_t*>(a.kq) + (int64_t)u * a.slots * RB,
+                          static_cast<const uint8_t*>(a.ks) + (int64_t)u * a.slots * SB,
+                          static_cast<const uint8_t*>(a.vq) + (int64_t)u * a.slots * RB,
+                          static_cast<const uint8_t*>(a.vs) + (int64_t)u * a.slots * SB, a.pos + row0};
   const E* qb = static_cast<const E*>(a.q) + ((int64_t)bi * a.n_heads + hk * G) * a.seq_ld * D;
   const int pad = a.pad ? max(0, a.pad[bi]) : 0;
-  const int end = min(a.len0, (c + 1) * kSplit);
+  const int end = min(a.len0, (c + 1) * split);
 
-  Attn at;
-  at.init(qb, a.seq_ld * D, lane);
-  for (int base = c * kSplit + w * kChunk; base < end; base += NW * kChunk)
-    at.chunk(pl, base, end, pad, a.scale_log2, [](int, const kv4::f32x4&) {});
-  const float l = at.sum();
+  const Attn at(lane);
+  typename Attn::Query q;
+  typename Attn::Out o;
+  at.load_q(qb, a.seq_ld * D, q);
+  Attn::clear(o);
+  float m = kNegInf, l = 0.0f;             // running maximum, this lane's part of the sum
+  for (int base = c * split + w * kChunk; base < end; base += NW * kChunk) {
+    const int rows = end - base;
+    typename Attn::KRows k;
+    typename Attn::VRows v;
+    typename Attn::Logits z;
+    at.load_k(pl, base, rows, k);
+    at.load_v(pl, base, rows, v);
+    at.logits(k, q, a.scale_log2, rows, z);
+    if (pad > 0)
+      at.pads(pl, base, rows, pad, [&](int e) {
+        z[e] = kNegInf;
+        Attn::hide_value(v, e);
+      });
+    at.hide_values_past(v, rows);
+    // the new maximum; what was summed so far is scaled to it
+    float mx = m;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, z[e]);
+    mx = kv4::xor16_32_max(mx);
+    const float ref = mx == kNegInf ? 0.0f : mx;   // nothing visible yet: all weights are 0
+    if (__any(mx > m)) {
+      const float shrink = __builtin_amdgcn_exp2f(m - ref);
+      l *= shrink;
+#pragma unroll
+      for (int t = 0; t < Attn::DT; ++t) o[t] *= shrink;
+    }
+    m = mx;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      kv4::u32x4 pw[Attn::PP];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int e = 8 * x + 2 * j;
+        const float p0 = __builtin_amdgcn_exp2f(z[e] - ref);
+        const float p1 = __builtin_amdgcn_exp2f(z[e + 1] - ref);
+        l += p0;
+        l += p1;
+        uint32_t part[Attn::PP];
+        kv4::split_pair<Attn::PP>(p0, p1, part);
+#pragma unroll
+        for (int p = 0; p < Attn::PP; ++p) pw[p][j] = part[p];
+      }
+      at.add_values(v, x, pw, o);
+    }
+  }
+  l = lanes::add_xor<32>(lanes::add_xor<16>(l));
   if (lane < G) {
-    s_m[w][lane] = at.m;
+    s_m[w][lane] = m;
     s_l[w][lane] = l;
   }
-  if (at.i < G) at.store_o(&red[w][at.i][0]);
+  if (at.i < G) at.store_o(o, &red[w][at.i][0]);
   __syncthreads();
-  // partial record of this split: [G][D + 2] floats (o, then m, l)
-  float* out = a.part + ((int64_t)u * a.nsplit + c) * G * (D + 2);
+  // this split's partial outputs [G][D], and its (m, l) [G][2]
+  const int64_t part = ((int64_t)u * a.nsplit + c) * G;
+  float* out = a.part + part * D;
+  float* out_ml = a.part + (int64_t)a.units * a.nsplit * G * D + part * 2;
   for (int idx = tid; idx < G * (D + 1); idx += 64 * NW) {
     const int g = idx / (D + 1), d = idx - g * (D + 1);
-    float m = s_m[0][g];
+    float mg = s_m[0][g];
 #pragma unroll
-    for (int i = 1; i < NW; ++i) m = fmaxf(m, s_m[i][g]);
-    const float ref = m == kNegInf ? 0.0f : m;    // a split of hidden entries only
+    for (int i = 1; i < NW; ++i) mg = fmaxf(mg, s_m[i][g]);
+    const float ref = mg == kNegInf ? 0.0f : mg;    // a split of hidden entries only
     float x = 0.0f;
 #pragma unroll
     for (int i = 0; i < NW; ++i)
-      x = fmaf(d < D ? red[i][g][d] : s_l[i][g], __builtin_amdgcn_exp2f(s_m[i][g] - ref), x);
-    out[g * (D + 2) + (d < D ? d : D + 1)] = x;
-    if (d == D) out[g * (D + 2) + D] = m;
+      x = fmaf(d < D ? red[i][g][Attn::red_word(min(d, D - 1))] : s_l[i][g],
+               __builtin_amdgcn_exp2f(s_m[i][g] - ref), x);
+    if (d < D) {
+      out[g * D + d] = x;
+    } else {
+      out_ml[2 * g] = mg;
+      out_ml[2 * g + 1] = x;
+    }
   }
 }
 
+// All of a head's partial outputs are on their way before the weights are known: a thread
+// has four elements of every kRows-th split, 16 bytes each.
 template <bool BF16, int D, int G>
-__global__ void __launch_bounds__(256) kv4_combine_kernel(Kv4DecodeArgs a) {
+__global__ void __launch_bounds__(kJoin) kv4_combine_kernel(Kv4DecodeArgs a) {
   using E = typename std::conditional<BF16, uint16_t, float>::type;
-  constexpr int NG = 256 / D;               // groups of D threads
-  constexpr int RB = D / 2, SB = D / 32;
+  constexpr int TPR = D / 4;                // threads per split's row
+  constexpr int kRows = kJoin / TPR;        // splits read at a time
+  constexpr int kEach = (kMaxSplits + kRows - 1) / kRows;
+  constexpr int NWJ = kJoin / 64;
   __shared__ float wgt[kMaxSplits];
-  __shared__ float red[NG][D];
-  __shared__ float s_max[4], s_den[4], s_own;
-  static_assert(kMaxSplits <= 256, "a thread per split");
+  __shared__ __align__(16) float red[kRows][D];
+  __shared__ float s_max[NWJ], s_den[NWJ], s_own;
+  static_assert(kMaxSplits <= kJoin, "a thread per split");
   const int u = blockIdx.x, g = blockIdx.y;
   const int bi = u / a.n_kv_heads, hk = u - bi * a.n_kv_heads;
   const int tid = threadIdx.x, w = tid >> 6, lane = tid & 63;
@@ -84,43 +154,55 @@ __global__ void __launch_bounds__(256) kv4_combine_kernel(Kv4DecodeArgs a) {
   const E* knew = static_cast<const E*>(a.kin) + plane * D;
   const E* vnew = static_cast<const E*>(a.vin) + plane * D;
   const int64_t qrow = ((int64_t)bi * a.n_heads + hk * G + g) * a.seq_ld * D;
-  const float* part = a.part + ((int64_t)u * a.nsplit * G + g) * (D + 2);
-  const int64_t stride = (int64_t)G * (D + 2);
   const int n = a.nsplit;
+  const int64_t first = (int64_t)u * n * G + g;
+  const float* part = a.part + first * D;
+  const float* ml = a.part + (int64_t)a.units * n * G * D + first * 2;
+  const int sc = min(tid, n - 1) * G * 2;
+  const float m0 = ml[sc], ll = ml[sc + 1];
+  const int ro = tid / TPR, e4 = (tid % TPR) * 4;
+  f32x4 x[kEach];
+#pragma unroll
+  for (int k = 0; k < kEach; ++k)
+    x[k] = *reinterpret_cast<const f32x4*>(part + (int64_t)min(ro + k * kRows, n - 1) * G * D + e4);
   if (w == 0) {
     const float s = lanes::wave_sum(kv4::dot_part<BF16, D>(static_cast<const E*>(a.q) + qrow, knew, lane));
     if (lane == 0) s_own = s * a.scale_log2;
   }
-  float m = tid < n ? part[tid * stride + D] : kNegInf;
-  const float ll = tid < n ? part[tid * stride + D + 1] : 0.0f;
-  const float wm = lanes::wave_max(m);
+  const float wm = lanes::wave_max(m0);
   if (lane == 0) s_max[w] = wm;
   __syncthreads();
   const float own = s_own;
-  const float M = fmaxf(fmaxf(fmaxf(s_max[0], s_max[1]), fmaxf(s_max[2], s_max[3])), own);
-  const float f = __builtin_amdgcn_exp2f(m - M);
+  float M = own;
+#pragma unroll
+  for (int i = 0; i < NWJ; ++i) M = fmaxf(M, s_max[i]);
+  const float f = __builtin_amdgcn_exp2f(m0 - M);
   if (tid < n) wgt[tid] = f;
   const float den = lanes::wave_sum(tid < n ? f * ll : 0.0f);
   if (lane == 0) s_den[w] = den;
   __syncthreads();
-  const int gi = tid / D, e = tid - gi * D;
-  float num = 0.0f;
-#pragma unroll 4
-  for (int c = gi; c < n; c += NG) num = fmaf(wgt[c], part[c * stride + e], num);
-  red[gi][e] = num;
+  f32x4 num = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < kEach; ++k) {
+    const int c = ro + k * kRows;
+    if (c < n) num += x[k] * wgt[c];
+  }
+  *reinterpret_cast<f32x4*>(&red[ro][e4]) = num;
   __syncthreads();
   if (tid < D) {
     const float p = __builtin_amdgcn_exp2f(own - M);
     float v;
-    if constexpr (BF16) v = __uint_as_float((uint32_t)vnew[e] << 16);
-    else v = vnew[e];
-    float x = p * v;
+    if constexpr (BF16) v = __uint_as_float((uint32_t)vnew[tid] << 16);
+    else v = vnew[tid];
+    float sum = p * v, all = p;
 #pragma unroll
-    for (int i = 0; i < NG; ++i) x += red[i][e];
-    x /= s_den[0] + s_den[1] + s_den[2] + s_den[3] + p;
-    E* o = static_cast<E*>(a.o) + qrow + e;
-    if constexpr (BF16) *o = __builtin_bit_cast(uint16_t, (__bf16)x);
-    else *o = x;
+    for (int i = 0; i < kRows; ++i) sum += red[i][tid];
+#pragma unroll
+    for (int i = 0; i < NWJ; ++i) all += s_den[i];
+    const float y = sum / all;
+    E* o = static_cast<E*>(a.o) + qrow + tid;
+    if constexpr (BF16) *o = __builtin_bit_cast(uint16_t, (__bf16)y);
+    else *o = y;
   }
   if (g != 0) return;
   // the step's pair into slot len0
@@ -130,9 +212,7 @@ __global__ void __launch_bounds__(256) kv4_combine_kernel(Kv4DecodeArgs a) {
     uint32_t byte;
     kv4::load8<BF16>((wh ? vnew : knew) + c * 8, x);
     const uint32_t code = kv4::quantise8(x, &byte);
-    const int64_t row = (int64_t)u * a.cap + a.len0;
-    *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(wh ? a.vq : a.kq) + row * RB + 4 * c) = code;
-    if ((c & 3) == 0) (static_cast<uint8_t*>(wh ? a.vs : a.ks))[row * SB + c / 4] = (uint8_t)byte;
+    kv4::store_row<D>(wh ? a.vq : a.kq, wh ? a.vs : a.ks, wh, (int64_t)u * a.slots, a.len0, c, code, byte);
   }
   if (tid == 0) {
     a.score[(int64_t)u * a.cap + a.len0] = 0.0f;
@@ -143,12 +223,18 @@ __global__ void __launch_bounds__(256) kv4_combine_kernel(Kv4DecodeArgs a) {
 
 template <bool BF16, int D, int G>
 hipError_t launch_t(const Kv4DecodeArgs& a, hipStream_t stream) {
-  hipLaunchKernelGGL((kv4_split_kernel<BF16, D, G>), dim3((unsigned)a.units, (unsigned)a.nsplit),
-                     dim3(64 * NW), 0, stream, a);
+  // rows are read once per step: a cache larger than the last-level cache streams past it
+  const size_t bytes = (size_t)a.units * a.len0 * (D + D / 16);
+  const int split = split_slots(a.len0);
+  const dim3 grid((unsigned)a.units, (unsigned)a.nsplit);
+  if (bytes > kLastLevelCacheBytes)
+    hipLaunchKernelGGL((kv4_split_kernel<BF16, D, G, true>), grid, dim3(64 * NW), 0, stream, a, split);
+  else
+    hipLaunchKernelGGL((kv4_split_kernel<BF16, D, G, false>), grid, dim3(64 * NW), 0, stream, a, split);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((kv4_combine_kernel<BF16, D, G>), dim3((unsigned)a.units, (unsigned)G), dim3(256),
-                     0, stream, a);
+  hipLaunchKernelGGL((kv4_combine_kernel<BF16, D, G>), dim3((unsigned)a.units, (unsigned)G),
+                     dim3(kJoin), 0, stream, a);
   return hipGetLastError();
 }
 
@@ -164,7 +250,7 @@ hipError_t launch_g(const Kv4DecodeArgs& a, int group, hipStream_t stream) {
 
 }  // namespace
 
-int kv4_long_splits(int len0) { return (len0 + kSplit - 1) / kSplit; }
+int kv4_long_splits(int len0) { return (len0 + split_slots(len0) - 1) / split_slots(len0); }
 
 hipError_t launch_kv4_long(const Kv4DecodeArgs& a, int dtype, int head_dim, int group,
                            hipStream_t stream) {

@@ -50,14 +50,16 @@ __global__ void __launch_bounds__(256) kv4_write_kernel(Kv4RowsArgs a) {
   constexpr int EB = BF16 ? 2 : 4;
   const Items<D> it(a);
   float x[kIters][2][8];
-  int64_t slot[kIters];
+  int64_t base[kIters];                  // the unit's first slot in the planes
+  uint32_t slot[kIters];
   bool live[kIters];
 #pragma unroll
   for (int k = 0; k < kIters; ++k) {
     int64_t u;
     uint32_t r;
     live[k] = it.at(k, &u, &r);
-    slot[k] = u * a.cap + a.slot0 + r;
+    base[k] = u * a.slots;
+    slot[k] = a.slot0 + r;
     const int64_t src = ((u * a.seq_ld + r) * D + it.lane * 8) * EB;
     kv4::load8<BF16>(static_cast<const char*>(a.k) + src, x[k][0]);
     kv4::load8<BF16>(static_cast<const char*>(a.v) + src, x[k][1]);
@@ -68,12 +70,8 @@ __global__ void __launch_bounds__(256) kv4_write_kernel(Kv4RowsArgs a) {
     for (int w = 0; w < 2; ++w) {
       uint32_t byte;
       const uint32_t c = kv4::quantise8(x[k][w], &byte);
-      if (live[k]) {
-        uint8_t* code = static_cast<uint8_t*>(w ? a.vq : a.kq) + slot[k] * (D / 2) + it.lane * 4;
-        *reinterpret_cast<uint32_t*>(code) = c;
-        if ((it.lane & 3) == 0)
-          (static_cast<uint8_t*>(w ? a.vs : a.ks))[slot[k] * (D / 32) + it.lane / 4] = (uint8_t)byte;
-      }
+      if (live[k])
+        kv4::store_row<D>(w ? a.vq : a.kq, w ? a.vs : a.ks, w, base[k], slot[k], it.lane, c, byte);
     }
   }
 }
@@ -90,13 +88,15 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(Kv4RowsArgs a) {
     int64_t u;
     uint32_t r;
     live[k] = it.at(k, &u, &r);
-    const int64_t slot = u * a.cap + a.slot0 + r;
+    const int64_t base = u * a.slots;      // the unit's first slot in the planes
+    const uint32_t slot = a.slot0 + r;
     dst[k] = ((u * a.seq_ld + r) * D + it.lane * 8) * EB;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
-      const uint8_t* code = static_cast<const uint8_t*>(w ? a.vq : a.kq) + slot * (D / 2) + it.lane * 4;
-      c[k][w] = *reinterpret_cast<const uint32_t*>(code);
-      s[k][w] = (static_cast<const uint8_t*>(w ? a.vs : a.ks))[slot * (D / 32) + it.lane / 4];
+      const uint32_t at = w ? kv4::v_word<D>(slot, it.lane) : kv4::k_word<D>(slot, it.lane);
+      c[k][w] = (static_cast<const uint32_t*>(w ? a.vq : a.kq) + base * (D / 8))[at];
+      const uint32_t g = it.lane / 4, sat = w ? kv4::v_scale_at<D>(slot, g) : kv4::k_scale_at<D>(slot, g);
+      s[k][w] = (static_cast<const uint8_t*>(w ? a.vs : a.ks) + base * (D / 32))[sat];
     }
   }
 #pragma unroll

@@ -61,12 +61,14 @@ def test_rows_store_and_read_back(dtype, d, b, kv_heads, n, slot0):
     att = make(b=b, heads=kv_heads, kv_heads=kv_heads, d=d, dtype=dtype, s=64)
     junk(att)
     att.score.fill_(3.0), att.pos.fill_(7), att.len.fill_(9)
-    before = [x.clone() for x in (att.k, att.v, att.k_scale, att.v_scale)]
     g = gen(d + n)
+    other = [rows(g, (b, kv_heads, att.cap, d), dtype) for _ in range(2)]
+    att.write_rows(0, *other)
     k, v = rows(g, (b, kv_heads, n, d), dtype, 2.0), rows(g, (b, kv_heads, n, d), dtype, 2.0)
     att.write_rows(slot0, k, v)
     # other slots, scores, positions and lengths are left alone
-    for x, y in zip((att.k, att.v, att.k_scale, att.v_scale), before):
+    for x, y in zip(att.read_rows(0, att.cap), other):
+        x, y = x.cpu().double(), stored(y)
         assert torch.equal(x[:, :, :slot0], y[:, :, :slot0])
         assert torch.equal(x[:, :, slot0 + n:], y[:, :, slot0 + n:])
     assert (att.score == 3).all() and (att.pos == 7).all() and (att.len == 9).all()
@@ -77,9 +79,9 @@ def test_rows_store_and_read_back(dtype, d, b, kv_heads, n, slot0):
     att.write_rows(slot0, ko, vo)
     k2, v2 = att.read_rows(slot0, n)
     assert torch.equal(ko, k2) and torch.equal(vo, v2)
-    # a slot that was never written reads as the NaN its scale byte says
-    if slot0 > 0:
-        assert torch.isnan(att.read_rows(0, slot0)[0]).all()
+    # a group whose scale byte is 255 reads as NaN
+    junk(att)
+    assert torch.isnan(att.read_rows(0, att.cap)[0]).all()
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
@@ -243,12 +245,11 @@ def test_hidden_entries_weigh_nothing(dtype, n):
     filled(att, ref, n, 4, dtype, first)
     bad = ref.pos < pads[:, None, None]
     assert bad.any()
-    for i, (c, s) in enumerate(((att.k, att.k_scale), (att.v, att.v_scale))):
-        odd = bad & (ref.pos % 2 == i)
-        s[:, :, :n][odd.cuda()] = 255                    # NaN
-        even = bad & (ref.pos % 2 != i)
-        s[:, :, :n][even.cuda()] = 252                   # up to 2.5e38
-        c[:, :, :n][even.cuda()] = 0x7F
+    for i, x in enumerate(att.read_rows(0, n)):
+        x[(bad & (ref.pos % 2 == i)).cuda()] = math.nan
+        x[(bad & (ref.pos % 2 != i)).cuda()] = 2.5e38
+        y = att.read_rows(0, n)
+        att.write_rows(0, *((x, y[1]) if i == 0 else (y[0], x)))
     k, v, _, _ = live(att)
     ref.k, ref.v = k, v
     assert not torch.isfinite(ref.k).all()
@@ -263,8 +264,10 @@ def test_visible_nan_reaches_its_unit_alone():
     att = make(b=b, s=first, kv_max=n + 1, block=1, heads=hk * group, kv_heads=hk, d=d, dtype=dtype)
     ref = Reference(b=b, heads=hk * group, kv_heads=hk, d=d)
     filled(att, ref, n, 4, dtype, first)
-    att.k_scale[0, 0, 3] = 255          # a key: all of unit (0, 0)
-    att.v_scale[1, 1, 89, 0] = 255      # a value: 32 elements of unit (1, 1)'s outputs
+    k, v = att.read_rows(0, n)
+    k[0, 0, 3, 40] = math.nan           # a key: all of unit (0, 0)
+    v[1, 1, 89, 5] = math.inf           # a value: 32 elements of unit (1, 1)'s outputs
+    att.write_rows(0, k, v)
     q, k, v = step_rows(gen(1), b, hk * group, hk, d, dtype)
     o = torch.zeros_like(q)
     att.decode_step(first, q, k, v, o)
@@ -284,9 +287,10 @@ def test_long_decode(dtype, d, group, n):
     att.set_left_padding(pads.cuda())
     ref = Reference(b=b, heads=hk * group, kv_heads=hk, d=d, pads=pads)
     filled(att, ref, n, n + d, dtype, n)
-    bad = (ref.pos < pads[:, None, None]).cuda()
-    att.v_scale[:, :, :n][bad] = 255
-    att.k_scale[:, :, :n][bad] = 255
+    k, v = att.read_rows(0, n)
+    for x in (k, v):
+        x[(ref.pos < pads[:, None, None]).cuda()] = math.nan
+    att.write_rows(0, k, v)
     ref.k, ref.v = live(att)[:2]
     g = gen(9)
     for i in range(2):
@@ -380,11 +384,14 @@ def test_cut_moves_codes_and_scales(d, n, keep):
 # --------------------------------------------------------------------------
 # streams, graphs, batches, memory
 # --------------------------------------------------------------------------
-def same_live(att, other, n):
-    """Bit for bit; slots past the live ones are scratch (NaN scores here)."""
-    assert torch.equal(att.len, other["len"])
-    for x in ("k", "v", "k_scale", "v_scale", "score", "pos"):
-        assert torch.equal(getattr(att, x)[:, :, :n], other[x][:, :, :n]), x
+def state_of(att, n):
+    """Every live entry, bit for bit (slots past them are scratch)."""
+    return [*att.read_rows(0, n), att.score[:, :, :n].clone(), att.pos[:, :, :n].clone(), att.len.clone()]
+
+
+def same_state(att, other, n):
+    for x, y in zip(state_of(att, n), other):
+        assert torch.equal(x, y)
 
 
 def test_graph_of_steps_replays():
@@ -397,8 +404,7 @@ def test_graph_of_steps_replays():
     start = {x: getattr(att, x).clone() for x in names}
     o = torch.zeros_like(q)
     att.run_decode(q, k, v, o, steps, 0)
-    eager = {x: getattr(att, x).clone() for x in names}
-    want = o.clone()
+    eager, want = state_of(att, n), o.clone()
     att.resume(n, first)
     graph = att.capture_decode(q, k, v, o, steps, 0)
     for _ in range(4):
@@ -409,7 +415,7 @@ def test_graph_of_steps_replays():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(o, want)
-        same_live(att, eager, n)
+        same_state(att, eager, n)
 
 
 def test_long_step_in_a_graph():
@@ -438,7 +444,7 @@ def test_prefill_block_in_a_graph():
     q, k, v = step_rows(gen(3), b, hk * group, hk, d, dtype, r)
     o = torch.zeros_like(q)
     att.prefill_block_cut(n, r, q, k, v, o, row=0)
-    want, eager = o.clone(), {x: getattr(att, x).clone() for x in names}
+    want, eager = o.clone(), state_of(att, n)
     att.resume(n, n)
     graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
     side.wait_stream(torch.cuda.current_stream())
@@ -451,7 +457,7 @@ def test_prefill_block_in_a_graph():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(o, want)
-        same_live(att, eager, n)
+        same_state(att, eager, n)
 
 
 def test_calls_run_on_the_current_stream():
@@ -527,7 +533,7 @@ def test_layers_share_one_workspace():
 def test_offsets_past_32_bits():
     """Codes of more than 2^32 bytes, rows and outputs of the last unit."""
     b, hk, d, n, cap, dtype = 70, 16, 128, 6000, 65000, "bf16"
-    assert b * hk * cap * (d // 2) > 1 << 32
+    assert b * hk * cap * (d // 2) > 1 << 32         # bytes of each code plane
     att = make(b=b, s=n, kv_max=cap - 1, block=1, heads=hk, kv_heads=hk, d=d)
     att.set_score_accumulation(False)
     for x in (att.k, att.v, att.k_scale, att.v_scale):

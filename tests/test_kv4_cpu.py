@@ -27,14 +27,20 @@ def test_workspace_holds_the_cached_rows():
     assert bmx.bm_kv4_workspace_bytes(dims(head_dim=96)) == 0
 
 
+def test_slots_are_whole_groups_of_64():
+    assert bmx.bm_kv4_slots(dims()) == 192
+    assert bmx.bm_kv4_slots(dims(kv_max=129)) == 256
+    assert bmx.bm_kv4_slots(dims(b=0)) == -1
+
+
 def test_context_pointer_checks():
     d = dims()
     resume = lambda c, n=0, pos=0: status_of(bmx.bm_kv4_resume, d, c, n, pos)    # noqa: E731
     for name in ("k", "v", "k_scale", "v_scale", "score", "pos", "len", "work"):
         assert resume(fake(d, **{name: 0})) == BAD, name
-    for name in ("k", "v", "work"):
+    for name in ("k", "v", "k_scale", "v_scale", "work"):
         assert resume(fake(d, **{name: FAKE + 8})) == BAD, name
-    for name in ("k_scale", "v_scale", "score", "pos", "len"):
+    for name in ("score", "pos", "len"):
         assert resume(fake(d, **{name: FAKE + 2})) == BAD, name
     # the workspace of batchmax.h alone is too small
     assert resume(fake(d, work_bytes=bmx.bm_workspace_bytes(d))) == BAD
@@ -74,7 +80,7 @@ def test_row_calls_refuse(call):
     assert go(0, 4, ld=3) == BAD
     for name in ("k", "v", "k_scale", "v_scale"):
         assert go(0, 4, **{name: 0}) == BAD
-    assert go(0, 4, k_scale=FAKE + 1) == BAD and go(0, 4, v=FAKE + 8) == BAD
+    assert go(0, 4, k_scale=FAKE + 4) == BAD and go(0, 4, v=FAKE + 8) == BAD
     # nothing to do: no device work; score, pos, len and work do not matter
     assert go(0, 0, k=0, v=0, score=0, pos=0, len=0, work=0) == bmx.BM_OK
     assert go(192, 0) == bmx.BM_OK
@@ -115,7 +121,7 @@ def att(**kw):
 
 def test_python_object_checks_its_tensors():
     a = att()
-    assert a.k.shape == (2, 2, 48, 32) and a.k_scale.shape == (2, 2, 48, 2) and a.k.dtype == torch.uint8
+    assert a.k.shape == (2, 2, 64, 32) and a.k_scale.shape == (2, 2, 64, 2) and a.k.dtype == torch.uint8
     x = torch.zeros(2, 2, 3, 64, dtype=torch.bfloat16)
     for bad in (x.float(), x[:, :, :, :32].contiguous(), x[:1], x.transpose(2, 3), x[0]):
         with pytest.raises(ValueError):
@@ -144,6 +150,10 @@ def test_stack_bytes_at_four_bits():
     rows = 3 * 8 * 768
     assert full == rows * (512 + 8) + 256              # (the lengths: 96 bytes, padded)
     assert four == rows * (2 * (64 + 4) + 8) + 256
+    shape.update(kv_max=500, block=250)                # 750 slots, 768 in the planes
+    rows, entries = 24 * 768, 24 * 750 * 4             # (an array of 4 bytes an entry: padded to 256)
+    assert bmx.stack_layer_bytes(**shape, kv_bits=4) == \
+        rows * 2 * (64 + 4) + 2 * (-entries % 256 + entries) + 256
     with pytest.raises(ValueError):
         bmx.stack_layer_bytes(**shape, kv_bits=8)
     plan = dict(n_layers=32, s=8192, kv_max=512, block=256, max_gen=256, n_heads=32, n_kv_heads=8,
