@@ -663,8 +663,15 @@ class PDAttentionKV4(PDAttention):
         return bm_kv4_resume(self.dims, self.cache, length, next_pos)
 
     def _rows(self, k, v):
+        """Rows of k and v, checked with few torch calls; what is wrong is named on failure."""
+        s, d = k.shape, self.dims
+        if (len(s) == 4 and s == v.shape and s == (d.b, d.n_kv_heads, s[2], d.head_dim)
+                and k.dtype is self.tdtype and v.dtype is self.tdtype
+                and k.get_device() == self._dev_index and v.get_device() == self._dev_index
+                and k.is_contiguous() and v.is_contiguous()):
+            return s[2]
         for x, nm in ((k, "k"), (v, "v")):
-            self._check_tensor(x, self.dims.n_kv_heads, nm)
+            self._check_tensor(x, d.n_kv_heads, nm)
         if k.shape[2] != v.shape[2]:
             raise ValueError("k and v need the same number of rows")
         return k.shape[2]

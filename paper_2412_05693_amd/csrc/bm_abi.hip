@@ -376,14 +376,16 @@ int kv4_rows(const bm_dims* dims, const bm_kv4_cache* cache, int32_t slot0, int3
   a.slots = bm::kv4_slots(dims->kv_max + dims->block);
   a.slot0 = slot0;
   a.n = n;
-  const hipError_t e = bm::launch_kv4_rows(a, write, dims->dtype, dims->head_dim, stream);
+  const bm::Kv4RowsArgs none;
+  const hipError_t e =
+      bm::launch_kv4_rows(write ? none : a, write ? a : none, dims->dtype, dims->head_dim, stream);
   if (e != hipSuccess) return hip_fail(e, write ? "4-bit write launch" : "4-bit read launch");
   return ok();
 }
 
-// The same on a context's cache, unchecked.
-hipError_t ctx_rows(const bm_ctx* ctx, int slot0, int n, const void* k, const void* v,
-                    int64_t seq_ld, bool write, hipStream_t stream) {
+// Rows of a context's cache, for launch_kv4_rows.
+bm::Kv4RowsArgs ctx_rows(const bm_ctx* ctx, int slot0, int n, const void* k, const void* v,
+                         int64_t seq_ld) {
   bm::Kv4RowsArgs a;
   a.k = k;
   a.v = v;
@@ -396,7 +398,7 @@ hipError_t ctx_rows(const bm_ctx* ctx, int slot0, int n, const void* k, const vo
   a.slots = bm::kv4_slots(ctx->cap);
   a.slot0 = slot0;
   a.n = n;
-  return bm::launch_kv4_rows(a, write, ctx->dims.dtype, ctx->dims.head_dim, stream);
+  return a;
 }
 
 }  // namespace
@@ -497,20 +499,18 @@ int prefill_args(bm_ctx* ctx, int32_t t0, int32_t n_tok, const void* q, const vo
   return BM_OK;
 }
 
-// Enqueue a checked block's attention (a 4-bit cache: between the reading of its rows
-// and the storing of the block's) and the caller's event behind it.
+// Enqueue a checked block's attention (a 4-bit cache: behind the reading of its rows and
+// the storing of the block's) and the caller's event behind it.
 int attend(bm_ctx* ctx, const bm::PrefillArgs& a, hipStream_t stream) {
   hipError_t e;
-  if (ctx->k_scale && a.len0 > 0) {
-    e = ctx_rows(ctx, 0, a.len0, a.kc, a.vc, ctx->cap, false, stream);
-    if (e != hipSuccess) return hip_fail(e, "4-bit read launch");
+  if (ctx->k_scale) {
+    e = bm::launch_kv4_rows(ctx_rows(ctx, 0, a.len0, a.kc, a.vc, ctx->cap),
+                            ctx_rows(ctx, a.len0, a.n_tok, a.kin, a.vin, a.seq_ld), ctx->dims.dtype,
+                            ctx->dims.head_dim, stream);
+    if (e != hipSuccess) return hip_fail(e, "4-bit rows launch");
   }
   e = bm::launch_prefill(a, ctx->dims.dtype, ctx->dims.head_dim, ctx->group, stream);
   if (e != hipSuccess) return hip_fail(e, "prefill launch");
-  if (ctx->k_scale) {
-    e = ctx_rows(ctx, a.len0, a.n_tok, a.kin, a.vin, a.seq_ld, true, stream);
-    if (e != hipSuccess) return hip_fail(e, "4-bit write launch");
-  }
   if (ctx->split && (e = hipEventRecord(ctx->split, stream)) != hipSuccess)
     return hip_fail(e, "split event record");
   return BM_OK;

@@ -162,14 +162,14 @@ struct Kv4DecodeArgs {
 
 // Rows 0 .. n - 1 of [U, seq_ld, D] buffers to or from slots slot0 .. of a 4-bit cache.
 struct Kv4RowsArgs {
-  const void* k;      // (a read writes through them)
-  const void* v;
-  void* kq;
-  void* vq;
-  void* ks;
-  void* vs;
-  int64_t seq_ld;
-  int units, slots, slot0, n;
+  const void* k = nullptr;    // (a read writes through them)
+  const void* v = nullptr;
+  void* kq = nullptr;
+  void* vq = nullptr;
+  void* ks = nullptr;
+  void* vs = nullptr;
+  int64_t seq_ld = 0;
+  int units = 0, slots = 0, slot0 = 0, n = 0;
 };
 
 struct SynthArgs {
@@ -203,8 +203,9 @@ hipError_t launch_kv4_decode(const Kv4DecodeArgs& a, int dtype, int head_dim, in
 int kv4_long_splits(int len0);
 hipError_t launch_kv4_long(const Kv4DecodeArgs& a, int dtype, int head_dim, int group,
                            hipStream_t stream);
-hipError_t launch_kv4_rows(const Kv4RowsArgs& a, bool write, int dtype, int head_dim,
-                           hipStream_t stream);
+// read rows, then (independently: no slot and no row twice) write rows; either may have n = 0
+hipError_t launch_kv4_rows(const Kv4RowsArgs& read, const Kv4RowsArgs& write, int dtype,
+                           int head_dim, hipStream_t stream);
 hipError_t launch_reset(float* score, int32_t* len, size_t n_score, size_t n_len,
                         hipStream_t stream);
 hipError_t launch_synth_qkv(const SynthArgs& a, hipStream_t stream);

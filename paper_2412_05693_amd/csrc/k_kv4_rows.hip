@@ -12,19 +12,18 @@ namespace {
 
 using kv4::u32x4;
 
-constexpr int kIters = 4;   // row pairs a lane moves, loads of all of them in flight
-
-// Item i of a launch is row i % n of unit i / n.  A workgroup's first item is split
-// with one 64-bit division, the rest with 32-bit ones (n <= 65536).
-template <int D>
+// Item i of a launch is row i % n of unit i / n; a lane takes ITERS of them, the loads of
+// all in flight.  A workgroup's first item is split with one 64-bit division, the rest
+// with 32-bit ones (n <= 65536).
+template <int D, int ITERS>
 struct Items {
   static constexpr int kLanes = D / 8;              // lanes per row
   static constexpr int kRows = 256 / kLanes;        // rows a workgroup moves at a time
   int64_t u0, left;
   uint32_t r0, n;
   int lane, first;
-  __device__ __forceinline__ Items(const Kv4RowsArgs& a) {
-    const int64_t i0 = (int64_t)blockIdx.x * (kRows * kIters);
+  __device__ __forceinline__ Items(const Kv4RowsArgs& a, int64_t block) {
+    const int64_t i0 = block * (kRows * ITERS);
     u0 = i0 / a.n;
     r0 = (uint32_t)(i0 - u0 * a.n);
     n = (uint32_t)a.n;
@@ -45,16 +44,16 @@ struct Items {
   }
 };
 
-template <bool BF16, int D>
-__global__ void __launch_bounds__(256) kv4_write_kernel(Kv4RowsArgs a) {
+template <bool BF16, int D, int ITERS>
+__device__ __forceinline__ void write_rows(const Kv4RowsArgs& a, int64_t block) {
   constexpr int EB = BF16 ? 2 : 4;
-  const Items<D> it(a);
-  float x[kIters][2][8];
-  int64_t base[kIters];                  // the unit's first slot in the planes
-  uint32_t slot[kIters];
-  bool live[kIters];
+  const Items<D, ITERS> it(a, block);
+  float x[ITERS][2][8];
+  int64_t base[ITERS];                   // the unit's first slot in the planes
+  uint32_t slot[ITERS];
+  bool live[ITERS];
 #pragma unroll
-  for (int k = 0; k < kIters; ++k) {
+  for (int k = 0; k < ITERS; ++k) {
     int64_t u;
     uint32_t r;
     live[k] = it.at(k, &u, &r);
@@ -65,7 +64,7 @@ __global__ void __launch_bounds__(256) kv4_write_kernel(Kv4RowsArgs a) {
     kv4::load8<BF16>(static_cast<const char*>(a.v) + src, x[k][1]);
   }
 #pragma unroll
-  for (int k = 0; k < kIters; ++k) {
+  for (int k = 0; k < ITERS; ++k) {
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
       uint32_t byte;
@@ -76,15 +75,15 @@ __global__ void __launch_bounds__(256) kv4_write_kernel(Kv4RowsArgs a) {
   }
 }
 
-template <bool BF16, int D>
-__global__ void __launch_bounds__(256) kv4_read_kernel(Kv4RowsArgs a) {
+template <bool BF16, int D, int ITERS>
+__device__ __forceinline__ void read_rows(const Kv4RowsArgs& a, int64_t block) {
   constexpr int EB = BF16 ? 2 : 4;
-  const Items<D> it(a);
-  uint32_t c[kIters][2], s[kIters][2];
-  int64_t dst[kIters];
-  bool live[kIters];
+  const Items<D, ITERS> it(a, block);
+  uint32_t c[ITERS][2], s[ITERS][2];
+  int64_t dst[ITERS];
+  bool live[ITERS];
 #pragma unroll
-  for (int k = 0; k < kIters; ++k) {
+  for (int k = 0; k < ITERS; ++k) {
     int64_t u;
     uint32_t r;
     live[k] = it.at(k, &u, &r);
@@ -100,7 +99,7 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(Kv4RowsArgs a) {
     }
   }
 #pragma unroll
-  for (int k = 0; k < kIters; ++k) {
+  for (int k = 0; k < ITERS; ++k) {
     if (!live[k]) continue;
 #pragma unroll
     for (int w = 0; w < 2; ++w) {
@@ -123,26 +122,43 @@ __global__ void __launch_bounds__(256) kv4_read_kernel(Kv4RowsArgs a) {
   }
 }
 
-template <bool BF16, int D>
-hipError_t launch_t(const Kv4RowsArgs& a, bool write, hipStream_t stream) {
-  constexpr int64_t per = Items<D>::kRows * kIters;
-  const int64_t blocks = ((int64_t)a.units * a.n + per - 1) / per;
-  if (blocks > 0xFFFFFF) return hipErrorInvalidValue;   // 2^32 threads a launch
-  const dim3 grid((unsigned)blocks);
-  if (write)
-    hipLaunchKernelGGL((kv4_write_kernel<BF16, D>), grid, dim3(256), 0, stream, a);
+// Both directions in one launch: workgroups below `reads` read rows, the others write.
+template <bool BF16, int D, int ITERS>
+__global__ void __launch_bounds__(256) kv4_rows_kernel(Kv4RowsArgs r, Kv4RowsArgs w, int reads) {
+  if ((int)blockIdx.x < reads)
+    read_rows<BF16, D, ITERS>(r, blockIdx.x);
   else
-    hipLaunchKernelGGL((kv4_read_kernel<BF16, D>), grid, dim3(256), 0, stream, a);
+    write_rows<BF16, D, ITERS>(w, (int)blockIdx.x - reads);
+}
+
+// Row pairs of a launch from which a lane takes four: fewer leave workgroups for every
+// compute unit only if it takes one.
+constexpr int64_t kManyRows = 1 << 16;
+
+template <bool BF16, int D, int ITERS>
+hipError_t launch_i(const Kv4RowsArgs& r, const Kv4RowsArgs& w, hipStream_t stream) {
+  constexpr int64_t per = Items<D, ITERS>::kRows * ITERS;
+  const int64_t reads = ((int64_t)r.units * r.n + per - 1) / per;
+  const int64_t blocks = reads + ((int64_t)w.units * w.n + per - 1) / per;
+  if (blocks > 0xFFFFFF) return hipErrorInvalidValue;   // 2^32 threads a launch
+  hipLaunchKernelGGL((kv4_rows_kernel<BF16, D, ITERS>), dim3((unsigned)blocks), dim3(256), 0, stream, r, w,
+                     (int)reads);
   return hipGetLastError();
+}
+
+template <bool BF16, int D>
+hipError_t launch_t(const Kv4RowsArgs& r, const Kv4RowsArgs& w, hipStream_t stream) {
+  const bool many = (int64_t)r.units * r.n + (int64_t)w.units * w.n >= kManyRows;
+  return many ? launch_i<BF16, D, 4>(r, w, stream) : launch_i<BF16, D, 1>(r, w, stream);
 }
 
 }  // namespace
 
-hipError_t launch_kv4_rows(const Kv4RowsArgs& a, bool write, int dtype, int head_dim,
+hipError_t launch_kv4_rows(const Kv4RowsArgs& r, const Kv4RowsArgs& w, int dtype, int head_dim,
                            hipStream_t stream) {
   if (dtype == BM_BF16)
-    return head_dim == 128 ? launch_t<true, 128>(a, write, stream) : launch_t<true, 64>(a, write, stream);
-  return head_dim == 128 ? launch_t<false, 128>(a, write, stream) : launch_t<false, 64>(a, write, stream);
+    return head_dim == 128 ? launch_t<true, 128>(r, w, stream) : launch_t<true, 64>(r, w, stream);
+  return head_dim == 128 ? launch_t<false, 128>(r, w, stream) : launch_t<false, 64>(r, w, stream);
 }
 
 }  // namespace bm
