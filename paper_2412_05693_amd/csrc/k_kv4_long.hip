@@ -58,14 +58,19 @@ __global__ void __launch_bounds__(64 * NW, BF16 ? 3 : 2) kv4_split_kernel(Kv4Dec
   at.load_q(qb, a.seq_ld * D, q);
   Attn::clear(o);
   float m = kNegInf, l = 0.0f;             // running maximum, this lane's part of the sum
-  for (int base = c * split + w * kChunk; base < end; base += NW * kChunk) {
-    const int rows = end - base;
-    typename Attn::KRows k;
-    typename Attn::VRows v;
+  // A chunk's rows of K are dead once its logits are formed, those of V once they are added:
+  // the next chunk's loads take their registers there, and are on their way during the
+  // other half of the work.
+  typename Attn::KRows k;
+  typename Attn::VRows v;
+  int base = c * split + w * kChunk;
+  at.load_k(pl, base, end - base, k);
+  at.load_v(pl, base, end - base, v);
+  for (; base < end; base += NW * kChunk) {
+    const int rows = end - base, next = base + NW * kChunk;
     typename Attn::Logits z;
-    at.load_k(pl, base, rows, k);
-    at.load_v(pl, base, rows, v);
     at.logits(k, q, a.scale_log2, rows, z);
+    at.load_k(pl, next, end - next, k);
     if (pad > 0)
       at.pads(pl, base, rows, pad, [&](int e) {
         z[e] = kNegInf;
@@ -102,6 +107,7 @@ __global__ void __launch_bounds__(64 * NW, BF16 ? 3 : 2) kv4_split_kernel(Kv4Dec
       }
       at.add_values(v, x, pw, o);
     }
+    at.load_v(pl, next, end - next, v);
   }
   l = lanes::add_xor<32>(lanes::add_xor<16>(l));
   if (lane < G) {
