@@ -13,9 +13,10 @@ def stored(x):
     out = torch.empty_like(g)
     top = g.abs().amax(dim=-1)
     ok = torch.isfinite(g).all(dim=-1)
-    e = torch.full(top.shape, -119, dtype=torch.int32)
-    for power in range(-119, 125):          # the smallest E with top <= 6 2^E, at most 125
-        e += (top > 6.0 * 2.0 ** power).int()
+    # the smallest E with top <= 6 2^E: top / 6 = f 2^x with f in [.5, 1), in float64, where no
+    # quotient of a float32 rounds to a power of two that it is not
+    f, x = torch.frexp(top.nan_to_num(nan=1.0, posinf=1.0) / 6.0)
+    e = torch.where(f > 0.5, x, x - 1).clamp(-119, 125)
     s = torch.ldexp(torch.ones_like(top), e)[..., None]
     a = (g / s).abs()
     # distance to every grid value; the even code wins a tie (it is tried first)

@@ -188,6 +188,24 @@ def test_decode_step(dtype, d, group, n):
         same_cache(att, ref, n + 4, i + 1)
 
 
+@pytest.mark.parametrize("dtype,d,group", [("bf16", 128, 4), ("bf16", 64, 2), ("f32", 128, 1), ("f32", 64, 4)])
+@pytest.mark.parametrize("n,padded", [(127, False), (300, True), (1023, False)])
+def test_decode_step_of_many_units(dtype, d, group, n, padded):
+    """More units than every compute unit's three, which take one wave each up to 1023
+    entries: a step that appends and one that removes."""
+    b, hk, first = 771, 1, 2 * n
+    pads = torch.randint(0, first, (b,), generator=gen(n), dtype=torch.int32) if padded else None
+    att = make(b=b, s=first, kv_max=n + 1, block=1, heads=hk * group, kv_heads=hk, d=d, dtype=dtype)
+    ref = Reference(b=b, heads=hk * group, kv_heads=hk, d=d, pads=pads)
+    if padded:
+        att.set_left_padding(pads.cuda())
+    filled(att, ref, n, n + d, dtype, first)
+    g = gen(n)
+    for i in range(2):
+        decode(att, ref, first + i, *step_rows(g, b, hk * group, hk, d, dtype), dtype, n + 1)
+        same_cache(att, ref, n + 2, i + 1)
+
+
 @pytest.mark.parametrize("rule", ["sum", "recent", "tova"])
 @pytest.mark.parametrize("group", [1, 4])
 def test_decode_rules_and_removal_schedules(rule, group):
@@ -490,7 +508,7 @@ def test_a_sample_has_the_same_bits_in_any_batch(n):
     score = torch.rand((1, hk, n), generator=g).cuda()
     q1, k1, v1 = step_rows(g, 1, hk * group, hk, d, dtype)
     got = []
-    for b in (1, 3, 200):
+    for b in (1, 3, 400):               # 2 to 800 units: one wave per unit and four
         att = make(b=b, s=first, kv_max=n, block=1, heads=hk * group, kv_heads=hk, d=d)
         rep = lambda x: x.expand(b, *x.shape[1:]).contiguous()    # noqa: E731
         att.write_rows(0, rep(k), rep(v))
