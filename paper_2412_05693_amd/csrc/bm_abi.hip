@@ -492,6 +492,7 @@ int prefill_args(bm_ctx* ctx, int32_t t0, int32_t n_tok, const void* q, const vo
   a.npt_stride = ctx->lay.npt;
   a.units = ctx->units;
   a.accumulate = ctx->accumulate ? 1 : 0;
+  a.append = ctx->k_scale ? 0 : 1;
   a.pad = ctx->pad;
   a.lastw = ctx->rule == BM_RANK_TOVA ? reinterpret_cast<float*>(work_at(ctx, ctx->lay.lastw_off))
                                       : nullptr;

@@ -78,6 +78,7 @@ struct PrefillArgs {
   int n_heads, n_kv_heads, cap, len0, n_tok, t0, npt_used, npt_stride, units;
   int nsplit;         // workgroups per position tile (set by launch_prefill)
   int accumulate;     // 0: outputs only (no score sums; new entries get score 0)
+  int append;         // 0: the block's rows are stored elsewhere, kc and vc are only read
   const int32_t* pad; // [b] left pad tokens per sample, or null
   float* lastw;       // [U, cap] weights of the block's last query, or null
   float scale_log2;   // sm_scale * log2(e)

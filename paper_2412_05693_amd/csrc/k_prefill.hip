@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(kThreads, (BF16 || D == 64) ? 2 : 1) prefill_a
   //      so the workgroup waits for memory once before its first tile. ----
   const int64_t plane = ((int64_t)s.bi * a.n_kv_heads + s.hk) * a.seq_ld;
   constexpr int NA = (PT * C::CPR + kThreads - 1) / kThreads;   // chunks per thread
-  const int app_chunks = s.split == 0 ? (s.in_rows - s.pbase) * C::CPR : 0;
+  const int app_chunks = s.split == 0 && a.append ? (s.in_rows - s.pbase) * C::CPR : 0;
   u32x4 app_k[NA], app_v[NA];
   {
     const E* kin = static_cast<const E*>(a.kin);
