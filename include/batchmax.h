@@ -31,6 +31,9 @@
  * the caller's next synchronisation of the stream.  No C++ exception crosses
  * this boundary.
  *
+ * A cache can also be held in 4 bits: bm_kv4.h makes contexts over one, which
+ * every call below accepts.
+ *
  * Element types.  BM_F32: q, k, v, o and the K/V cache are float32.  BM_BF16:
  * they are bfloat16 with float32 accumulation.  Scores are always float32 and
  * positions int32.

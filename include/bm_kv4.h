@@ -23,6 +23,11 @@
  * attended to as given and stored in 4 bits; entries cached before the call
  * are attended to as they read back.  Scores, positions and lengths are those
  * of batchmax.h.
+ *
+ * A decode step gives hidden entries (left padding) and slots past the last
+ * no weight whatever they hold, NaN included.  A prefill block needs finite
+ * query, K and V rows at pad tokens, as bm_prefill_block does over a cache of
+ * the element type.
  */
 #ifndef BM_KV4_H
 #define BM_KV4_H

@@ -656,6 +656,12 @@ class PDAttentionKV4(PDAttention):
 
     _workspace_bytes = staticmethod(bm_kv4_workspace_bytes)
 
+    def _stream(self) -> int:
+        # the library launches on the current device: a stream of another one would not do
+        if self._dev_index is not None and self.torch.cuda.current_device() != self._dev_index:
+            raise ValueError(f"make {self.device} the current device")
+        return super()._stream()
+
     def _new_context(self) -> int:
         return bm_kv4_init(self.dims, self.cache, self._stream())
 

@@ -738,7 +738,8 @@ namespace {
 
 // A checked decode step over a 4-bit cache; outputs_only: more entries than a scoring
 // step takes, split over key chunks whose partial results go where a prefill block
-// reads the cached rows back (at most 520 bytes for each of 512 rows of 256 or more).
+// reads the cached rows back (for every 512 slots at most 4 heads' 520 bytes, where each
+// slot has 128 or more).
 int kv4_step(bm_ctx* ctx, int32_t pos, const void* q, const void* k, const void* v, void* o,
              int32_t seq_ld, bool outputs_only, hipStream_t stream) {
   bm::Kv4DecodeArgs a;

@@ -11,6 +11,13 @@
 //   3. outputs: 64 slots a wave, chunk c into stream c % kStreams, the streams' sums
 //      added in order; the step's own pair (as given, float32) joins at the end.
 // The next chunk's rows are on their way while one is computed.
+//
+// HBM-bound: 4.25 bits an element and 12 bytes an entry for its score and position.
+// 8192 units of 512 entries (d=128, G=4): 619 MB read and 30 written in 119 us, 5.4
+// TB/s (a copy: 5.2); the same with rows of scores alone left out takes 105.  The vector
+// pipes are busy 43% of the time (conversions and byte permutes half of that), the matrix
+// pipes 17%.  Few units are bound by the chain of a workgroup: 8 units 8.4 us, where
+// loads, two barriers and the launch itself are 7.4.
 #include <type_traits>
 
 #include "bm_internal.h"

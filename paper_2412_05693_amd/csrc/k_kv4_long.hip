@@ -4,6 +4,10 @@
 // waves attend to a split of the cached slots and leave one partial softmax per head;
 // kv4_combine_kernel, one workgroup per unit and head, joins them with the step's own
 // pair, writes the outputs and stores that pair in the slot behind the last.
+//
+// Bound by memory and, nearly as much, by the vector pipes (half of their work converts
+// and permutes rows): d=128, G=4, 64 units of 8192 entries take 15.9 + 3.7 us for 71 MB, 512
+// units 137 us for 587 MB (4.3 TB/s).
 #include <type_traits>
 
 #include "bm_internal.h"

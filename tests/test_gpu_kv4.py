@@ -499,6 +499,39 @@ def test_calls_run_on_the_current_stream():
     check(o, want, ref.out_tol(want, dtype, n + 1), "outputs")
 
 
+def test_another_current_device_is_refused(monkeypatch):
+    att = make()
+    x = torch.zeros(2, 2, 3, 128, dtype=torch.bfloat16, device="cuda")
+    q = torch.zeros(2, 4, 64, 128, dtype=torch.bfloat16, device="cuda")
+    k = torch.zeros(2, 2, 64, 128, dtype=torch.bfloat16, device="cuda")
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: att.device.index + 1)
+    for call in (lambda: att.write_rows(0, x, x), lambda: att.read_rows(0, 3, x, x.clone()),
+                 lambda: att.prefill_block(0, 16, q, k, k, q), lambda: att.evict_compact(-1),
+                 lambda: att.decode_step(64, q, k, k, q)):
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    assert att.length == 0 and att.next_pos == 0
+
+
+def test_whole_prompt_kept_then_a_long_step():
+    """Blocks without score sums, nothing removed, then steps over more entries than a
+    scoring one takes (the full-cache comparator on a 4-bit cache)."""
+    b, hk, group, d, s, block, steps, dtype = 1, 2, 2, 64, 4200, 1024, 2, "bf16"
+    att = make(b=b, s=s, kv_max=s + steps, block=block, max_gen=steps, heads=hk * group, kv_heads=hk, d=d)
+    att.set_score_accumulation(False)
+    ref = Reference(b=b, heads=hk * group, kv_heads=hk, d=d)
+    q, k, v = step_rows(gen(4), b, hk * group, hk, d, dtype, s + steps)
+    o = torch.empty_like(q)
+    att.run_prefill(q, k, v, o, fused_cut=True)
+    att.run_decode(q, k, v, o)
+    for t0 in (*range(0, s, block), *range(s, s + steps)):
+        r = min(block, s - t0) if t0 < s else 1
+        at = slice(t0, t0 + r)
+        want = ref.attend(t0, q[:, :, at], k[:, :, at], v[:, :, at], scores=False)
+        check(o[:, :, at], want, ref.out_tol(want, dtype, s, 2.0 ** -8), f"position {t0}")
+    same_cache(att, ref, s, 1, scores=False)
+
+
 @pytest.mark.parametrize("n", [100, 300, 1500])
 def test_a_sample_has_the_same_bits_in_any_batch(n):
     hk, group, d, dtype, first = 2, 4, 128, "bf16", 4000
