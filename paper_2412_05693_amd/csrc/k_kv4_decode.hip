@@ -14,10 +14,11 @@
 //
 // HBM-bound: 4.25 bits an element and 12 bytes an entry for its score and position.
 // 8192 units of 512 entries (d=128, G=4): 619 MB read and 30 written in 119 us, 5.4
-// TB/s (a copy: 5.2); the same with rows of scores alone left out takes 105.  The vector
-// pipes are busy 43% of the time (conversions and byte permutes half of that), the matrix
-// pipes 17%.  Few units are bound by the chain of a workgroup: 8 units 8.4 us, where
-// loads, two barriers and the launch itself are 7.4.
+// TB/s (a copy: 5.2).  The same loads without conversions and products take 111 us, 107
+// without the scores and positions too; an earlier layout whose rows came from the cache
+// took 91.  The vector pipes are busy 46% of the time, the matrix pipes 17%.  Few units are
+// bound by the chain of a workgroup: 8 units 8.7 us, and an earlier form with four waves
+// took 7.7 without conversions and products.
 #include <type_traits>
 
 #include "bm_internal.h"
