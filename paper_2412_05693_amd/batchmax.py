@@ -364,13 +364,16 @@ class PDAttention:
             self.work = (None if static_workspace else
                          torch.empty(self.work_bytes, dtype=torch.uint8, device=self.device))
         else:
-            # caller-provided views (for example slices of one arena); shapes checked
+            # caller-provided views (for example slices of one arena), checked
             for nm, x in zip((*want, "work"), buffers, strict=True):
                 setattr(self, nm, x)
-            for nm, (shp, _) in want.items():
+            for nm, (shp, dt) in want.items():
                 x = getattr(self, nm)
-                if tuple(x.shape) != shp or not x.is_contiguous() or x.device != self.device:
-                    raise ValueError(f"buffer {nm}: need a contiguous {shp} tensor on {self.device}")
+                if (tuple(x.shape) != shp or not x.is_contiguous() or x.device != self.device
+                        or x.element_size() != dt.itemsize):
+                    raise ValueError(f"buffer {nm}: need a contiguous {shp} tensor of {dt} on {self.device}")
+            if not self.work.is_contiguous() or self.work.device != self.device:
+                raise ValueError(f"buffer work: need a contiguous tensor on {self.device}")
             if self.work.numel() * self.work.element_size() < self.work_bytes:
                 raise ValueError("work buffer is smaller than bm_workspace_bytes")
         self.cache = self._cache()

@@ -144,6 +144,26 @@ def test_python_object_checks_its_tensors():
         att(buffers=[*parts[:-1], parts[-1][:100]])
 
 
+@pytest.mark.parametrize("cls", [bmx.PDAttentionKV4, bmx.PDAttention])
+def test_buffers_of_another_element_size_are_refused(cls):
+    a = cls(b=2, s=64, kv_max=32, block=8, max_gen=16, n_heads=4, n_kv_heads=2, head_dim=64, device="cpu",
+            init=False)
+    names = [*a._buffers(), "work"]
+    parts = [getattr(a, n) for n in names]
+    args = dict(b=2, s=64, kv_max=32, block=8, max_gen=16, n_heads=4, n_kv_heads=2, head_dim=64, device="cpu",
+                init=False)
+    cls(**args, buffers=parts)
+    small = {1: None, 2: torch.uint8, 4: torch.float16}
+    for i, x in enumerate(parts[:-1]):
+        if (dt := small[x.element_size()]) is not None:
+            with pytest.raises(ValueError, match=names[i]):
+                cls(**args, buffers=[*parts[:i], x.to(dt), *parts[i + 1:]])
+    wide = torch.empty(2 * parts[-1].numel(), dtype=torch.uint8)[::2]
+    for work in (wide, parts[-1].to("meta")):
+        with pytest.raises(ValueError, match="work"):
+            cls(**args, buffers=[*parts[:-1], work])
+
+
 def test_stack_bytes_at_four_bits():
     shape = dict(b=3, kv_max=512, block=256, n_kv_heads=8, head_dim=128, dtype="bf16")
     full, four = bmx.stack_layer_bytes(**shape), bmx.stack_layer_bytes(**shape, kv_bits=4)
