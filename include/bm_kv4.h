@@ -4,9 +4,9 @@
  * Every K and V row of the cache is stored as 4-bit floats (e2m1: 0, .5, 1,
  * 1.5, 2, 3, 4, 6 and their negatives) with one power-of-two scale for each
  * group of 32 consecutive elements (the OCP microscaling format MXFP4): 4.25
- * bits an element, so the memory of a bfloat16 cache holds 3.76 times the
- * entries.  Groups lie inside one row, so single entries are written, evicted
- * and moved without touching their neighbours.
+ * bits an element, so the memory of bfloat16 rows holds 3.76 times as many (scores
+ * and positions stay as they are).  Groups lie inside one row, so single entries
+ * are written, evicted and moved without touching their neighbours.
  *
  *   E   = the smallest integer with max|x_i| <= 6 * 2^E, within [-119, 125]
  *   x^  = 2^E * e2m1(x_i / 2^E), rounded to nearest, ties to the even code

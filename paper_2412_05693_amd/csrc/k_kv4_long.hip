@@ -5,9 +5,9 @@
 // kv4_combine_kernel, one workgroup per unit and head, joins them with the step's own
 // pair, writes the outputs and stores that pair in the slot behind the last.
 //
-// Bound by memory and, nearly as much, by the vector pipes (half of their work converts
-// and permutes rows): d=128, G=4, 64 units of 8192 entries take 15.9 + 3.7 us for 71 MB, 512
-// units 137 us for 587 MB (4.3 TB/s).
+// d=128, G=4: 64 units of 8192 entries take 16.4 + 5.0 us (shortest 15.7 + 3.5) for 71 MB, a
+// chain of loads and products per wave with the vector pipes busy 32% of the time and the
+// matrix pipes 10%; 512 units 137 us for 587 MB (4.3 TB/s), bound by memory.
 #include <type_traits>
 
 #include "bm_internal.h"

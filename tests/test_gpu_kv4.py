@@ -381,6 +381,32 @@ def test_prompt_and_generation(fused, rule, dtype, d, group, padded):
         same_cache(att, ref, 96, s + i + 1)
 
 
+@pytest.mark.parametrize("dtype,d,group,padded", [("bf16", 128, 4, False), ("bf16", 64, 2, True),
+                                                  ("f32", 64, 1, True)])
+def test_rows_left_in_the_workspace_change_nothing(dtype, d, group, padded):
+    """The space for rows read back holds NaN, or zeros, before every call: the same bits."""
+    b, hk, s, kv_max, block = 2, 2, 203, 57, 39
+    q, k, v = step_rows(gen(7), b, hk * group, hk, d, dtype, s + 2)
+    got = []
+    for fill in (0, 255):
+        att = make(b=b, s=s, kv_max=kv_max, block=block, max_gen=2, heads=hk * group, kv_heads=hk, d=d,
+                   dtype=dtype)
+        junk(att)
+        if padded:
+            att.set_left_padding(torch.tensor([0, 75], dtype=torch.int32).cuda())
+        rows_at = -(-bmx.bm_workspace_bytes(att.dims) // 256) * 256
+        o = torch.zeros_like(q)
+        for t0 in range(0, s, block):
+            att.work[rows_at:].fill_(fill)
+            att.prefill_block_cut(t0, min(block, s - t0), q, k, v, o)
+        for i in range(2):
+            att.work[rows_at:].fill_(fill)
+            att.decode_step(s + i, q, k, v, o, row=s + i)
+        got.append((o, *live(att)))
+    assert all(torch.equal(x, y) for x, y in zip(*got, strict=True))
+    assert torch.isfinite(got[0][0]).all()
+
+
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("n,keep", [(700, 400), (1000, 999), (2500, 1500), (4600, 4000)])
 def test_cut_moves_codes_and_scales(d, n, keep):
