@@ -370,7 +370,7 @@ class PDAttention:
             for nm, (shp, dt) in want.items():
                 x = getattr(self, nm)
                 if (tuple(x.shape) != shp or not x.is_contiguous() or x.device != self.device
-                        or x.element_size() != dt.itemsize):
+                        or not self._takes(x.dtype, dt)):
                     raise ValueError(f"buffer {nm}: need a contiguous {shp} tensor of {dt} on {self.device}")
             if not self.work.is_contiguous() or self.work.device != self.device:
                 raise ValueError(f"buffer work: need a contiguous tensor on {self.device}")
@@ -406,6 +406,11 @@ class PDAttention:
     def _cache(self):
         return bm_cache(self.k.data_ptr(), self.v.data_ptr(), self.score.data_ptr(),
                         self.pos.data_ptr(), self.len.data_ptr(), *self._work_ptr())
+
+    @staticmethod
+    def _takes(given, want) -> bool:
+        """Whether a caller's tensor of type ``given`` can stand for one of type ``want``."""
+        return given.itemsize == want.itemsize
 
     _workspace_bytes = staticmethod(bm_workspace_bytes)
 
@@ -635,7 +640,7 @@ class PDAttentionKV4(PDAttention):
 
     ``k``, ``v`` hold the codes, uint8 ``[b, n_kv_heads, slots, d / 2]``, ``k_scale``, ``v_scale``
     the scale bytes, uint8 ``[b, n_kv_heads, slots, d / 32]``, in the library's own order of
-    bytes within a unit.  ``buffers``: those four, then score, pos, len and work.
+    bytes within a unit.  ``buffers``: those four, then score (float32), pos, len (int32) and work.
     ``write_rows`` and ``read_rows`` convert rows of the configured dtype to and from slots.
     """
 
@@ -656,6 +661,11 @@ class PDAttentionKV4(PDAttention):
         return bm_kv4_cache(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(),
                             self.v_scale.data_ptr(), self.score.data_ptr(), self.pos.data_ptr(),
                             self.len.data_ptr(), *self._work_ptr())
+
+    @staticmethod
+    def _takes(given, want) -> bool:
+        # codes, scores and positions of another type would be read as other values
+        return given == want
 
     _workspace_bytes = staticmethod(bm_kv4_workspace_bytes)
 
