@@ -17,6 +17,7 @@ from __future__ import annotations
 import ctypes
 import math
 import os
+import warnings
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 # BATCHMAX_LIB selects another build of the same library (the host-sanitizer
@@ -335,7 +336,12 @@ class PDAttention:
                  dtype="bf16", sm_scale=0.0, device="cuda", init=True, buffers=None,
                  static_workspace=False):
         """``static_workspace``: no workspace tensor; contexts come from
-        bm_init_static_workspace and use the library's static device array."""
+        bm_init_static_workspace and use the library's static device array.
+
+        ``buffers``: the caller's own k, v, score (float32), pos, len (int32) and work,
+        contiguous on the device.  A tensor of another type whose elements are at least as
+        large is raw storage (a warning says so): the object's attribute is then a view
+        of its first bytes in the type that the library reads."""
         import torch
 
         self.torch = torch
@@ -372,6 +378,10 @@ class PDAttention:
                 if (tuple(x.shape) != shp or not x.is_contiguous() or x.device != self.device
                         or not self._takes(x.dtype, dt)):
                     raise ValueError(f"buffer {nm}: need a contiguous {shp} tensor of {dt} on {self.device}")
+                if x.dtype != dt:
+                    warnings.warn(f"buffer {nm}: {x.dtype} taken as raw storage of {dt}", stacklevel=2)
+                    raw = x.detach().view(-1).view(torch.uint8)
+                    setattr(self, nm, raw[:x.numel() * dt.itemsize].view(dt).view(shp))
             if not self.work.is_contiguous() or self.work.device != self.device:
                 raise ValueError(f"buffer work: need a contiguous tensor on {self.device}")
             if self.work.numel() * self.work.element_size() < self.work_bytes:
@@ -410,7 +420,7 @@ class PDAttention:
     @staticmethod
     def _takes(given, want) -> bool:
         """Whether a caller's tensor of type ``given`` can stand for one of type ``want``."""
-        return given.itemsize == want.itemsize
+        return given.itemsize >= want.itemsize
 
     _workspace_bytes = staticmethod(bm_workspace_bytes)
 
