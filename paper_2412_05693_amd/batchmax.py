@@ -485,21 +485,20 @@ class PDAttention:
             self._SETTERS[key](self.ctx, val)   # raises before anything is stored
         self._settings[key] = val
 
-    def reset(self) -> None:
-        if self.ctx is not None:
-            bm_destroy(self.ctx)
-            self.ctx = None
-        self.ctx = self._new_context()
+    def _replace_context(self, new) -> None:
+        # (the new one was made first: a refusal leaves the old one in place)
+        old, self.ctx = self.ctx, new
+        if old is not None:
+            bm_destroy(old)
         self._apply_settings()
+
+    def reset(self) -> None:
+        self._replace_context(self._new_context())
 
     def resume(self, length: int, next_pos: int) -> None:
         if self.static_workspace:
             raise ValueError("resume needs a caller-allocated workspace")
-        if self.ctx is not None:
-            bm_destroy(self.ctx)
-            self.ctx = None
-        self.ctx = self._resumed_context(length, next_pos)
-        self._apply_settings()
+        self._replace_context(self._resumed_context(length, next_pos))
 
     def _block_args(self, t0, n_tok, q, k, v, o, row):
         row = t0 if row is None else row
