@@ -249,7 +249,15 @@ def bm_kv4_init(dims: bm_dims, cache: bm_kv4_cache, stream: int) -> int:
     return out.value
 
 
+def _int32(*values: int) -> None:
+    """ctypes passes an integer modulo 2^32: refuse one that the library would not see."""
+    for x in values:
+        if not -(1 << 31) <= x < 1 << 31:
+            raise ValueError(f"{x} does not fit in 32 bits")
+
+
 def bm_kv4_resume(dims: bm_dims, cache: bm_kv4_cache, length: int, next_pos: int) -> int:
+    _int32(length, next_pos)
     out = ctypes.c_void_p()
     _check(_lib.bm_kv4_resume(ctypes.byref(dims), ctypes.byref(cache), length, next_pos,
                               ctypes.byref(out)))
@@ -258,11 +266,13 @@ def bm_kv4_resume(dims: bm_dims, cache: bm_kv4_cache, length: int, next_pos: int
 
 def bm_kv4_write(dims: bm_dims, cache: bm_kv4_cache, slot0: int, n: int, k: int, v: int,
                  seq_ld: int, stream: int) -> None:
+    _int32(slot0, n, seq_ld)
     _check(_lib.bm_kv4_write(ctypes.byref(dims), ctypes.byref(cache), slot0, n, k, v, seq_ld, stream))
 
 
 def bm_kv4_read(dims: bm_dims, cache: bm_kv4_cache, slot0: int, n: int, k: int, v: int,
                 seq_ld: int, stream: int) -> None:
+    _int32(slot0, n, seq_ld)
     _check(_lib.bm_kv4_read(ctypes.byref(dims), ctypes.byref(cache), slot0, n, k, v, seq_ld, stream))
 
 
