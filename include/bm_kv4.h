@@ -95,7 +95,8 @@ int bm_kv4_write(const bm_dims* dims, const bm_kv4_cache* cache, int32_t slot0, 
                  const void* k, const void* v, int32_t seq_ld, hipStream_t stream);
 
 /* The inverse: slots slot0 .. slot0 + n - 1 of every unit into rows 0 .. n - 1
- * of k and v.  Rows from n on are left as they are.  k and v must not overlap. */
+ * of k and v.  Rows from n on are left as they are.  BM_ERR_INVALID_ARG if a row of k
+ * and one of v overlap. */
 int bm_kv4_read(const bm_dims* dims, const bm_kv4_cache* cache, int32_t slot0, int32_t n, void* k,
                 void* v, int32_t seq_ld, hipStream_t stream);
 

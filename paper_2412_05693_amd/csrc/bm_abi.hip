@@ -343,6 +343,13 @@ int kv4_ctx(const bm_dims* dims, const bm_kv4_cache* cache, bm_ctx** out) {
   return BM_OK;
 }
 
+// Whether runs of `run` bytes, one every `stride` of `planes` planes, from k and from v on meet.
+bool runs_overlap(const void* k, const void* v, int64_t planes, uint64_t stride, uint64_t run) {
+  const uint64_t x = (uintptr_t)k, y = (uintptr_t)v, apart = x < y ? y - x : x - y;
+  const uint64_t p = apart / stride, rest = apart % stride;
+  return (p < (uint64_t)planes && rest < run) || (p + 1 < (uint64_t)planes && stride - rest < run);
+}
+
 // Rows between buffers of the element type and slots of a 4-bit cache.
 int kv4_rows(const bm_dims* dims, const bm_kv4_cache* cache, int32_t slot0, int32_t n,
              const void* k, const void* v, int32_t seq_ld, bool write, hipStream_t stream) {
@@ -364,6 +371,9 @@ int kv4_rows(const bm_dims* dims, const bm_kv4_cache* cache, int32_t slot0, int3
   if (((uintptr_t)k | (uintptr_t)v) & 15)
     return fail(BM_ERR_INVALID_ARG, "k and v must be 16-byte aligned");
   if (seq_ld < n) return fail(BM_ERR_INVALID_ARG, "seq_ld %d < n %d", seq_ld, n);
+  const uint64_t row = (uint64_t)dims->head_dim * (dims->dtype == BM_BF16 ? 2 : 4);
+  if (!write && runs_overlap(k, v, (int64_t)dims->b * dims->n_kv_heads, seq_ld * row, n * row))
+    return fail(BM_ERR_INVALID_ARG, "the rows of k and v overlap");
   bm::Kv4RowsArgs a;
   a.k = k;
   a.v = v;
