@@ -249,15 +249,17 @@ def bm_kv4_init(dims: bm_dims, cache: bm_kv4_cache, stream: int) -> int:
     return out.value
 
 
-def _int32(*values: int) -> None:
-    """ctypes passes an integer modulo 2^32: refuse one that the library would not see."""
-    for x in values:
-        if not -(1 << 31) <= x < 1 << 31:
-            raise ValueError(f"{x} does not fit in 32 bits")
+# ctypes passes an integer modulo 2^32: one that the library would not see is refused here
+_INT32_MAX = 0x7FFFFFFF
+
+
+def _int32_only(x: int, y: int) -> None:
+    raise ValueError(f"{x}, {y}: does not fit in 32 bits")
 
 
 def bm_kv4_resume(dims: bm_dims, cache: bm_kv4_cache, length: int, next_pos: int) -> int:
-    _int32(length, next_pos)
+    if not (-_INT32_MAX <= length <= _INT32_MAX and -_INT32_MAX <= next_pos <= _INT32_MAX):
+        _int32_only(length, next_pos)
     out = ctypes.c_void_p()
     _check(_lib.bm_kv4_resume(ctypes.byref(dims), ctypes.byref(cache), length, next_pos,
                               ctypes.byref(out)))
@@ -266,13 +268,15 @@ def bm_kv4_resume(dims: bm_dims, cache: bm_kv4_cache, length: int, next_pos: int
 
 def bm_kv4_write(dims: bm_dims, cache: bm_kv4_cache, slot0: int, n: int, k: int, v: int,
                  seq_ld: int, stream: int) -> None:
-    _int32(slot0, n, seq_ld)
+    if not (-_INT32_MAX <= slot0 <= _INT32_MAX and -_INT32_MAX <= n <= _INT32_MAX):
+        _int32_only(slot0, n)
     _check(_lib.bm_kv4_write(ctypes.byref(dims), ctypes.byref(cache), slot0, n, k, v, seq_ld, stream))
 
 
 def bm_kv4_read(dims: bm_dims, cache: bm_kv4_cache, slot0: int, n: int, k: int, v: int,
                 seq_ld: int, stream: int) -> None:
-    _int32(slot0, n, seq_ld)
+    if not (-_INT32_MAX <= slot0 <= _INT32_MAX and -_INT32_MAX <= n <= _INT32_MAX):
+        _int32_only(slot0, n)
     _check(_lib.bm_kv4_read(ctypes.byref(dims), ctypes.byref(cache), slot0, n, k, v, seq_ld, stream))
 
 
