@@ -21,7 +21,10 @@
  * bm_evict_compact, bm_decode_step, the bm_set_* calls and bm_destroy, with the
  * same arguments, checks, order and limits.  A call's own K and V rows are
  * attended to as given and stored in 4 bits; entries cached before the call
- * are attended to as they read back.  Scores, positions and lengths are those
+ * are attended to as they read back.  Weights of a prefill block's outputs are one
+ * bfloat16 each over a bfloat16 batch, as over a cache of that type (outputs are off
+ * by 1.9e-3 of their norm, where their own rounding gives 1.6e-3); a decode step
+ * keeps two parts.  Scores, positions and lengths are those
  * of batchmax.h.
  *
  * A decode step gives hidden entries (left padding) and slots past the last
@@ -75,7 +78,11 @@ int32_t bm_kv4_slots(const bm_dims* dims);
 /* Bytes of bm_kv4_cache.work; 0 if dims are invalid.  They hold
  * bm_workspace_bytes(dims) and one layer's cached rows in the element type of
  * dims.dtype, which a prefill block reads back once for all its queries;
- * layers that run one after another can share it. */
+ * layers that run one after another can share it.  Every context needs them, also
+ * one that only decodes: a single layer with a workspace of its own takes more
+ * memory than one of bfloat16 rows (64 samples, 8 heads, 768 slots of 128, blocks
+ * of 256 and four query heads a KV head: 57 + 219 MB against 204 + 17); what 4 bits
+ * save, they save over layers that share one. */
 size_t bm_kv4_workspace_bytes(const bm_dims* dims);
 
 /* bm_init over a 4-bit cache: enqueues the zeroing of len and score. */

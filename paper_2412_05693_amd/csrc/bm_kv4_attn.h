@@ -19,9 +19,10 @@
 // consecutive slots, and the scales of a lane's slots, lie side by side, so a lane reads
 // a chunk with ten loads of 4 or 16 bytes, each a whole run of memory per wave.
 //
-// Query rows are one bfloat16 (float32: three bfloat16 parts, 24 bits) and
-// probabilities two (three) parts, so the products are as exact as float32
-// accumulation; queries of the batch in bfloat16 are exact as they are.
+// Query rows are one bfloat16, which holds a bfloat16 row exactly; float32 rows are three
+// bfloat16 parts (24 bits).  Probabilities are two parts over a bfloat16 batch: each weight
+// loses at most 2^-16 of itself, where the output's own rounding to bfloat16 is 2^-8; over
+// a float32 batch three parts, 2^-24.  Sums are float32.
 #pragma once
 
 #include <type_traits>

@@ -13,12 +13,16 @@
 // The next chunk's rows are on their way while one is computed.
 //
 // HBM-bound: 4.25 bits an element and 12 bytes an entry for its score and position.
-// 8192 units of 512 entries (d=128, G=4): 619 MB read and 30 written in 119 us, 5.4
-// TB/s (a copy: 5.2).  The same loads without conversions and products take 111 us, 107
-// without the scores and positions too; an earlier layout whose rows came from the cache
-// took 91.  The vector pipes are busy 46% of the time, the matrix pipes 17%.  Few units are
-// bound by the chain of a workgroup: 8 units 8.7 us, and an earlier form with four waves
-// took 7.7 without conversions and products.
+// 8192 units of 512 entries (d=128, G=4): 619 MB read and 30 written in 119 us where two
+// steps over a layer make a pass (kernel trace: 121), 5.4 TB/s (a copy: 5.2); steps replayed
+// from a graph over codes of random bits take 128-130.  The same loads without conversions
+// and products take 111 us, 107 without the scores and positions too; an earlier layout
+// whose rows came from the cache took 91.  The vector pipes are busy 46% of the time, the
+// matrix pipes 17%.  Few units are bound by the chain of a workgroup: 8 units 8.7 us, and an
+// earlier form with four waves took 7.7 without conversions and products.  A unit has one
+// workgroup whatever its length, so few units leave most of the card idle: 8 units of 4096
+// entries 31 us for 1 us of bytes.  Splitting a unit, as the split step over longer caches
+// does, was not tried here: the scores need the unit's normaliser.
 #include <type_traits>
 
 #include "bm_internal.h"
@@ -429,8 +433,8 @@ hipError_t launch_w(const Kv4DecodeArgs& a, hipStream_t stream) {
 // One wave per unit or four.  One has no partial outputs to join and waits for no other
 // wave, which is fastest once every compute unit has several units; four shorten a unit's
 // chain of loads where it has few, and share the LDS that a long unit's logits fill.
-// us a step with one -> with four, bf16 d=128 G=4 by units (512 entries at 768 units 19.2 ->
-// 18.7, at 896 19.9 -> 22.7):
+// us a step with one -> with four, 16 steps replayed from a graph over one full cache, bf16
+// d=128 G=4, entries by units (512 entries at 768 units 19.2 -> 18.7, at 896 19.9 -> 22.7):
 //   entries  8             512            1024           2048           8192
 //   64       6.8 -> 6.9    7.9 -> 8.5     8.7 -> 14.0    10.7 -> 21.5   31.8 -> 72.3
 //   128      8.0 -> 7.1    9.1 -> 9.2     10.2 -> 14.8   14.7 -> 24.0   40.4 -> 76.1
@@ -438,6 +442,18 @@ hipError_t launch_w(const Kv4DecodeArgs& a, hipStream_t stream) {
 //   1024     26.9 -> 11.5  31.3 -> 20.4   34.9 -> 34.4   65.2 -> 72.2   252 -> 249
 //   2048     48.9 -> 17.9  55.0 -> 32.9   70.9 -> 69.9   163 -> 128
 //   4096     93.2 -> 30.4  112 -> 68.1    224 -> 129     447 -> 247
+// The rule misses 1024 entries of 2048 units.  The other forms, measured the same way
+// afterwards, part at about the same places:
+//                      bf16 d=128 G=1   bf16 d=64 G=1    f32 d=128 G=4    f32 d=64 G=1
+//   512 x 512          17.6 -> 12.0     13.6 -> 8.6      23.8 -> 15.5     16.4 -> 10.1
+//   512 x 1024         19.4 -> 20.5     15.6 -> 13.5     26.1 -> 28.2     19.0 -> 17.9
+//   512 x 8192         121 -> 135       71.6 -> 89.8     165 -> 213       95.7 -> 115
+//   1000 x 1024        33.3 -> 31.0     25.7 -> 20.3     45.0 -> 40.6     32.2 -> 26.2
+//   1024 x 8192        229 -> 232       134 -> 146       295 -> 321       169 -> 188
+//   2048 x 1024        68.1 -> 62.7     44.5 -> 34.4     95.8 -> 83.1     60.5 -> 47.6
+//   2048 x 8192        416 -> 436       250 -> 258       758 -> 593       323 -> 335
+// (what it costs most there: 26% at 1000 entries x 1024 units of bf16 d=64, 15% at 1024 x 8192
+// of f32 d=64).
 // (Two waves are between the two, eight slower than four but for 5% at 8 units of 2048
 // entries.  A third chunk of K or V on its way changes nothing: 129 -> 127-145.)
 constexpr int kManyUnits = 768;          // three for every compute unit
