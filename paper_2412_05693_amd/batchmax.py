@@ -69,6 +69,7 @@ class bm_kv4_cache(ctypes.Structure):
 
 
 BM_KV4_GROUP = 32       # elements that share one scale of a 4-bit row
+_INT32_MAX = 0x7FFFFFFF # ctypes passes an integer modulo 2^32: the library would not see one beyond
 
 
 def _load() -> ctypes.CDLL:
@@ -249,17 +250,7 @@ def bm_kv4_init(dims: bm_dims, cache: bm_kv4_cache, stream: int) -> int:
     return out.value
 
 
-# ctypes passes an integer modulo 2^32: one that the library would not see is refused here
-_INT32_MAX = 0x7FFFFFFF
-
-
-def _int32_only(x: int, y: int) -> None:
-    raise ValueError(f"{x}, {y}: does not fit in 32 bits")
-
-
 def bm_kv4_resume(dims: bm_dims, cache: bm_kv4_cache, length: int, next_pos: int) -> int:
-    if not (-_INT32_MAX <= length <= _INT32_MAX and -_INT32_MAX <= next_pos <= _INT32_MAX):
-        _int32_only(length, next_pos)
     out = ctypes.c_void_p()
     _check(_lib.bm_kv4_resume(ctypes.byref(dims), ctypes.byref(cache), length, next_pos,
                               ctypes.byref(out)))
@@ -268,15 +259,11 @@ def bm_kv4_resume(dims: bm_dims, cache: bm_kv4_cache, length: int, next_pos: int
 
 def bm_kv4_write(dims: bm_dims, cache: bm_kv4_cache, slot0: int, n: int, k: int, v: int,
                  seq_ld: int, stream: int) -> None:
-    if not (-_INT32_MAX <= slot0 <= _INT32_MAX and -_INT32_MAX <= n <= _INT32_MAX):
-        _int32_only(slot0, n)
     _check(_lib.bm_kv4_write(ctypes.byref(dims), ctypes.byref(cache), slot0, n, k, v, seq_ld, stream))
 
 
 def bm_kv4_read(dims: bm_dims, cache: bm_kv4_cache, slot0: int, n: int, k: int, v: int,
                 seq_ld: int, stream: int) -> None:
-    if not (-_INT32_MAX <= slot0 <= _INT32_MAX and -_INT32_MAX <= n <= _INT32_MAX):
-        _int32_only(slot0, n)
     _check(_lib.bm_kv4_read(ctypes.byref(dims), ctypes.byref(cache), slot0, n, k, v, seq_ld, stream))
 
 
@@ -702,6 +689,8 @@ class PDAttentionKV4(PDAttention):
         return bm_kv4_init(self.dims, self.cache, self._stream())
 
     def _resumed_context(self, length, next_pos) -> int:
+        if not (-_INT32_MAX <= length <= _INT32_MAX and -_INT32_MAX <= next_pos <= _INT32_MAX):
+            raise ValueError(f"length {length}, next_pos {next_pos}: beyond 32 bits")
         return bm_kv4_resume(self.dims, self.cache, length, next_pos)
 
     def _rows(self, k, v):
@@ -722,6 +711,8 @@ class PDAttentionKV4(PDAttention):
         """Store every row of k, v ``[b, n_kv_heads, n, d]`` in slots slot0 .. slot0 + n - 1 of
         its unit; scores, positions and lengths are left as they are."""
         n = self._rows(k, v)
+        if not -_INT32_MAX <= slot0 <= _INT32_MAX:
+            raise ValueError(f"slot0 {slot0}: beyond 32 bits")
         bm_kv4_write(self.dims, self.cache, slot0, n, k.data_ptr(), v.data_ptr(), n, self._stream())
 
     def read_rows(self, slot0, n, k=None, v=None):
@@ -734,6 +725,8 @@ class PDAttentionKV4(PDAttention):
             v = t.empty_like(k)
         if self._rows(k, v) != n:
             raise ValueError(f"k and v need {n} rows")
+        if not -_INT32_MAX <= slot0 <= _INT32_MAX:
+            raise ValueError(f"slot0 {slot0}: beyond 32 bits")
         bm_kv4_read(self.dims, self.cache, slot0, n, k.data_ptr(), v.data_ptr(), n, self._stream())
         return k, v
 
