@@ -68,6 +68,12 @@ class bm_kv4_cache(ctypes.Structure):
                 ("work_bytes", ctypes.c_size_t)]
 
 
+class bm_win_cache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("work", ctypes.c_void_p),
+                ("work_bytes", ctypes.c_size_t)]
+
+
+BM_DRAFT_MAX = 64       # nodes of a tree of drafted tokens
 BM_KV4_GROUP = 32       # elements that share one scale of a 4-bit row
 _INT32_MAX = 0x7FFFFFFF # ctypes passes an integer modulo 2^32: the library would not see one beyond
 
@@ -85,6 +91,7 @@ def _load() -> ctypes.CDLL:
     P, I32, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
     dims_p, cache_p = ctypes.POINTER(bm_dims), ctypes.POINTER(bm_cache)
     kv4_p = ctypes.POINTER(bm_kv4_cache)
+    win_p = ctypes.POINTER(bm_win_cache)
     sig = {
         "bm_abi_version": (ctypes.c_int, []),
         "bm_last_error": (ctypes.c_char_p, []),
@@ -111,6 +118,13 @@ def _load() -> ctypes.CDLL:
         "bm_kv4_resume": (ctypes.c_int, [dims_p, kv4_p, I32, I32, ctypes.POINTER(P)]),
         "bm_kv4_write": (ctypes.c_int, [dims_p, kv4_p, I32, I32, P, P, I32, P]),
         "bm_kv4_read": (ctypes.c_int, [dims_p, kv4_p, I32, I32, P, P, I32, P]),
+        "bm_win_workspace_bytes": (SZ, [dims_p]),
+        "bm_win_validate": (ctypes.c_int, [dims_p, I32]),
+        "bm_win_init": (ctypes.c_int, [dims_p, I32, win_p, ctypes.POINTER(P)]),
+        "bm_win_resume": (ctypes.c_int, [dims_p, I32, win_p, I32, ctypes.POINTER(P)]),
+        "bm_draft_workspace_bytes": (SZ, [dims_p, I32]),
+        "bm_draft_attend": (ctypes.c_int, [P, I32, P, P, P, P, P, I32, P, P, SZ, P]),
+        "bm_draft_accept": (ctypes.c_int, [P, I32, I32, P, P, P, P, P, I32, P, P]),
         "bm_ctx_len": (I32, [P]),
         "bm_ctx_next_pos": (I32, [P]),
         "bm_destroy": (None, [P]),
@@ -137,6 +151,8 @@ EXPORTED = ("bm_abi_version", "bm_last_error", "bm_cache_slots", "bm_workspace_b
             "bm_set_score_accumulation", "bm_set_left_padding", "bm_set_split_event",
             "bm_decode_step", "bm_ctx_len", "bm_ctx_next_pos", "bm_destroy", "bm_synth_qkv",
             "bm_kv4_slots", "bm_kv4_workspace_bytes", "bm_kv4_init", "bm_kv4_resume", "bm_kv4_write", "bm_kv4_read",
+            "bm_win_workspace_bytes", "bm_win_validate", "bm_win_init", "bm_win_resume",
+            "bm_draft_workspace_bytes", "bm_draft_attend", "bm_draft_accept",
             "bm_philox4x32_10", "bm_probe_stream_read", "bm_probe_mfma",
             "bm_prefill_timeline", "bm_prefill_tile_workgroups")
 
@@ -267,6 +283,41 @@ def bm_kv4_read(dims: bm_dims, cache: bm_kv4_cache, slot0: int, n: int, k: int, 
     _check(_lib.bm_kv4_read(ctypes.byref(dims), ctypes.byref(cache), slot0, n, k, v, seq_ld, stream))
 
 
+def bm_win_workspace_bytes(dims: bm_dims) -> int:
+    return _lib.bm_win_workspace_bytes(ctypes.byref(dims))
+
+
+def bm_win_validate(dims: bm_dims, sinks: int) -> None:
+    _check(_lib.bm_win_validate(ctypes.byref(dims), sinks))
+
+
+def bm_win_init(dims: bm_dims, sinks: int, cache: bm_win_cache) -> int:
+    out = ctypes.c_void_p()
+    _check(_lib.bm_win_init(ctypes.byref(dims), sinks, ctypes.byref(cache), ctypes.byref(out)))
+    return out.value
+
+
+def bm_win_resume(dims: bm_dims, sinks: int, cache: bm_win_cache, next_pos: int) -> int:
+    out = ctypes.c_void_p()
+    _check(_lib.bm_win_resume(ctypes.byref(dims), sinks, ctypes.byref(cache), next_pos,
+                              ctypes.byref(out)))
+    return out.value
+
+
+def bm_draft_workspace_bytes(dims: bm_dims, n: int) -> int:
+    return _lib.bm_draft_workspace_bytes(ctypes.byref(dims), n)
+
+
+def bm_draft_attend(ctx: int, n: int, parent: int, q: int, k: int, v: int, o: int, seq_ld: int,
+                    lse: int, work: int, work_bytes: int, stream: int) -> None:
+    _check(_lib.bm_draft_attend(ctx, n, parent, q, k, v, o, seq_ld, lse, work, work_bytes, stream))
+
+
+def bm_draft_accept(ctx: int, n: int, m: int, path: int, count: int, q: int, k: int, v: int,
+                    seq_ld: int, lse: int, stream: int) -> None:
+    _check(_lib.bm_draft_accept(ctx, n, m, path, count, q, k, v, seq_ld, lse, stream))
+
+
 def bm_ctx_len(ctx: int) -> int:
     return _lib.bm_ctx_len(ctx)
 
@@ -349,13 +400,12 @@ class PDAttention:
         self.dims = make_dims(b=b, s=s, kv_max=kv_max, block=block, max_gen=max_gen,
                               n_heads=n_heads, n_kv_heads=n_kv_heads, head_dim=head_dim,
                               dtype=dtype, sm_scale=sm_scale)
-        bm_validate_dims(self.dims)
+        self.cap = self._validate()
         self.tdtype = torch.float32 if self.dims.dtype == BM_F32 else torch.bfloat16
         dev = torch.device(device)
         if dev.type == "cuda" and dev.index is None:
             dev = torch.device("cuda", torch.cuda.current_device())
         self.device = dev
-        self.cap = bm_cache_slots(self.dims)
         self.group = n_heads // n_kv_heads
         U = b * n_kv_heads
         self.work_bytes = self._workspace_bytes(self.dims)
@@ -396,6 +446,7 @@ class PDAttention:
         self._bhd = (b, n_heads, n_kv_heads, head_dim)
         self._row_bytes = head_dim * (4 if self.dims.dtype == BM_F32 else 2)
         self.ctx = None
+        self._draft_works = []
         # schedule settings (bm_set_*): kept here and applied again to every new
         # context, so they survive reset() and resume()
         self._settings = {}
@@ -403,6 +454,11 @@ class PDAttention:
             self.reset()
 
     # -- the cache ----------------------------------------------------------------
+    def _validate(self) -> int:
+        """Check the dimensions; returns the slots a unit has."""
+        bm_validate_dims(self.dims)
+        return bm_cache_slots(self.dims)
+
     def _buffers(self) -> dict:
         """Shape and element type of every tensor of the cache, in the order of ``buffers``."""
         t, d = self.torch, self.dims
@@ -584,6 +640,73 @@ class PDAttention:
         bm_decode_step(self.ctx, pos, self._row_ptr(q, row), self._row_ptr(k, row),
                        self._row_ptr(v, row), self._row_ptr(o, row), T, self._stream())
 
+    # -- drafted tokens (include/bm_draft.h) -----------------------------------------
+    def _ints(self, x, shape, name):
+        t = self.torch
+        if x.dtype != t.int32 or x.device != self.device or not x.is_contiguous() or \
+                tuple(x.shape) != shape:
+            raise ValueError(f"{name}: need a contiguous int32 {list(shape)} tensor on {self.device}")
+        return x.data_ptr()
+
+    def _lse_ptr(self, lse, n):
+        if lse is None:
+            return None
+        t, shape = self.torch, (self.dims.b, self.dims.n_heads, n)
+        if lse.dtype != t.float32 or lse.device != self.device or not lse.is_contiguous() or \
+                tuple(lse.shape) != shape:
+            raise ValueError(f"lse: need a contiguous float32 {list(shape)} tensor on {self.device}")
+        return lse.data_ptr()
+
+    def _tree_rows(self, n, q, k, v, o, row):
+        """Pointers of rows row .. row + n - 1 of q, k, v (and o)."""
+        if not (self._args_ok(q, k, v, o) and 0 <= row and row + n <= q.shape[2]):
+            H, Hk = self.dims.n_heads, self.dims.n_kv_heads
+            for x, hh, nm in ((q, H, "q"), (k, Hk, "k"), (v, Hk, "v"), (o, H, "o")):
+                self._check_tensor(x, hh, nm)
+                if x.shape[2] != q.shape[2]:
+                    raise ValueError("q, k, v and o need the same number of rows")
+            raise ValueError(f"rows [{row}, {row + n}) exceed {q.shape[2]}")
+        if self.torch.cuda.current_device() != self._dev_index:
+            # the library launches on the current device: a stream of another one would not do
+            raise ValueError(f"make {self.device} the current device")
+        return self._row_ptrs(q, k, v, o, row)
+
+    def draft_attend(self, parent, q, k, v, o, lse=None, row=0) -> None:
+        """The attention of a tree's n nodes over the cache, their ancestors and themselves:
+        rows row .. row + n - 1 of q, k, v into o.  ``parent`` int32 ``[b, n]`` (-1: a root);
+        ``lse`` float32 ``[b, n_heads, n]`` or None takes their log-sum-exps.  The cache
+        is left as it is (one above the decode bound is cut to it)."""
+        n = parent.shape[-1]
+        tree = self._ints(parent, (self.dims.b, n), "parent")
+        rows = self._tree_rows(n, q, k, v, o, row)
+        need = bm_draft_workspace_bytes(self.dims, n)
+        if self._draft_work is None or self._draft_work.numel() < need:
+            # (kept for later calls; of another size for a larger tree.  The old one stays
+            # with graphs that were captured over it)
+            self._draft_works.append(self.torch.empty(max(need, 16), dtype=self.torch.uint8, device=self.device))
+        work = self._draft_work
+        bm_draft_attend(self.ctx, n, tree, *rows, q.shape[2], self._lse_ptr(lse, n), work.data_ptr(),
+                        work.numel(), self._stream())
+
+    @property
+    def _draft_work(self):
+        return self._draft_works[-1] if self._draft_works else None
+
+    def draft_accept(self, path, q, k, v, lse=None, count=None, row=0, n=None) -> None:
+        """Append the m tokens ``path`` (int32 ``[b, m]``: node numbers, a root and then each
+        one's child) of the tree of n nodes (by default all rows from ``row`` on; ``lse``, if
+        given, has n columns) and advance by m.  ``lse``: as draft_attend left it.  ``count``
+        int32 ``[b]``: sample j takes only the first count[j]; the samples' left padding has to
+        be set, and that tensor grows by m - count."""
+        if n is None:
+            n = lse.shape[-1] if lse is not None else q.shape[2] - row
+        m = path.shape[-1]
+        tree = self._ints(path, (self.dims.b, m), "path")
+        taken = None if count is None else self._ints(count, (self.dims.b,), "count")
+        rows = self._tree_rows(n, q, k, v, q, row)
+        bm_draft_accept(self.ctx, n, m, tree, taken, *rows[:3], q.shape[2], self._lse_ptr(lse, n),
+                        self._stream())
+
     def run_prefill(self, q, k, v, o, fused_cut=False) -> None:
         """Algorithm 1 prefill under the block loop: every block, then a cut
         (with ``fused_cut`` through prefill_block_cut)."""
@@ -729,6 +852,60 @@ class PDAttentionKV4(PDAttention):
             raise ValueError(f"slot0 {slot0}: beyond 32 bits")
         bm_kv4_read(self.dims, self.cache, slot0, n, k.data_ptr(), v.data_ptr(), n, self._stream())
         return k, v
+
+
+class WindowAttention(PDAttention):
+    """Attention with a sliding window and sinks over a cache of window + sinks rows a unit
+    (include/bm_window.h): a token sees the last ``window`` tokens, its own included, and the
+    first ``sinks`` of its sample.  ``prefill_block`` takes up to ``block`` tokens (by default
+    all of the prompt), ``decode_step`` one; drafted tokens as over a bounded cache.
+
+    ``k``, ``v``: ``[b, n_kv_heads, window + sinks, d]``; token j < sinks lies in slot j, any other
+    one in slot sinks + (j - sinks) mod window, j counted from the sample's first real token.
+    ``buffers``: those two and work."""
+
+    def __init__(self, *, window, sinks=0, b, s, max_gen, block=None, static_workspace=False, **kw):
+        if static_workspace:
+            raise ValueError("a window cache needs a caller-allocated workspace")
+        if not (1 <= window <= _INT32_MAX and 0 <= sinks <= _INT32_MAX):
+            raise ValueError(f"window {window} must be positive, sinks {sinks} not negative")
+        self.window, self.sinks = window, sinks
+        super().__init__(b=b, s=s, kv_max=window + sinks, block=s if block is None else block,
+                         max_gen=max_gen, **kw)
+
+    def _validate(self):
+        bm_win_validate(self.dims, self.sinks)
+        return self.dims.kv_max
+
+    def _buffers(self) -> dict:
+        d = self.dims
+        row = (d.b, d.n_kv_heads, self.cap, d.head_dim)
+        return {"k": (row, self.tdtype), "v": (row, self.tdtype)}
+
+    def _cache(self):
+        return bm_win_cache(self.k.data_ptr(), self.v.data_ptr(), *self._work_ptr())
+
+    @staticmethod
+    def _takes(given, want) -> bool:
+        # rows of another type would be read as other values
+        return given == want
+
+    _workspace_bytes = staticmethod(bm_win_workspace_bytes)
+
+    def _stream(self) -> int:
+        # the library launches on the current device: a stream of another one would not do
+        if self._dev_index is not None and self.torch.cuda.current_device() != self._dev_index:
+            raise ValueError(f"make {self.device} the current device")
+        return super()._stream()
+
+    def _new_context(self) -> int:
+        return bm_win_init(self.dims, self.sinks, self.cache)
+
+    def resume(self, next_pos: int) -> None:
+        """A context over the rows of the tokens before ``next_pos`` as they lie in k and v."""
+        if not -_INT32_MAX <= next_pos <= _INT32_MAX:
+            raise ValueError(f"next_pos {next_pos}: beyond 32 bits")
+        self._replace_context(bm_win_resume(self.dims, self.sinks, self.cache, next_pos))
 
 
 # ---------------------------------------------------------------------------

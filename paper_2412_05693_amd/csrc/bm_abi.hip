@@ -37,6 +37,9 @@ struct bm_ctx {
   void* k_scale;      // null: rows of dims.dtype
   void* v_scale;
   size_t rows_k_off, rows_v_off;
+  // a window cache (bm_window.h): no score, pos and len, cap = kv_max slots
+  int32_t window;     // 0: a bounded cache
+  int32_t sinks;
 };
 
 namespace {
@@ -189,6 +192,7 @@ int make_ctx(const bm_dims* dims, const bm_cache* cache, size_t work_need, bm_ct
   c->split = nullptr;
   c->k_scale = c->v_scale = nullptr;
   c->rows_k_off = c->rows_v_off = 0;
+  c->window = c->sinks = 0;
   *out = c;
   return BM_OK;
 }
@@ -451,14 +455,166 @@ BM_EXPORT int bm_kv4_read(const bm_dims* dims, const bm_kv4_cache* cache, int32_
   return kv4_rows(dims, cache, slot0, n, k, v, seq_ld, false, stream);
 }
 
+// ---------------------------------------------------------------------------
+// a window cache (bm_window.h)
+// ---------------------------------------------------------------------------
+namespace {
+
+int check_win(const bm_dims* d, int32_t sinks) {
+  if (!d) return fail(BM_ERR_INVALID_ARG, "dims is null");
+  if (d->block < 1) return fail(BM_ERR_INVALID_ARG, "block=%d must be positive", d->block);
+  bm_dims one = *d;
+  one.block = 1;      // (the blocks of a window cache are not bounded)
+  const int st = check_dims(&one);
+  if (st != BM_OK) return st;
+  if (sinks < 0 || sinks >= d->kv_max)
+    return fail(BM_ERR_INVALID_ARG, "sinks %d outside [0, kv_max=%d)", sinks, d->kv_max);
+  return BM_OK;
+}
+
+int win_ctx(const bm_dims* dims, int32_t sinks, const bm_win_cache* cache, int32_t next_pos,
+            bm_ctx** out) {
+  if (!out) return fail(BM_ERR_INVALID_ARG, "cache or out is null");
+  *out = nullptr;
+  const int st = check_win(dims, sinks);
+  if (st != BM_OK) return st;
+  if (!cache) return fail(BM_ERR_INVALID_ARG, "cache or out is null");
+  if (!cache->k || !cache->v || !cache->work)
+    return fail(BM_ERR_INVALID_ARG, "a cache pointer is null");
+  if (((uintptr_t)cache->k | (uintptr_t)cache->v | (uintptr_t)cache->work) & 15)
+    return fail(BM_ERR_INVALID_ARG, "k, v and work must be 16-byte aligned");
+  const size_t need = bm_win_workspace_bytes(dims);
+  if (cache->work_bytes < need)
+    return fail(BM_ERR_INVALID_ARG, "work_bytes %zu < required %zu", cache->work_bytes, need);
+  if (next_pos < 0 || next_pos > dims->s + dims->max_gen)
+    return fail(BM_ERR_INVALID_ARG, "resume state next_pos=%d is not reachable", next_pos);
+  bm_ctx* c = new (std::nothrow) bm_ctx{};
+  if (!c) return fail(BM_ERR_INVALID_ARG, "out of host memory");
+  c->dims = *dims;
+  c->cache = bm_cache{cache->k, cache->v, nullptr, nullptr, nullptr, cache->work, cache->work_bytes};
+  c->group = dims->n_heads / dims->n_kv_heads;
+  c->cap = dims->kv_max;
+  c->units = dims->b * dims->n_kv_heads;
+  c->elem_bytes = dims->dtype == BM_BF16 ? 2 : 4;
+  c->sm_scale = eff_scale(*dims);
+  c->kv_dec = dims->kv_max;
+  c->rule = BM_RANK_RECENT;
+  c->window = dims->kv_max - sinks;
+  c->sinks = sinks;
+  c->next_pos = next_pos;
+  c->last_pos = next_pos - 1;
+  c->len = next_pos < c->cap ? next_pos : c->cap;
+  *out = c;
+  return ok();
+}
+
+// The settings of scores and cuts have no meaning over a window cache.
+int no_window(const bm_ctx* ctx, const char* what) {
+  if (!ctx) return fail(BM_ERR_INVALID_ARG, "ctx is null");
+  if (ctx->window) return fail(BM_ERR_UNSUPPORTED, "a window cache has no %s", what);
+  return BM_OK;
+}
+
+void win_advance(bm_ctx* ctx, int32_t n) {
+  ctx->next_pos += n;
+  ctx->last_pos = ctx->next_pos - 1;
+  ctx->len = ctx->next_pos < ctx->cap ? ctx->next_pos : ctx->cap;
+}
+
+// The tokens of a checked prefill call.
+int win_prompt(bm_ctx* ctx, int32_t n_tok, const void* q, const void* k, const void* v, void* o,
+               int32_t seq_ld, hipStream_t stream) {
+  if (!bm::prompt_fits(ctx->units, ctx->group, n_tok))
+    return fail(BM_ERR_UNSUPPORTED, "%d tokens of %d units are too many for one launch", n_tok,
+                ctx->units);
+  bm::PromptArgs a;
+  a.q = q;
+  a.kin = k;
+  a.vin = v;
+  a.o = o;
+  a.kc = ctx->cache.k;
+  a.vc = ctx->cache.v;
+  a.pad = ctx->pad;
+  a.seq_ld = seq_ld;
+  a.n_heads = ctx->dims.n_heads;
+  a.n_kv_heads = ctx->dims.n_kv_heads;
+  a.units = ctx->units;
+  a.window = ctx->window;
+  a.sinks = ctx->sinks;
+  a.t0 = ctx->next_pos;
+  a.n_tok = n_tok;
+  a.scale_log2 = ctx->sm_scale * 1.4426950408889634f;
+  hipError_t e = bm::launch_prompt(a, ctx->dims.dtype, ctx->dims.head_dim, ctx->group, stream);
+  if (e != hipSuccess) return hip_fail(e, "window prompt launch");
+  if (ctx->split && (e = hipEventRecord(ctx->split, stream)) != hipSuccess)
+    return hip_fail(e, "split event record");
+  win_advance(ctx, n_tok);
+  return ok();
+}
+
+// n nodes over the context's cache as it is; nothing is advanced.
+bm::NodesArgs nodes_args(const bm_ctx* ctx, int32_t n, const int32_t* parent, const void* q,
+                         const void* k, const void* v, void* o, int32_t seq_ld, float* lse,
+                         void* work) {
+  bm::NodesArgs a;
+  a.q = q;
+  a.kin = k;
+  a.vin = v;
+  a.o = o;
+  a.lse = lse;
+  a.parent = parent;
+  a.kc = ctx->cache.k;
+  a.vc = ctx->cache.v;
+  a.pos = ctx->cache.pos;
+  a.pad = ctx->pad;
+  a.part = static_cast<float*>(work);
+  a.seq_ld = seq_ld;
+  a.n_heads = ctx->dims.n_heads;
+  a.n_kv_heads = ctx->dims.n_kv_heads;
+  a.units = ctx->units;
+  a.slots = ctx->cap;
+  a.len0 = ctx->len;
+  a.n = n;
+  a.next_pos = ctx->next_pos;
+  a.window = ctx->window;
+  a.sinks = ctx->sinks;
+  a.nsplit = 1;
+  a.store = 0;
+  a.scale_log2 = ctx->sm_scale * 1.4426950408889634f;
+  return a;
+}
+
+}  // namespace
+
+BM_EXPORT size_t bm_win_workspace_bytes(const bm_dims* dims) {
+  if (check_win(dims, 0) != BM_OK) return 0;
+  return bm::nodes_work_bytes(dims->b * dims->n_kv_heads, dims->head_dim,
+                              dims->n_heads / dims->n_kv_heads, 1);
+}
+
+BM_EXPORT int bm_win_validate(const bm_dims* dims, int32_t sinks) {
+  const int st = check_win(dims, sinks);
+  return st == BM_OK ? ok() : st;
+}
+
+BM_EXPORT int bm_win_init(const bm_dims* dims, int32_t sinks, const bm_win_cache* cache,
+                          bm_ctx** out) {
+  return win_ctx(dims, sinks, cache, 0, out);
+}
+
+BM_EXPORT int bm_win_resume(const bm_dims* dims, int32_t sinks, const bm_win_cache* cache,
+                            int32_t next_pos, bm_ctx** out) {
+  return win_ctx(dims, sinks, cache, next_pos, out);
+}
+
 namespace {
 
 int check_rule(const bm_ctx* ctx);
 int cut_to(bm_ctx* ctx, int target, int32_t curr_id, hipStream_t stream);
 
-// Checks of a prefill block (all on the host); fills the kernel arguments.
-int prefill_args(bm_ctx* ctx, int32_t t0, int32_t n_tok, const void* q, const void* k,
-                 const void* v, void* o, int32_t seq_ld, bm::PrefillArgs* out) {
+// Checks of a prefill call's arguments and order, over either cache.
+int check_block(const bm_ctx* ctx, int32_t t0, int32_t n_tok, const void* q, const void* k,
+                const void* v, const void* o, int32_t seq_ld) {
   if (!ctx) return fail(BM_ERR_INVALID_ARG, "ctx is null");
   if (!q || !k || !v || !o) return fail(BM_ERR_INVALID_ARG, "q, k, v or o is null");
   if (n_tok < 1 || n_tok > ctx->dims.block)
@@ -471,6 +627,14 @@ int prefill_args(bm_ctx* ctx, int32_t t0, int32_t n_tok, const void* q, const vo
   if ((int64_t)t0 + n_tok > ctx->dims.s)
     return fail(BM_ERR_ORDER, "block [%d, %d) runs past the prompt length s=%d", t0, t0 + n_tok,
                 ctx->dims.s);
+  return BM_OK;
+}
+
+// Checks of a bounded cache's prefill block (all on the host); fills the kernel arguments.
+int prefill_args(bm_ctx* ctx, int32_t t0, int32_t n_tok, const void* q, const void* k,
+                 const void* v, void* o, int32_t seq_ld, bm::PrefillArgs* out) {
+  const int st = check_block(ctx, t0, n_tok, q, k, v, o, seq_ld);
+  if (st != BM_OK) return st;
   if (ctx->len > ctx->dims.kv_max)
     return fail(BM_ERR_ORDER, "cache holds %d > kv_max=%d entries: evict before the next block",
                 ctx->len, ctx->dims.kv_max);
@@ -539,6 +703,10 @@ void advance(bm_ctx* ctx, int32_t t0, int32_t n_tok) {
 BM_EXPORT int bm_prefill_block(bm_ctx* ctx, int32_t t0, int32_t n_tok, const void* q,
                                const void* k, const void* v, void* o, int32_t seq_ld,
                                hipStream_t stream) {
+  if (ctx && ctx->window) {
+    const int ws = check_block(ctx, t0, n_tok, q, k, v, o, seq_ld);
+    return ws == BM_OK ? win_prompt(ctx, n_tok, q, k, v, o, seq_ld, stream) : ws;
+  }
   bm::PrefillArgs a;
   int st = prefill_args(ctx, t0, n_tok, q, k, v, o, seq_ld, &a);
   if (st != BM_OK) return st;
@@ -553,6 +721,14 @@ BM_EXPORT int bm_prefill_block(bm_ctx* ctx, int32_t t0, int32_t n_tok, const voi
 BM_EXPORT int bm_prefill_block_cut(bm_ctx* ctx, int32_t t0, int32_t n_tok, const void* q,
                                    const void* k, const void* v, void* o, int32_t seq_ld,
                                    hipStream_t stream) {
+  if (ctx && ctx->window) {
+    const int ws = check_block(ctx, t0, n_tok, q, k, v, o, seq_ld);
+    return ws == BM_OK ? win_prompt(ctx, n_tok, q, k, v, o, seq_ld, stream) : ws;
+  }
+  if (ctx && ctx->window) {
+    const int ws = check_block(ctx, t0, n_tok, q, k, v, o, seq_ld);
+    return ws == BM_OK ? win_prompt(ctx, n_tok, q, k, v, o, seq_ld, stream) : ws;
+  }
   bm::PrefillArgs a;
   int st = prefill_args(ctx, t0, n_tok, q, k, v, o, seq_ld, &a);
   if (st != BM_OK) return st;
@@ -698,7 +874,8 @@ BM_EXPORT int bm_evict_compact(bm_ctx* ctx, int32_t curr_id, hipStream_t stream)
 }
 
 BM_EXPORT int bm_set_rank_rule(bm_ctx* ctx, int32_t rule) {
-  if (!ctx) return fail(BM_ERR_INVALID_ARG, "ctx is null");
+  const int st = no_window(ctx, "ranking rule");
+  if (st != BM_OK) return st;
   if (rule != BM_RANK_AVE && rule != BM_RANK_SUM && rule != BM_RANK_RECENT &&
       rule != BM_RANK_TOVA)
     return fail(BM_ERR_INVALID_ARG, "unknown ranking rule %d", rule);
@@ -707,7 +884,8 @@ BM_EXPORT int bm_set_rank_rule(bm_ctx* ctx, int32_t rule) {
 }
 
 BM_EXPORT int bm_set_decode_bound(bm_ctx* ctx, int32_t bound) {
-  if (!ctx) return fail(BM_ERR_INVALID_ARG, "ctx is null");
+  const int st = no_window(ctx, "decode bound");
+  if (st != BM_OK) return st;
   if (bound < 1 || bound > ctx->dims.kv_max)
     return fail(BM_ERR_INVALID_ARG, "decode bound %d outside [1, kv_max=%d]", bound,
                 ctx->dims.kv_max);
@@ -729,14 +907,16 @@ BM_EXPORT int bm_set_split_event(bm_ctx* ctx, hipEvent_t event) {
 }
 
 BM_EXPORT int bm_set_score_accumulation(bm_ctx* ctx, int32_t on) {
-  if (!ctx) return fail(BM_ERR_INVALID_ARG, "ctx is null");
+  const int st = no_window(ctx, "scores");
+  if (st != BM_OK) return st;
   if (on != 0 && on != 1) return fail(BM_ERR_INVALID_ARG, "score accumulation flag %d", on);
   ctx->accumulate = on != 0;
   return ok();
 }
 
 BM_EXPORT int bm_set_decode_removal(bm_ctx* ctx, int32_t p) {
-  if (!ctx) return fail(BM_ERR_INVALID_ARG, "ctx is null");
+  const int st = no_window(ctx, "removals");
+  if (st != BM_OK) return st;
   if (p < 0 || p > ctx->dims.kv_max)
     return fail(BM_ERR_INVALID_ARG, "decode removal p=%d outside [0, kv_max=%d]", p,
                 ctx->dims.kv_max);
@@ -808,6 +988,16 @@ BM_EXPORT int bm_decode_step(bm_ctx* ctx, int32_t pos, const void* q, const void
   if ((int64_t)pos >= (int64_t)ctx->dims.s + ctx->dims.max_gen)
     return fail(BM_ERR_ORDER, "decode pos=%d beyond s + max_gen = %d", pos,
                 ctx->dims.s + ctx->dims.max_gen);
+  if (ctx->window) {
+    // one node that is then stored
+    bm::NodesArgs a = nodes_args(ctx, 1, nullptr, q, k, v, o, seq_ld, nullptr, ctx->cache.work);
+    a.store = 1;
+    const hipError_t e =
+        bm::launch_nodes(a, ctx->dims.dtype, ctx->dims.head_dim, ctx->group, stream);
+    if (e != hipSuccess) return hip_fail(e, "window decode launch");
+    win_advance(ctx, 1);
+    return ok();
+  }
   if (ctx->len > ctx->dims.kv_max)
     return fail(BM_ERR_CAPACITY, "cache holds %d > kv_max=%d entries: evict after the last block",
                 ctx->len, ctx->dims.kv_max);
@@ -908,6 +1098,135 @@ BM_EXPORT int bm_decode_step(bm_ctx* ctx, int32_t pos, const void* q, const void
   return ok();
 }
 
+// ---------------------------------------------------------------------------
+// drafted tokens (bm_draft.h)
+// ---------------------------------------------------------------------------
+namespace {
+
+// What both calls ask of the context and of the tree.
+int check_draft(const bm_ctx* ctx, int32_t n, const void* q, const void* k, const void* v,
+                int32_t seq_ld) {
+  if (!ctx) return fail(BM_ERR_INVALID_ARG, "ctx is null");
+  if (ctx->k_scale)
+    return fail(BM_ERR_UNSUPPORTED, "drafted tokens over a cache held in 4 bits");
+  if (ctx->p_dec > 0)
+    return fail(BM_ERR_UNSUPPORTED, "drafted tokens with a decode removal of p=%d", ctx->p_dec);
+  if (n < 1) return fail(BM_ERR_INVALID_ARG, "n %d < 1", n);
+  if (n > BM_DRAFT_MAX) return fail(BM_ERR_UNSUPPORTED, "n %d exceeds %d", n, BM_DRAFT_MAX);
+  if (seq_ld < n) return fail(BM_ERR_INVALID_ARG, "seq_ld %d < n %d", seq_ld, n);
+  if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v) & 15)
+    return fail(BM_ERR_INVALID_ARG, "q, k and v must be 16-byte aligned");
+  if (ctx->next_pos < ctx->dims.s)
+    return fail(BM_ERR_ORDER, "a draft at %d before the prompt (s=%d) is processed", ctx->next_pos,
+                ctx->dims.s);
+  return BM_OK;
+}
+
+}  // namespace
+
+BM_EXPORT size_t bm_draft_workspace_bytes(const bm_dims* dims, int32_t n) {
+  if (check_win(dims, 0) != BM_OK || n < 1 || n > BM_DRAFT_MAX) return 0;
+  return bm::nodes_work_bytes(dims->b * dims->n_kv_heads, dims->head_dim,
+                              dims->n_heads / dims->n_kv_heads, n);
+}
+
+BM_EXPORT int bm_draft_attend(bm_ctx* ctx, int32_t n, const int32_t* parent, const void* q,
+                              const void* k, const void* v, void* o, int32_t seq_ld, float* lse,
+                              void* work, size_t work_bytes, hipStream_t stream) {
+  int st = check_draft(ctx, n, q, k, v, seq_ld);
+  if (st != BM_OK) return st;
+  if (!q || !k || !v || !o) return fail(BM_ERR_INVALID_ARG, "q, k, v or o is null");
+  if (!parent || !work) return fail(BM_ERR_INVALID_ARG, "parent or work is null");
+  if (((uintptr_t)o | (uintptr_t)work) & 15)
+    return fail(BM_ERR_INVALID_ARG, "o and work must be 16-byte aligned");
+  if (((uintptr_t)parent | (uintptr_t)lse) & 3)
+    return fail(BM_ERR_INVALID_ARG, "parent and lse must be 4-byte aligned");
+  const size_t need = bm::nodes_work_bytes(ctx->units, ctx->dims.head_dim, ctx->group, n);
+  if (work_bytes < need)
+    return fail(BM_ERR_INVALID_ARG, "work_bytes %zu < required %zu", work_bytes, need);
+  if (ctx->next_pos >= ctx->dims.s + ctx->dims.max_gen)
+    return fail(BM_ERR_ORDER, "a draft at %d beyond s + max_gen = %d", ctx->next_pos,
+                ctx->dims.s + ctx->dims.max_gen);
+  if (!ctx->window && ctx->len > ctx->dims.kv_max)
+    return fail(BM_ERR_CAPACITY, "cache holds %d > kv_max=%d entries: evict after the last block",
+                ctx->len, ctx->dims.kv_max);
+  if (!ctx->window && ctx->len > ctx->kv_dec) {
+    if ((st = check_rule(ctx)) != BM_OK) return st;
+    if ((st = cut_to(ctx, ctx->kv_dec, ctx->last_pos, stream)) != BM_OK) return st;
+  }
+  const bm::NodesArgs a = nodes_args(ctx, n, parent, q, k, v, o, seq_ld, lse, work);
+  const hipError_t e = bm::launch_nodes(a, ctx->dims.dtype, ctx->dims.head_dim, ctx->group, stream);
+  if (e != hipSuccess) return hip_fail(e, "draft attention launch");
+  return ok();
+}
+
+BM_EXPORT int bm_draft_accept(bm_ctx* ctx, int32_t n, int32_t m, const int32_t* path,
+                              const int32_t* count, const void* q, const void* k, const void* v,
+                              int32_t seq_ld, const float* lse, hipStream_t stream) {
+  int st = check_draft(ctx, n, q, k, v, seq_ld);
+  if (st != BM_OK) return st;
+  if (m < 1 || m > n) return fail(BM_ERR_INVALID_ARG, "m %d outside [1, n=%d]", m, n);
+  if (!path || !k || !v) return fail(BM_ERR_INVALID_ARG, "path, k or v is null");
+  if (((uintptr_t)path | (uintptr_t)count | (uintptr_t)lse) & 3)
+    return fail(BM_ERR_INVALID_ARG, "path, count and lse must be 4-byte aligned");
+  if (count && !ctx->pad)
+    return fail(BM_ERR_ORDER, "count needs the samples' left padding (zeros where there is none)");
+  if ((int64_t)ctx->next_pos + m > (int64_t)ctx->dims.s + ctx->dims.max_gen)
+    return fail(BM_ERR_ORDER, "tokens [%d, %d) run past s + max_gen = %d", ctx->next_pos,
+                ctx->next_pos + m, ctx->dims.s + ctx->dims.max_gen);
+  const bool scores = !ctx->window && ctx->accumulate;
+  bool cuts = false;
+  if (!ctx->window) {
+    if (ctx->len > ctx->kv_dec)
+      return fail(BM_ERR_ORDER, "cache holds %d > decode bound %d entries", ctx->len, ctx->kv_dec);
+    if (ctx->len + m > ctx->cap)
+      return fail(BM_ERR_CAPACITY, "len %d + m %d exceeds cap %d", ctx->len, m, ctx->cap);
+    if (scores && (!q || !lse)) return fail(BM_ERR_INVALID_ARG, "q or lse is null");
+    cuts = ctx->len + m > ctx->kv_dec;
+    if (cuts && (!ctx->scores_valid || !ctx->accumulate) && ctx->rule != BM_RANK_RECENT)
+      return fail(BM_ERR_ORDER,
+                  "a block ran without score accumulation: only BM_RANK_RECENT can rank this cache");
+  }
+  bm::AcceptArgs a;
+  a.q = q;
+  a.kin = k;
+  a.vin = v;
+  a.lse = scores ? lse : nullptr;
+  a.path = path;
+  a.count = count;
+  a.kc = ctx->cache.k;
+  a.vc = ctx->cache.v;
+  a.score = ctx->cache.score;
+  a.pos = ctx->cache.pos;
+  a.len = ctx->cache.len;
+  a.lastw = scores && ctx->rule == BM_RANK_TOVA
+                ? reinterpret_cast<float*>(work_at(ctx, ctx->lay.lastw_off))
+                : nullptr;
+  // (the caller's array, which count says may be written)
+  a.pad = const_cast<int32_t*>(ctx->pad);
+  a.seq_ld = seq_ld;
+  a.n_heads = ctx->dims.n_heads;
+  a.n_kv_heads = ctx->dims.n_kv_heads;
+  a.units = ctx->units;
+  a.slots = ctx->cap;
+  a.len0 = ctx->len;
+  a.n = n;
+  a.m = m;
+  a.next_pos = ctx->next_pos;
+  a.window = ctx->window;
+  a.sinks = ctx->sinks;
+  a.scale_log2 = ctx->sm_scale * 1.4426950408889634f;
+  const hipError_t e = bm::launch_accept(a, ctx->dims.dtype, ctx->dims.head_dim, ctx->group, stream);
+  if (e != hipSuccess) return hip_fail(e, "accept launch");
+  if (ctx->window) {
+    win_advance(ctx, m);
+    return ok();
+  }
+  advance(ctx, ctx->next_pos, m);
+  if (cuts && (st = cut_to(ctx, ctx->kv_dec, ctx->last_pos, stream)) != BM_OK) return st;
+  return ok();
+}
+
 BM_EXPORT int32_t bm_ctx_len(const bm_ctx* ctx) { return ctx ? ctx->len : -1; }
 
 BM_EXPORT int32_t bm_ctx_next_pos(const bm_ctx* ctx) { return ctx ? ctx->next_pos : -1; }
@@ -988,7 +1307,7 @@ BM_EXPORT int bm_probe_mfma(int32_t iters, float* sink, int32_t blocks, hipStrea
 
 BM_EXPORT int32_t bm_prefill_tile_workgroups(const bm_ctx* ctx, int32_t n_tok, const void* q,
                                              const void* o, int32_t seq_ld) {
-  if (!ctx || n_tok < 1 || n_tok > ctx->dims.block || seq_ld < n_tok) return -1;
+  if (!ctx || ctx->window || n_tok < 1 || n_tok > ctx->dims.block || seq_ld < n_tok) return -1;
   bm::PrefillArgs a{};
   a.q = q;
   a.o = const_cast<void*>(o);

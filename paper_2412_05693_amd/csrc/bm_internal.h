@@ -7,9 +7,11 @@
 #include <stdint.h>
 
 #include "batchmax.h"
+#include "bm_draft.h"
 #include "bm_kv4.h"
 #include "bm_probe.h"
 #include "bm_synth.h"
+#include "bm_window.h"
 
 namespace bm {
 
@@ -173,6 +175,61 @@ struct Kv4RowsArgs {
   int units = 0, slots = 0, slot0 = 0, n = 0;
 };
 
+// Tokens t0 .. t0 + n_tok - 1 through a window cache (bm_window.h).
+struct PromptArgs {
+  const void* q;      // row t0 of [b, H, seq_ld, D]
+  const void* kin;    // row t0 of [b, Hk, seq_ld, D]
+  const void* vin;
+  void* o;
+  void* kc;           // cache [U, window + sinks, D]
+  void* vc;
+  const int32_t* pad; // [b] left pad tokens per sample, or null
+  int64_t seq_ld;
+  int n_heads, n_kv_heads, units, window, sinks, t0, n_tok;
+  float scale_log2;
+};
+
+// The n nodes of a tree (one: a token) over a cache: a bounded one of len0 entries
+// (window 0) or a window cache.
+struct NodesArgs {
+  const void* q;      // [b, H, seq_ld, D] row 0
+  const void* kin;    // [b, Hk, seq_ld, D]
+  const void* vin;
+  void* o;
+  float* lse;         // [b, H, n] or null
+  const int32_t* parent;   // [b, n], or null: every node is a root
+  void* kc;           // cache [U, slots, D]
+  void* vc;
+  const int32_t* pos; // [U, slots] (bounded cache)
+  const int32_t* pad; // [b] left pad tokens per sample, or null
+  float* part;        // [U][nsplit][G n][D] partial outputs, then their [..][2] (m, l)
+  int64_t seq_ld;
+  int n_heads, n_kv_heads, units, slots, len0, n, next_pos, window, sinks;
+  int nsplit;         // workgroups over a unit's entries (set by launch_nodes)
+  int store;          // the node's rows go into the window cache (n == 1)
+  float scale_log2;
+};
+
+// m of a tree's n nodes behind a cache.
+struct AcceptArgs {
+  const void* q;      // [b, H, seq_ld, D] row 0
+  const void* kin;    // [b, Hk, seq_ld, D]
+  const void* vin;
+  const float* lse;   // [b, H, n], or null: no scores
+  const int32_t* path;     // [b, m]
+  const int32_t* count;    // [b] or null
+  void* kc;           // cache [U, slots, D]
+  void* vc;
+  float* score;       // [U, slots] (bounded cache)
+  int32_t* pos;
+  int32_t* len;       // [U]
+  float* lastw;       // [U, slots] weights of the last accepted query, or null
+  int32_t* pad;       // [b], or null
+  int64_t seq_ld;
+  int n_heads, n_kv_heads, units, slots, len0, n, m, next_pos, window, sinks;
+  float scale_log2;
+};
+
 struct SynthArgs {
   void* q;
   void* k;
@@ -207,6 +264,13 @@ hipError_t launch_kv4_long(const Kv4DecodeArgs& a, int dtype, int head_dim, int 
 // read rows, then (independently: no slot and no row twice) write rows; either may have n = 0
 hipError_t launch_kv4_rows(const Kv4RowsArgs& read, const Kv4RowsArgs& write, int dtype,
                            int head_dim, hipStream_t stream);
+hipError_t launch_prompt(const PromptArgs& a, int dtype, int head_dim, int group, hipStream_t stream);
+// whether a launch of that size can be made
+bool prompt_fits(int units, int group, int n_tok);
+hipError_t launch_nodes(const NodesArgs& a, int dtype, int head_dim, int group, hipStream_t stream);
+// bytes of NodesArgs.part for n nodes, whatever the cache holds
+size_t nodes_work_bytes(int units, int head_dim, int group, int n);
+hipError_t launch_accept(const AcceptArgs& a, int dtype, int head_dim, int group, hipStream_t stream);
 hipError_t launch_reset(float* score, int32_t* len, size_t n_score, size_t n_len,
                         hipStream_t stream);
 hipError_t launch_synth_qkv(const SynthArgs& a, hipStream_t stream);

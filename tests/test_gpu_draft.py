@@ -1,0 +1,580 @@
+"""Drafted tokens over bounded and window caches: a tree's attention against a 64-bit
+reference, and accepted paths against the calls that would have brought the same tokens."""
+import pytest
+import torch
+
+from paper_2412_05693_amd import batchmax as bmx
+from test_gpu_window import DT, NAN, Run, rows
+from window_reference import check_rows, lineage, random_tree, tree_over
+
+pytestmark = pytest.mark.gpu
+
+
+class Bound:
+    """A bounded cache that has seen a prompt, and what the tests ask of it."""
+
+    def __init__(self, *, dtype="bf16", b=2, heads=4, kv_heads=1, d=128, s=150, kv_max=100, block=50, max_gen=256,
+                 pads=None, seed=1, rule=None, accumulate=True):
+        self.dtype, self.b, self.h, self.hk, self.d, self.seed = dtype, b, heads, kv_heads, d, seed
+        self.group = heads // kv_heads
+        self.att = bmx.PDAttention(b=b, s=s, kv_max=kv_max, block=block, max_gen=max_gen, n_heads=heads,
+                                   n_kv_heads=kv_heads, head_dim=d, dtype=dtype)
+        for x in (self.att.k, self.att.v):
+            x.fill_(NAN)
+        if rule:
+            self.att.set_rank_rule(rule)
+        self.att.set_score_accumulation(accumulate)
+        self.pads = None
+        if pads is not None:
+            self.pads = torch.tensor(pads, dtype=torch.int32, device="cuda")
+            self.att.set_left_padding(self.pads)
+        q, k, v = self.qkv(s)
+        o = torch.zeros_like(q)
+        self.att.run_prefill(q, k, v, o, fused_cut=True)
+        self.prompt = q, k, v
+
+    def qkv(self, t):
+        self.seed += 1
+        return [rows(1000 * self.seed + i, self.b, hh, t, self.d, self.dtype).cuda()
+                for i, hh in enumerate((self.h, self.hk, self.hk))]
+
+    def check_tree(self, parent, q, k, v, o, lse):
+        n, L = parent.shape[1], self.att.length
+        for j in range(self.b):
+            pad = 0 if self.pads is None else max(0, int(self.pads[j]))
+            for head in range(self.h):
+                u = head // self.group
+                seen = (self.att.pos[j, u, :L] >= pad).cpu()
+                exact = tree_over(self.att.k[j, u, :L], self.att.v[j, u, :L], seen, parent[j].tolist(), q[j, head, :n],
+                                  k[j, u, :n], v[j, u, :n], self.d ** -0.5, DT[self.dtype])
+                check_rows(o[j, head, :n], exact, f"sample {j} head {head}")
+                for a, row in enumerate(exact):
+                    assert abs(float(lse[j, head, a]) - row.lse) <= row.lse_tol, (j, head, a)
+
+    def entries(self, j, u, pad=0):
+        """{position less the pad: (score, k row, v row)} of the entries that are no pads."""
+        L = self.att.length
+        pos = self.att.pos[j, u, :L].tolist()
+        assert len(set(pos)) == L
+        sc, k, v = (x[j, u, :L].cpu() for x in (self.att.score, self.att.k, self.att.v))
+        return {p - pad: (float(sc[i]), k[i], v[i]) for i, p in enumerate(pos) if p >= pad}
+
+
+def trees(b, n, seed=0):
+    chain = torch.arange(-1, n - 1).expand(b, n).int().contiguous()
+    flat = torch.full((b, n), -1, dtype=torch.int32)
+    odd = random_tree(b, n, seed + 1)
+    odd[:, 0] = 7                                            # parents that come after their node,
+    odd[:, n // 2] = n // 2                                  # are it, or are no node: roots
+    odd[:, n - 1] = 2 ** 31 - 1
+    odd[0, n // 3] = -2 ** 31
+    return {"chain": chain, "flat": flat, "random": random_tree(b, n, seed), "odd": odd}
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,heads,kv_heads", [(128, 4, 1), (64, 4, 2), (128, 2, 2), (64, 3, 3), (64, 4, 1), (128, 4, 2)])
+@pytest.mark.parametrize("n", [1, 5, 16, 33, 64])
+def test_a_tree_over_a_bounded_cache(dtype, d, heads, kv_heads, n):
+    c = Bound(dtype=dtype, d=d, heads=heads, kv_heads=kv_heads)
+    before = [x.clone() for x in (c.att.k, c.att.v, c.att.score, c.att.pos, c.att.len)]
+    for name, parent in trees(c.b, n).items():
+        q, k, v = c.qkv(n)
+        o, lse = torch.full_like(q, 5), torch.zeros((c.b, c.h, n), device="cuda")
+        c.att.draft_attend(parent.cuda(), q, k, v, o, lse=lse)
+        c.check_tree(parent, q, k, v, o, lse)
+        o2 = torch.zeros_like(o)
+        c.att.draft_attend(parent.cuda(), q, k, v, o2)       # without the log-sum-exps
+        assert torch.equal(o, o2), name
+    for x, y in zip(before, (c.att.k, c.att.v, c.att.score, c.att.pos, c.att.len)):
+        assert torch.equal(x.nan_to_num(), y.nan_to_num())
+    assert c.att.length == 100 and c.att.next_pos == 150
+
+
+@pytest.mark.parametrize("length", [1, 2, 31, 32, 33, 127, 128, 129, 500])
+@pytest.mark.parametrize("n,group", [(1, 1), (3, 4), (17, 2), (64, 4)])
+def test_cache_lengths_at_tile_borders(length, n, group):
+    c = Bound(b=1, heads=group, kv_heads=1, s=length, kv_max=600, block=512)
+    parent = random_tree(1, n, length)
+    q, k, v = c.qkv(n)
+    o, lse = torch.zeros_like(q), torch.zeros((1, group, n), device="cuda")
+    c.att.draft_attend(parent.cuda(), q, k, v, o, lse=lse)
+    c.check_tree(parent, q, k, v, o, lse)
+
+
+def test_an_empty_cache():
+    c = Bound(b=1, s=10, kv_max=600)
+    c.att.resume(0, 10)
+    parent = random_tree(1, 9, 4)
+    q, k, v = c.qkv(9)
+    o, lse = torch.zeros_like(q), torch.zeros((1, 4, 9), device="cuda")
+    c.att.draft_attend(parent.cuda(), q, k, v, o, lse=lse)
+    c.check_tree(parent, q, k, v, o, lse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("length,n", [(5000, 7), (9000, 64), (4096, 1)])
+def test_a_tree_over_a_long_cache(dtype, length, n):
+    """Caches that several workgroups share."""
+    c = Bound(dtype=dtype, b=1, heads=4, kv_heads=2, d=64, s=length, kv_max=length, block=1000, accumulate=False)
+    parent = random_tree(1, n, length)
+    q, k, v = c.qkv(n)
+    o, lse = torch.zeros_like(q), torch.zeros((1, 4, n), device="cuda")
+    c.att.draft_attend(parent.cuda(), q, k, v, o, lse=lse)
+    c.check_tree(parent, q, k, v, o, lse)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,group", [(3, 1), (13, 4), (64, 2)])
+def test_padded_samples(dtype, n, group):
+    """Pads in the cache weigh nothing whatever their rows hold, and samples of pads alone
+    see the nodes alone."""
+    c = Bound(dtype=dtype, b=3, heads=2 * group, kv_heads=2, s=90, kv_max=120, d=64, pads=[0, 33, 90])
+    L = c.att.length
+    hidden = c.att.pos[:, :, :L] < c.pads[:, None, None]
+    for x in (c.att.k, c.att.v):
+        x[:, :, :L][hidden] = NAN
+    parent = random_tree(3, n, 9)
+    q, k, v = c.qkv(n)
+    o, lse = torch.zeros_like(q), torch.zeros((3, 2 * group, n), device="cuda")
+    c.att.draft_attend(parent.cuda(), q, k, v, o, lse=lse)
+    c.check_tree(parent, q, k, v, o, lse)
+
+
+def test_nodes_before_a_sample_begins():
+    """Pads beyond the prompt: nodes at pad positions give zeros and -inf."""
+    c = Bound(b=2, s=20, kv_max=50)
+    c.pads = torch.tensor([0, 22], dtype=torch.int32, device="cuda")
+    c.att.set_left_padding(c.pads)
+    parent = torch.arange(-1, 4).expand(2, 5).int().contiguous()
+    q, k, v = c.qkv(5)
+    o, lse = torch.ones_like(q), torch.zeros((2, 4, 5), device="cuda")
+    c.att.draft_attend(parent.cuda(), q, k, v, o, lse=lse)
+    assert (o[1, :, :2] == 0).all() and (lse[1, :, :2] == -float("inf")).all()
+    # the third node is the sample's first token
+    want = tree_over(k[1, 0, :0], v[1, 0, :0], torch.zeros(0, dtype=torch.bool), [-1, 0, 1], q[1, 2, 2:5], k[1, 0, 2:5],
+                     v[1, 0, 2:5], 128 ** -0.5, torch.bfloat16)
+    check_rows(o[1, 2, 2:5], want)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [NAN, float("inf"), -float("inf")])
+@pytest.mark.parametrize("n,group", [(6, 4), (40, 1), (64, 4)])
+def test_nodes_that_are_no_ancestors_weigh_nothing(dtype, bad, n, group):
+    """Rows that a program never filled (unused nodes, another branch) reach their own
+    descendants alone."""
+    c = Bound(dtype=dtype, b=2, heads=group, kv_heads=1, d=64)
+    parent = random_tree(2, n, 5)
+    unused = [2, n - 1]
+    parent[:, 3:n - 1][parent[:, 3:n - 1] == 2] = 0          # nobody hangs from node 2
+    q, k, v = c.qkv(n)
+    for a in unused:
+        k[:, :, a] = bad
+        v[:, :, a] = bad
+    o, lse = torch.zeros_like(q), torch.zeros((2, group, n), device="cuda")
+    c.att.draft_attend(parent.cuda(), q, k, v, o, lse=lse)
+    for x in (q, k, v, o):
+        x[:, :, unused] = 0
+    for j in range(2):
+        for head in range(group):
+            L = c.att.length
+            exact = tree_over(c.att.k[j, 0, :L], c.att.v[j, 0, :L], torch.ones(L, dtype=torch.bool), parent[j].tolist(),
+                              q[j, head], k[j, 0], v[j, 0], 64 ** -0.5, DT[dtype])
+            for a, row in enumerate(exact):
+                if a not in unused:
+                    check_rows(o[j, head, a:a + 1], [row], f"node {a}")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("heads,kv_heads,d", [(4, 1, 128), (2, 2, 64), (4, 2, 64)])
+@pytest.mark.parametrize("window,sinks,tokens", [(40, 4, 200), (3, 2, 50), (1, 0, 9), (300, 0, 120), (64, 20, 30), (2500, 4, 3001)])
+def test_a_tree_over_a_window_cache(dtype, heads, kv_heads, d, window, sinks, tokens):
+    r = Run(dtype=dtype, window=window, sinks=sinks, s=tokens, b=3, heads=heads, kv_heads=kv_heads, d=d,
+            pads=[0, 5, tokens])
+    r.go(tokens, heads=(), samples=())
+    before = r.att.k.clone()
+    for n in (1, 6, 29):
+        parent = trees(3, n)["chain"] if n == 6 else random_tree(3, n, n)
+        q, k, v = (rows(50 + n + i, 3, hh, n, d, dtype) for i, hh in enumerate((heads, kv_heads, kv_heads)))
+        o, lse = torch.zeros_like(q).cuda(), torch.zeros((3, heads, n), device="cuda")
+        r.att.draft_attend(parent.cuda(), q.cuda(), k.cuda(), v.cuda(), o, lse=lse)
+        want = r.ref.tree(parent, q, k, v, heads=range(heads) if tokens < 1000 else (heads - 1,))
+        for (j, head), exact in want.items():
+            check_rows(o[j, head], exact, f"sample {j} head {head} n {n}")
+            for a, row in enumerate(exact):
+                assert abs(float(lse[j, head, a]) - row.lse) <= row.lse_tol, (j, head, a)
+    assert torch.equal(before.nan_to_num(), r.att.k.nan_to_num())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("bad", [NAN, float("inf")])
+def test_cached_rows_that_the_window_hides_from_some_nodes(dtype, bad):
+    """An entry that shallow nodes see and deep ones do not reaches the shallow ones alone."""
+    r = Run(dtype=dtype, window=20, sinks=2, s=60, b=1, heads=2, d=64)
+    r.go(60)
+    # the token at index 60 - 20 + 2 is the oldest that a node of depth 1 sees
+    slot = 2 + (42 - 2) % 20
+    r.att.v[0, :, slot] = bad
+    parent = torch.arange(-1, 5).expand(1, 6).int().contiguous()
+    q, k, v = (rows(5 + i, 1, hh, 6, 64, dtype) for i, hh in enumerate((2, 1, 1)))
+    o = torch.zeros_like(q).cuda()
+    r.att.draft_attend(parent.cuda(), q.cuda(), k.cuda(), v.cuda(), o)
+    want = r.ref.tree(parent, q, k, v)
+    for head in range(2):
+        assert not torch.isfinite(o[0, head, :2].float()).any()
+        check_rows(o[0, head, 2:], want[0, head][2:])
+
+
+# --------------------------------------------------------------------------
+# accepted paths
+# --------------------------------------------------------------------------
+def pick_path(parent, m, seed):
+    """A chain of m nodes from a root in every sample's tree (some are made)."""
+    g = torch.Generator().manual_seed(seed)
+    b, n = parent.shape
+    path = torch.stack([torch.randperm(n, generator=g)[:m].sort().values for _ in range(b)])
+    for j in range(b):
+        up = -1
+        for a in path[j].tolist():
+            parent[j, a] = up
+            up = a
+    return path.int()
+
+
+def gather(x, path):
+    return x.gather(2, path.long().to(x.device)[:, None, :, None].expand(-1, x.shape[1], -1, x.shape[3])).contiguous()
+
+
+def same_entries(got, want, exact_sets=True):
+    assert set(got) == set(want)
+    for p, (score, k, v) in want.items():
+        assert abs(got[p][0] - score) <= 1e-3 * abs(score) + 1e-5, (p, got[p][0], score)   # the parity protocol's
+        assert torch.equal(got[p][1], k) and torch.equal(got[p][2], v), p
+
+
+@pytest.mark.parametrize("rule", ["ave", "sum", "recent", "tova"])
+@pytest.mark.parametrize("dtype,heads,kv_heads,d", [("bf16", 4, 1, 128), ("f32", 4, 2, 64), ("bf16", 2, 2, 64)])
+@pytest.mark.parametrize("m,s", [(1, 150), (4, 150), (7, 97), (3, 60)])
+def test_an_accepted_path_is_a_prefill_block(rule, dtype, heads, kv_heads, d, m, s):
+    """Accepting a path leaves what a prompt of m more tokens leaves: entries, scores and
+    lengths, at the bound, on the way over it, and below it; generation then goes on alike."""
+    kw = dict(dtype=dtype, heads=heads, kv_heads=kv_heads, d=d, rule=rule, block=50)
+    c, e = Bound(s=s, **kw), Bound(s=s, **kw)
+    n = 12
+    parent = random_tree(2, n, m)
+    path = pick_path(parent, m, s)
+    q, k, v = c.qkv(n)
+    o, lse = torch.zeros_like(q), torch.zeros((2, heads, n), device="cuda")
+    c.att.draft_attend(parent.cuda(), q, k, v, o, lse=lse)
+    c.att.draft_accept(path.cuda(), q, k, v, lse=lse)
+    # the same state with a longer prompt
+    e.att.dims.s = s + m
+    e.att.resume(e.att.length, s)
+    qe, ke, ve = (gather(x, path) for x in (q, k, v))
+    oe = torch.zeros_like(qe)
+    e.att.prefill_block_cut(s, m, qe, ke, ve, oe, row=0)
+    assert c.att.length == e.att.length == min(100, s + m) and c.att.next_pos == e.att.next_pos == s + m
+    assert torch.equal(c.att.len, e.att.len) and (c.att.len == c.att.length).all()
+    tol = 2e-2 if dtype == "bf16" else 1e-4                          # the parity protocol's
+    assert (gather(o, path) - oe).abs().max() <= tol
+    for j in range(2):
+        for u in range(kv_heads):
+            same_entries(c.entries(j, u), e.entries(j, u))
+    x = c.qkv(1)
+    oc, oe = torch.zeros_like(x[0]), torch.zeros_like(x[0])
+    c.att.decode_step(s + m, *x, oc)
+    e.att.decode_step(s + m, *x, oe)
+    assert (oc - oe).abs().max() <= tol
+    for j in range(2):
+        for u in range(kv_heads):
+            same_entries(c.entries(j, u), e.entries(j, u))
+
+
+@pytest.mark.parametrize("rule", ["ave", "recent", "tova"])
+@pytest.mark.parametrize("dtype,pads", [("bf16", [0, 0, 0]), ("f32", [0, 20, 7])])
+@pytest.mark.parametrize("s", [150, 70])
+def test_samples_that_take_different_numbers(rule, dtype, pads, s):
+    """Rounds in which every sample takes its own number of tokens, and steps between them:
+    each sample ends where it ends by itself."""
+    kw = dict(dtype=dtype, heads=4, kv_heads=2, d=64, rule=rule, block=30, s=s)
+    c = Bound(b=3, pads=pads, **kw)
+    alone = [Bound(b=1, pads=[pads[j]], **kw) for j in range(3)]
+    q, k, v = c.prompt
+    for j, x in enumerate(alone):                                    # the batch's own prompts
+        x.att.reset()
+        mine = [y[j:j + 1].contiguous() for y in (q, k, v)]
+        x.att.run_prefill(*mine, torch.zeros_like(mine[0]), fused_cut=True)
+    n, m = 9, 4
+    tol = 2e-2 if dtype == "bf16" else 1e-4
+    for round_, taken in enumerate([(4, 1, 0), (2, 2, 4), (0, 0, 0), (1, 4, 3), (3, 3, 3)]):
+        parent = random_tree(3, n, round_)
+        path = pick_path(parent, m, round_)
+        q, k, v = c.qkv(n)
+        o, lse = torch.zeros_like(q), torch.zeros((3, 4, n), device="cuda")
+        c.att.draft_attend(parent.cuda(), q, k, v, o, lse=lse)
+        count = torch.tensor(taken, dtype=torch.int32, device="cuda")
+        c.att.draft_accept(path.cuda(), q, k, v, lse=lse, count=count)
+        step = c.qkv(1)
+        os_ = torch.zeros_like(step[0])
+        c.att.decode_step(c.att.next_pos, *step, os_)
+        for j, x in enumerate(alone):
+            mine = [y[j:j + 1].contiguous() for y in (q, k, v)]
+            oj, lj = torch.zeros_like(mine[0]), torch.zeros((1, 4, n), device="cuda")
+            x.att.draft_attend(parent[j:j + 1].contiguous().cuda(), *mine, oj, lse=lj)
+            assert (oj[0] - o[j]).abs().max() <= tol, (round_, j)
+            if taken[j]:
+                x.att.draft_accept(path[j:j + 1, :taken[j]].contiguous().cuda(), *mine, lse=lj)
+            mine = [y[j:j + 1].contiguous() for y in step]
+            oj = torch.zeros_like(mine[0])
+            x.att.decode_step(x.att.next_pos, *mine, oj)
+            assert (oj[0] - os_[j]).abs().max() <= tol, (round_, j)
+            late = c.att.next_pos - x.att.next_pos
+            assert int(c.pads[j]) == pads[j] + late
+            for u in range(2):
+                same_entries(c.entries(j, u, int(c.pads[j])), x.entries(0, u, pads[j]))
+
+
+def test_counts_and_path_numbers_outside_their_range():
+    """They are taken within it: nothing is read or written elsewhere."""
+    kw = dict(b=2, pads=[0, 0], s=60, block=30)
+    c, e = Bound(**kw), Bound(**kw)
+    q, k, v = c.qkv(5)
+    e.seed = c.seed
+    parent = torch.arange(-1, 4).expand(2, 5).int().contiguous().cuda()
+    path = torch.tensor([[0, 1, 2], [0, 3, 4]], dtype=torch.int32, device="cuda")
+    wild = torch.tensor([[-7, 1, 2], [-2 ** 31, 3, 2 ** 31 - 1]], dtype=torch.int32, device="cuda")
+    for x, p, count in ((c, wild, [99, -1]), (e, path, [3, 0])):
+        o, lse = torch.zeros_like(q), torch.zeros((2, 4, 5), device="cuda")
+        x.att.draft_attend(parent, q, k, v, o, lse=lse)
+        x.att.draft_accept(p, q, k, v, lse=lse, count=torch.tensor(count, dtype=torch.int32, device="cuda"))
+    assert torch.equal(c.pads, e.pads) and torch.equal(c.att.score[:, :, :63], e.att.score[:, :, :63])
+    for y in ("k", "v", "pos"):
+        a, b = getattr(c.att, y), getattr(e.att, y)
+        assert torch.equal(a[:, :, :63], b[:, :, :63])
+        if y != "pos":
+            assert torch.isnan(a[:, :, 63:]).all()
+
+
+def test_the_same_node_twice():
+    """A path that names a node twice appends its row twice."""
+    c = Bound(b=1, s=60, block=30, heads=1)
+    q, k, v = c.qkv(3)
+    o, lse = torch.zeros_like(q), torch.zeros((1, 1, 3), device="cuda")
+    c.att.draft_attend(torch.tensor([[-1, 0, 1]], dtype=torch.int32, device="cuda"), q, k, v, o, lse=lse)
+    c.att.draft_accept(torch.tensor([[1, 1]], dtype=torch.int32, device="cuda"), q, k, v, lse=lse)
+    assert c.att.length == 62
+    assert torch.equal(c.att.k[0, 0, 60], k[0, 0, 1]) and torch.equal(c.att.k[0, 0, 61], k[0, 0, 1])
+
+
+def test_without_scores():
+    """Score accumulation off: lse is not needed, new entries get score 0, and only the most
+    recent can then rank."""
+    c = Bound(b=1, s=90, block=30, accumulate=False, rule="recent")
+    q, k, v = c.qkv(4)
+    parent = torch.arange(-1, 3).view(1, 4).int().cuda()
+    o = torch.zeros_like(q)
+    c.att.draft_attend(parent, q, k, v, o)
+    path = torch.arange(4).view(1, 4).int().cuda()
+    c.att.draft_accept(path, q, k, v)
+    assert c.att.length == 94 and (c.att.score[:, :, :94] == 0).all()
+    for _ in range(3):
+        c.att.draft_attend(parent, q, k, v, o)
+        c.att.draft_accept(path, q, k, v)
+    assert c.att.length == 100 and sorted(c.att.pos[0, 0, :100].tolist()) == list(range(6, 106))
+    c.att.set_rank_rule("ave")
+    with pytest.raises(bmx.BatchMaxError):
+        c.att.draft_accept(path, q, k, v)
+
+
+def test_a_decode_bound_below_the_cache():
+    """The attention first cuts to the bound, as a step does; the acceptance keeps to it."""
+    c, e = Bound(b=2, s=150), Bound(b=2, s=150)
+    for x in (c, e):
+        x.att.set_decode_bound(64)
+    q, k, v = c.qkv(3)
+    parent = torch.arange(-1, 2).expand(2, 3).int().contiguous().cuda()
+    o, lse = torch.zeros_like(q), torch.zeros((2, 4, 3), device="cuda")
+    c.att.draft_attend(parent, q, k, v, o, lse=lse)
+    assert c.att.length == 64
+    oe = torch.zeros_like(q)
+    e.att.decode_step(150, q, k, v, oe)                  # its row 0 sees the same cache
+    assert (o[:, :, 0] - oe[:, :, 0]).abs().max() <= 2e-2
+    c.att.draft_accept(torch.zeros((2, 1), dtype=torch.int32, device="cuda"), q, k, v, lse=lse)
+    assert c.att.length == 64
+    for j in range(2):
+        same_entries(c.entries(j, 0), e.entries(j, 0))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window,sinks,tokens", [(40, 4, 90), (2, 1, 30), (3, 0, 30), (100, 8, 5)])
+def test_accepted_paths_over_a_window_cache(dtype, window, sinks, tokens):
+    """Rounds with the samples' own numbers of tokens, against the reference's sequences."""
+    r = Run(dtype=dtype, window=window, sinks=sinks, s=tokens, b=3, heads=2, kv_heads=2, d=64, pads=[0, 3, 4])
+    r.go(tokens, heads=(), samples=())
+    pads = r.att._pads
+    n, m = 8, 5
+    for round_, taken in enumerate([None, (5, 0, 2), (1, 5, 5), (0, 0, 0), (4, 3, 1)]):
+        parent = random_tree(3, n, round_)
+        path = pick_path(parent, m, round_)
+        q, k, v = (rows(70 * round_ + i, 3, 2, n, 64, dtype) for i in range(3))
+        o = torch.zeros_like(q).cuda()
+        r.att.draft_attend(parent.cuda(), q.cuda(), k.cuda(), v.cuda(), o)
+        for (j, head), exact in r.ref.tree(parent, q, k, v).items():
+            check_rows(o[j, head], exact, f"round {round_} sample {j} head {head}")
+        count = None if taken is None else torch.tensor(taken, dtype=torch.int32)
+        old = pads.clone()
+        r.att.draft_accept(path.cuda(), q.cuda(), k.cuda(), v.cuda(), count=None if count is None else count.cuda())
+        r.ref.accept(path, count, k, v)
+        assert torch.equal(pads, old + (0 if count is None else m - count.cuda()))
+        r.check_slots()
+        r.pads = None                                # (its rows need no pads any more)
+        r.go(1, step=True)
+        r.check_slots()
+
+
+def test_count_needs_left_padding():
+    c = Bound(b=2, s=60)
+    q, k, v = c.qkv(2)
+    o, lse = torch.zeros_like(q), torch.zeros((2, 4, 2), device="cuda")
+    c.att.draft_attend(torch.full((2, 2), -1, dtype=torch.int32, device="cuda"), q, k, v, o, lse=lse)
+    with pytest.raises(bmx.BatchMaxError) as err:
+        c.att.draft_accept(torch.zeros((2, 1), dtype=torch.int32, device="cuda"), q, k, v, lse=lse,
+                           count=torch.ones(2, dtype=torch.int32, device="cuda"))
+    assert err.value.status == bmx.BM_ERR_ORDER and c.att.length == 60 and c.att.next_pos == 60
+
+
+def test_a_workspace_full_of_nan_changes_no_bit():
+    c = Bound(b=1, s=5000, kv_max=5000, block=1000, accumulate=False)
+    parent = random_tree(1, 20, 3).cuda()
+    q, k, v = c.qkv(20)
+    outs = []
+    for fill in (0, 255):
+        o = torch.zeros_like(q)
+        c.att.draft_attend(parent, q, k, v, o)
+        c.att._draft_work.fill_(fill)
+        o = torch.zeros_like(q)
+        c.att.draft_attend(parent, q, k, v, o)
+        outs.append(o)
+    assert torch.equal(*outs)
+
+
+def test_rows_of_larger_buffers():
+    c = Bound(b=2, s=60)
+    parent = random_tree(2, 6, 8)
+    q, k, v = c.qkv(6)
+    big = []
+    for x in (q, k, v):
+        y = torch.full((2, x.shape[1], 11, 128), NAN, dtype=x.dtype, device="cuda")
+        y[:, :, 3:9] = x
+        big.append(y)
+    o, lse = torch.full_like(big[0], 9), torch.zeros((2, 4, 6), device="cuda")
+    c.att.draft_attend(parent.cuda(), *big, o, lse=lse, row=3)
+    c.check_tree(parent, q, k, v, o[:, :, 3:9].contiguous(), lse)
+    assert (o[:, :, :3] == 9).all() and (o[:, :, 9:] == 9).all()
+    path = pick_path(parent, 2, 1)
+    c.att.draft_accept(path.cuda(), *big, lse=lse, row=3)
+    assert torch.equal(c.att.k[:, :, 60:62], gather(k, path)) and torch.equal(c.att.v[:, :, 60:62], gather(v, path))
+
+
+@pytest.mark.parametrize("kind", ["bound", "window"])
+def test_a_round_in_a_graph(kind):
+    """A captured round, replayed from the same state with eager work between: the same bits."""
+    if kind == "bound":
+        c = Bound(b=3, pads=[0, 4, 60], s=150, heads=4, kv_heads=2)
+        att, pads, hk = c.att, c.pads, 2
+        names = ("k", "v", "score", "pos", "len")
+    else:
+        c = Run(window=50, sinks=4, s=150, b=3, pads=[0, 4, 60], heads=4, kv_heads=2)
+        c.go(150, heads=(), samples=())
+        att, pads, hk = c.att, c.att._pads, 2
+        names = ("k", "v")
+    n, m = 10, 3
+    parent = random_tree(3, n, 2)
+    path = pick_path(parent, m, 2).cuda()
+    parent, count = parent.cuda(), torch.tensor([3, 1, 0], dtype=torch.int32, device="cuda")
+    q, k, v = (rows(i, 3, hh, n, 128, "bf16").cuda() for i, hh in enumerate((4, hk, hk)))
+    o, lse = torch.zeros_like(q), torch.zeros((3, 4, n), device="cuda")
+    start = {x: getattr(att, x).clone() for x in names} | {"pads": pads.clone()}
+    state = lambda: {x: getattr(att, x) for x in names} | {"pads": pads}             # noqa: E731
+
+    def again():
+        for x, y in state().items():
+            y.copy_(start[x])
+        o.zero_()
+        lse.zero_()
+
+    def go():
+        att.draft_attend(parent, q, k, v, o, lse=lse)
+        att.draft_accept(path, q, k, v, lse=lse, count=count)
+
+    length, pos = att.length, att.next_pos
+    go()
+    want = {x: y.clone() for x, y in state().items()} | {"o": o.clone(), "lse": lse.clone()}
+    again()
+    att.resume(*((length, pos) if kind == "bound" else (pos,)))
+    side, g = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(g, stream=side):
+        go()
+    torch.cuda.current_stream().wait_stream(side)
+    other = Bound(b=1, s=60)
+    for i in range(3):
+        again()
+        g.replay()
+        if i == 0:
+            x = other.qkv(64)
+            other.att.draft_attend(random_tree(1, 64, 1).cuda(), *x, torch.zeros_like(x[0]))
+            att._draft_works.append(torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+        torch.cuda.synchronize()
+        got = state() | {"o": o, "lse": lse}
+        for x, y in want.items():
+            assert torch.equal(y.nan_to_num(), got[x].nan_to_num()), (i, x)
+
+
+def test_two_streams():
+    a, b = Bound(seed=1, s=300, kv_max=300, block=300), Bound(seed=9, s=300, kv_max=300, block=300)
+    parent = random_tree(2, 30, 3)
+    data = [x.qkv(30) for x in (a, b)]
+    outs = [(torch.zeros_like(x[0]), torch.zeros((2, 4, 30), device="cuda")) for x in data]
+    tree = parent.cuda()
+    torch.cuda.synchronize()
+    for c, x, (o, lse) in zip((a, b), data, outs):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            c.att.draft_attend(tree, *x, o, lse=lse)
+    torch.cuda.synchronize()
+    for c, x, (o, lse) in zip((a, b), data, outs):
+        c.check_tree(parent, *x, o, lse)
+
+
+def test_speculation_gives_what_steps_give():
+    """Prompt, then rounds whose paths hold the very tokens that steps would bring: the same
+    outputs, over a cache that removes nothing and over a window cache."""
+    for kind in ("bound", "window"):
+        out = []
+        for drafted in (False, True):
+            if kind == "bound":
+                c = Bound(b=2, s=80, kv_max=200, block=80, heads=4, kv_heads=2, dtype="f32", d=64, seed=5)
+                att = c.att
+            else:
+                c = Run(window=30, sinks=3, s=80, b=2, heads=4, kv_heads=2, dtype="f32", d=64, seed=5)
+                c.go(80, heads=(), samples=())
+                att = c.att
+            q, k, v = (rows(900 + i, 2, hh, 24, 64, "f32").cuda() for i, hh in enumerate((4, 2, 2)))
+            o = torch.zeros_like(q)
+            if not drafted:
+                for t in range(24):
+                    att.decode_step(80 + t, q, k, v, o, row=t)
+            else:
+                for t in range(0, 24, 4):
+                    # the four tokens as nodes 1, 3, 4, 6 of a tree with other branches
+                    parent = torch.tensor([[-1, -1, 1, 1, 3, 0, 4]] * 2, dtype=torch.int32, device="cuda")
+                    where = [1, 3, 4, 6]
+                    x = [torch.randn((2, y.shape[1], 7, 64), device="cuda") for y in (q, k, v)]
+                    for y, z in zip(x, (q, k, v)):
+                        y[:, :, where] = z[:, :, t:t + 4]
+                    ot, lse = torch.zeros_like(x[0]), torch.zeros((2, 4, 7), device="cuda")
+                    att.draft_attend(parent, *x, ot, lse=lse)
+                    o[:, :, t:t + 4] = ot[:, :, where]
+                    att.draft_accept(torch.tensor([where] * 2, dtype=torch.int32, device="cuda"), *x, lse=lse)
+            out.append(o)
+        assert (out[0] - out[1]).abs().max() <= 1e-5, kind
+    assert lineage([-1, -1, 1, 1, 3, 0, 4])[6] == [1, 3, 4, 6]
