@@ -18,13 +18,15 @@ def bounds(dtype, z_off, p, vv, *, packed):
     the absolute products at most A, off by (d + 3) 2^-24 A; exp2 and its argument add 2 ulp
     (2^-22).  A weight p = e / l has that error twice (its own and the sum's), sums of L terms
     add L 2^-24 each way, and rescaling by the running maximum one rounding a tile of 32 keys.
-    Packed weights are one bfloat16 each (half a step: 2^-8 relative), and outputs are
-    rounded once to their type (half a step of their size).
+    Packed weights are one bfloat16 each (half a step: 2^-8 relative).  Others of a bfloat16
+    product are two, the nearest bfloat16, off by at most 2^-8 p, and the nearest one to
+    that rest, off by at most 2^-8 of it: 2^-16 p.  Outputs are rounded once to their type
+    (half a step of their size).
     """
     length = p.shape[-1]
     rel_p = 2 * (z_off + 2.0 ** -22) + (2 * length + length / 16 + 8) * 2.0 ** -24
-    if packed:
-        rel_p = rel_p + 2.0 ** -8
+    if dtype == torch.bfloat16:
+        rel_p = rel_p + (2.0 ** -8 if packed else 2.0 ** -16)
     return rel_p * (p @ vv), torch.finfo(dtype).eps / 2
 
 
