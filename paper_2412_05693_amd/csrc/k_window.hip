@@ -6,8 +6,25 @@
 #include "bm_lanes.h"
 #include "bm_window_dev.h"
 
+// a lambda of the kernel, always part of it
+#define BM_LAMBDA __device__ __attribute__((always_inline))
+
 namespace bm {
 namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __bf16 __attribute__((vector_size(8))) bf16v4;   // operand type of the LDS transpose read
+typedef __attribute__((address_space(3))) bf16v4 lds_bf16v4;
+typedef __attribute__((address_space(3))) void lds_void;
+typedef __attribute__((address_space(3))) u32x4 lds_u32x4;
+// the LDS object at byte `off` (an address kept as a number, so that it takes one register
+// and an immediate offset)
+template <typename T>
+__device__ __forceinline__ T* lds_at(uint32_t off) { return (T*)(uintptr_t)off; }
 
 constexpr float kNegInf = -__builtin_huge_valf();
 
@@ -16,9 +33,397 @@ __device__ __forceinline__ float as_float(float x) { return x; }
 __device__ __forceinline__ void put(uint16_t* p, float x) { *reinterpret_cast<__bf16*>(p) = (__bf16)x; }
 __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 
-// one wave a query row
+// ---- bfloat16: tiles of 64 keys in LDS, 256 query rows a workgroup ----
+//
+// A workgroup is one unit and 256 / G tokens in all its G heads; a wave owns 64 rows of one
+// head (two tiles of 32).  The keys that some row sees are numbered v = 0, 1, ..: the sinks
+// before the first row's window, then everything from there to the last row.  With the row's
+// index i and `shift` = what an index has more than its number behind the sinks, key v is
+// visible iff  v <= i - shift  and  (v < sinks  or  v > i - shift - window).
+//
+// In halves of 32 keys, three stages at a time, so that matrix and vector work is there
+// for each other: the logits of half t + 1 (S^T = K Q^T), the weights of half t, and
+// O^T += V^T P^T of half t - 1.  LDS row order and operand layouts are those of the
+// prefill kernel: K rows with bits 2 and 3 of their number swapped, so that a lane's
+// logits are the second product's operand, V through the transposing LDS read.
+// A wave of 64 rows reads every tile once for two products, which halves the LDS traffic
+// of one with 32 rows.
+constexpr int kPromptRows = 64;              // of a wave
+constexpr int kPromptWaves = 4;
+constexpr int kPromptTile = 64;              // keys
+constexpr float kRescaleLog2 = 8.0f;         // the maximum moves once a logit is 2^8 beyond it
+
+__device__ __forceinline__ int kappa(int m) { return (m & ~12) | ((m & 4) << 1) | ((m & 8) >> 1); }
+
+// chunk c of an LDS row r lies at position c ^ swz(r): no bank conflicts
+template <int RB>
+__device__ __forceinline__ constexpr int swz_k(int r) { return RB >= 256 ? r & 15 : (r >> 1) & 7; }
+template <int RB>
+__device__ __forceinline__ constexpr int swz_v(int r) { return RB >= 256 ? (r & 3) << 2 : ((r >> 1) & 1) << 2; }
+
+__device__ __forceinline__ float xhalf_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  bf16x2 r = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, r);
+}
+// logit register r of lane half h within a half tile: its key
+__device__ __forceinline__ constexpr int key_of(int r, int h) {
+  return 16 * (r >> 3) + 8 * h + 4 * ((r >> 2) & 1) + (r & 3);
+}
+
+template <int D, int G>
+__global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(PromptArgs a, int tiles_per_unit) {
+  constexpr int RB = 2 * D, CPR = RB / 16, KK = D / 16, MT = D / 32;
+  constexpr int TILE = kPromptTile * RB;                     // bytes
+  constexpr int NCOPY = kPromptTile * CPR / (64 * kPromptWaves);   // 16-byte chunks of a thread and tile
+  constexpr int RPC = kPromptTile / NCOPY;                   // rows of a round of copies
+  constexpr int PT = kPromptWaves * kPromptRows / G;         // tokens of a workgroup
+  __shared__ __attribute__((aligned(2 * TILE))) char lds[4 * TILE];
+  char* const kbuf = lds;
+  char* const vbuf = lds + 2 * TILE;
+
+  // workgroups of a unit on one XCD (they share keys): ids go round-robin over the 8 XCDs
+  const int nwg = gridDim.x, L = blockIdx.x, q8 = nwg >> 3, r8 = nwg & 7, xcd = L & 7;
+  const int lin = xcd * q8 + min(xcd, r8) + (L >> 3);
+  const int u = lin / tiles_per_unit, pt = lin - u * tiles_per_unit;
+  const int bi = u / a.n_kv_heads, hk = u - bi * a.n_kv_heads;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int n = lane & 31, h = lane >> 5;
+  const int pad = a.pad ? max(0, __builtin_amdgcn_readfirstlane(a.pad[bi])) : 0;
+  const int r0 = a.t0 - pad;                                 // the index of the call's first token
+  const int p0 = pt * PT, tw = p0 + (w / G) * kPromptRows;   // first token of the workgroup, the wave
+  const int p1 = min(p0 + PT, a.n_tok);
+  const int64_t head = (int64_t)bi * a.n_heads + hk * G + w % G;
+
+  if (r0 + p1 - 1 < 0) {
+    // pad tokens alone
+    for (int c = lane; c < kPromptRows * CPR; c += 64) {
+      const int t = tw + c / CPR;
+      if (t < a.n_tok)
+        *reinterpret_cast<u32x4*>(static_cast<char*>(a.o) + (head * a.seq_ld + t) * RB + (c % CPR) * 16) = u32x4{0, 0, 0, 0};
+    }
+    return;
+  }
+
+  // ---- the keys' numbers ----
+  const int first = max(r0 + p0, 0), last = r0 + p1 - 1;     // indices of real rows
+  const int lo = max(0, first - a.window + 1);
+  const int lead = min(a.sinks, lo), shift = lo - lead;
+  const int nv = lead + last - lo + 1;
+  const int nt = (nv + kPromptTile - 1) / kPromptTile;
+  // ring places of the cached keys: number v lies at place0 + v (less the window at its end)
+  const int ring0 = max(lo, a.sinks) - a.sinks;
+  const int place0 = ring0 % a.window - (ring0 + a.sinks - shift);
+  const char* kc = static_cast<const char*>(a.kc) + (int64_t)u * (a.window + a.sinks) * RB;
+  const char* vc = static_cast<const char*>(a.vc) + (int64_t)u * (a.window + a.sinks) * RB;
+  const char* ki = static_cast<const char*>(a.kin) + (int64_t)u * a.seq_ld * RB;
+  const char* vi = static_cast<const char*>(a.vin) + (int64_t)u * a.seq_ld * RB;
+
+  // ---- copies: thread's chunk of rows crow, crow + RPC, .. of a tile, through registers ----
+  const int crow = threadIdx.x / CPR, cch = threadIdx.x % CPR;
+  u32x4 ks[NCOPY], vs[NCOPY];
+  auto load_rows = [&](u32x4 (&x)[NCOPY], const char* cached, const char* input, int t) BM_LAMBDA {
+    const int v0 = t * kPromptTile;
+    const int j0 = v0 + shift;
+    if (v0 >= lead && j0 >= r0 && v0 + kPromptTile <= nv) {
+      // rows of the call alone: one run
+      const char* p = input + (int64_t)(j0 - r0) * RB;
+#pragma unroll
+      for (int i = 0; i < NCOPY; ++i)
+        x[i] = *reinterpret_cast<const u32x4*>(p + (crow + i * RPC) * RB + cch * 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NCOPY; ++i) {
+        const int v = min(v0 + crow + i * RPC, nv - 1);
+        const int j = v < lead ? v : v + shift;
+        int slot = j;
+        if (j >= a.sinks) {
+          slot = place0 + v;
+          slot = a.sinks + (slot >= a.window ? slot - a.window : slot);
+        }
+        const char* p = j < r0 ? cached + (int64_t)slot * RB : input + (int64_t)(j - r0) * RB;
+        x[i] = *reinterpret_cast<const u32x4*>(p + cch * 16);
+      }
+    }
+  };
+  auto store_k = [&](int t) BM_LAMBDA {
+#pragma unroll
+    for (int i = 0; i < NCOPY; ++i) {
+      const int r = crow + i * RPC, at = (r & ~31) + kappa(r & 31);
+      *reinterpret_cast<u32x4*>(kbuf + (t & 1) * TILE + at * RB + (cch ^ swz_k<RB>(at)) * 16) = ks[i];
+    }
+  };
+  auto store_v = [&](int t) BM_LAMBDA {
+#pragma unroll
+    for (int i = 0; i < NCOPY; ++i) {
+      const int r = crow + i * RPC;
+      *reinterpret_cast<u32x4*>(vbuf + (t & 1) * TILE + r * RB + (cch ^ swz_v<RB>(r)) * 16) = vs[i];
+    }
+  };
+  load_rows(ks, kc, ki, 0);
+  load_rows(vs, vc, vi, 0);
+
+  // ---- queries: lane (n, h) holds row n, chunks 2 kk + h ----
+  bf16x8 qf[2][KK];
+#pragma unroll
+  for (int rt = 0; rt < 2; ++rt) {
+    const int t = min(tw + 32 * rt + n, a.n_tok - 1);
+    const char* q = static_cast<const char*>(a.q) + (head * a.seq_ld + t) * RB;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      qf[rt][kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(q + 16 * (2 * kk + h)));
+  }
+  store_k(0);
+  store_v(0);
+  load_rows(ks, kc, ki, min(1, nt - 1));
+  store_k(1);
+  load_rows(ks, kc, ki, min(2, nt - 1));
+  load_rows(vs, vc, vi, min(1, nt - 1));
+
+  // what a row sees, in key numbers (rows that are no tokens take the nearest one's)
+  int vhi[2];
+#pragma unroll
+  for (int rt = 0; rt < 2; ++rt)
+    vhi[rt] = max(min(r0 + tw + 32 * rt + n, last), first) - shift;
+  const int wfirst = max(min(r0 + tw, last), first) - shift;
+  const int wlast = max(min(r0 + tw + kPromptRows - 1, last), first) - shift;
+  // a half whose keys every row of the wave sees
+  auto plain = [&](int t) BM_LAMBDA {
+    const int v0 = 32 * t;
+    return v0 + 31 <= wfirst && (v0 + 31 < a.sinks || v0 > wlast - a.window);
+  };
+
+  const int frag0 = n * RB + (h ^ swz_k<RB>(n)) * 16;
+  const int j16 = lane & 15, vrow = 8 * h + (j16 >> 2);
+  const int vbase = vrow * RB + 16 * swz_v<RB>(vrow) + (16 * ((lane >> 4) & 1) + 4 * (j16 & 3)) * 2;
+  const float c2 = a.scale_log2;
+
+  f32x16 o[2][MT];
+  float m[2] = {kNegInf, kNegInf}, l[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) o[rt][mt] = f32x16{};
+
+  // operand addresses in LDS: K of tile t + 1's or t's parity, V of the half before
+  uint32_t ka[KK], va[MT];
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) ka[kk] = lds0 + (uint32_t)(frag0 ^ (32 * kk));
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt) va[mt] = lds0 + 3 * TILE + (uint32_t)(vbase ^ (64 * mt));
+
+  // hide what rows do not see of half t
+  auto hide = [&](f32x16 (&z)[2], float (&top)[2], int t) BM_LAMBDA {
+    const int v0 = 32 * t + 8 * h;
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt) {
+      // (lane half h's keys all have 8 h: it comes off the limits)
+      const int hi = vhi[rt] - v0, low = vhi[rt] - a.window - v0, sk = a.sinks - v0;
+      top[rt] = kNegInf;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int k = key_of(r, 0);
+        z[rt][r] = k <= hi && (k > low || k < sk) ? z[rt][r] : kNegInf;
+        top[rt] = fmaxf(top[rt], z[rt][r]);
+      }
+    }
+  };
+
+  // One half: zo holds half t's logits (what nobody sees is hidden), top their maxima, po half
+  // t - 1's weights.  KH, VH: which half of its tile t + 1, and t - 1, is.
+  auto step = [&](auto kh_tag, f32x16 (&zn)[2], f32x16 (&zo)[2], u32x4 (&pn)[2][2], const u32x4 (&po)[2][2],
+                  float (&top)[2], int t) BM_LAMBDA {
+    constexpr int KH = decltype(kh_tag)::value;
+    // the maximum a row's weights are taken against; O follows behind this step's product
+    float f[2] = {1.0f, 1.0f};
+    const bool raised = __ballot(top[0] * c2 > m[0] + kRescaleLog2 || top[1] * c2 > m[1] + kRescaleLog2) != 0;
+    if (raised) {
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt) {
+        const float mn = fmaxf(m[rt], xhalf_max(top[rt]) * c2);
+        f[rt] = mn == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - mn);
+        m[rt] = mn;
+        l[rt] *= f[rt];
+      }
+    }
+    float ref[2];
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt) ref[rt] = m[rt] == kNegInf ? 0.0f : m[rt];
+
+    // 2 KK logit products, then 4 MT value products; pairs of weights between them, in three
+    // stages (argument, exp2, sum and packing) so that none waits for the one before
+    constexpr int NQ = 2 * KK, NP = 4 * MT, NS = NQ + NP, kAhead = 2, NB = kAhead + 1;
+    bf16x8 kf[NB];
+    u32x4 vf[NB];
+    auto k_fetch = [&](int j) BM_LAMBDA {
+      kf[j % NB] = __builtin_bit_cast(bf16x8, *lds_at<lds_u32x4>(ka[j] + KH * 32 * RB));
+    };
+    auto v_fetch = [&](int j) BM_LAMBDA {
+      const uint32_t x = va[j % MT] + (KH * 32 + 16 * (j / MT)) * RB;
+      const bf16v4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_at<lds_bf16v4>(x));
+      const bf16v4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_at<lds_bf16v4>(x + 4 * RB));
+      const u32x2 y0 = __builtin_bit_cast(u32x2, x0), y1 = __builtin_bit_cast(u32x2, x1);
+      vf[j % NB] = u32x4{y0.x, y0.y, y1.x, y1.y};
+    };
+    float x[2][2], e[2][2];
+    float sum[2] = {0.0f, 0.0f};
+    auto args = [&](int p) BM_LAMBDA {   // pair p: logits 2 p, 2 p + 1 of the lane's 32
+#pragma unroll
+      for (int i = 0; i < 2; ++i) x[p & 1][i] = fmaf(zo[p / 8][2 * (p % 8) + i], c2, -ref[p / 8]);
+    };
+    auto exps = [&](int p) BM_LAMBDA {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) e[p & 1][i] = __builtin_amdgcn_exp2f(x[p & 1][i]);
+    };
+    auto sums = [&](int p) BM_LAMBDA {
+      sum[p / 8] += e[p & 1][0];
+      sum[p / 8] += e[p & 1][1];
+      pn[p / 8][(p / 4) & 1][p & 3] = pack2(e[p & 1][0], e[p & 1][1]);
+    };
+    auto pair = [&](int p) BM_LAMBDA {
+      exps(p);
+      if (p > 0) sums(p - 1);
+      if (p + 1 < 16) args(p + 1);
+    };
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) k_fetch(j);
+    args(0);
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) {
+      const int kk = j / 2, rt = j % 2;
+      __builtin_amdgcn_sched_barrier(0);
+      zn[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk % NB], qf[rt][kk], kk == 0 ? f32x16{} : zn[rt], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (rt == 0) {
+        if (kk + kAhead < KK) k_fetch(kk + kAhead);
+        else v_fetch(kk + kAhead - KK);
+      }
+#pragma unroll
+      for (int p = 0; p < 16; ++p)
+        if (p * NS / 16 == j) pair(p);
+    }
+    float nt0[2] = {kNegInf, kNegInf};
+#pragma unroll
+    for (int j = 0; j < NP; ++j) {
+      const int q = j / 2, rt = j % 2, mt = q % MT, s = q / MT;
+      __builtin_amdgcn_sched_barrier(0);
+      o[rt][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[q % NB]),
+                                                          __builtin_bit_cast(bf16x8, po[rt][s]), o[rt][mt], 0, 0, 0);
+      __builtin_amdgcn_sched_barrier(0);
+      if (rt == 0 && q + kAhead < NP / 2) v_fetch(q + kAhead);
+#pragma unroll
+      for (int p = 0; p < 16; ++p)
+        if (p * NS / 16 == NQ + j) pair(p);
+#pragma unroll
+      for (int r = 0; r < 32 / NP; ++r) {
+        const int i = j * (32 / NP) + r;
+        nt0[i / 16] = fmaxf(nt0[i / 16], zn[i / 16][i % 16]);
+      }
+    }
+    sums(15);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt) l[rt] += sum[rt];
+    if (raised) {
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) o[rt][mt] *= f[rt];
+    }
+    top[0] = nt0[0];
+    top[1] = nt0[1];
+    if (!plain(t + 1)) hide(zn, top, t + 1);
+  };
+
+  f32x16 za[2], zb[2];
+  u32x4 pa[2][2], pb[2][2];
+  float top[2] = {kNegInf, kNegInf};
+  // nothing comes before the first half: weights and values of zero
+#pragma unroll
+  for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) pb[rt][s] = u32x4{0, 0, 0, 0};
+  for (int c = threadIdx.x; c < 32 * CPR; c += 64 * kPromptWaves)
+    *reinterpret_cast<u32x4*>(vbuf + TILE + 32 * RB + c * 16) = u32x4{0, 0, 0, 0};
+  __syncthreads();
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk) {
+    const bf16x8 kf = __builtin_bit_cast(bf16x8, *lds_at<lds_u32x4>(ka[kk]));
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt)
+      za[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[rt][kk], kk == 0 ? f32x16{} : za[rt], 0, 0, 0);
+  }
+#pragma unroll
+  for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) top[rt] = fmaxf(top[rt], za[rt][r]);
+  if (!plain(0)) hide(za, top, 0);
+  // Tile t's halves: behind the first one K(t) and V(t - 1) are done with, and K(t + 2) and
+  // V(t + 1) take their places; the barrier behind the next tile's first half shows them.
+  for (int t = 0; t < nt; ++t) {
+    step(std::integral_constant<int, 1>{}, zb, za, pa, pb, top, 2 * t);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) ka[kk] ^= TILE;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) va[mt] ^= TILE;
+    __syncthreads();
+    if (t + 1 < nt) {
+      store_v(t + 1);
+      if (t + 2 < nt) store_k(t + 2);
+      load_rows(ks, kc, ki, min(t + 3, nt - 1));
+      load_rows(vs, vc, vi, min(t + 2, nt - 1));
+    }
+    step(std::integral_constant<int, 0>{}, za, zb, pb, pa, top, 2 * t + 1);
+  }
+  // the last half's values
+#pragma unroll
+  for (int q = 0; q < 2 * MT; ++q) {
+    const uint32_t x = va[q % MT] + (32 + 16 * (q / MT)) * RB;
+    const bf16v4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_at<lds_bf16v4>(x));
+    const bf16v4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_at<lds_bf16v4>(x + 4 * RB));
+    const u32x2 y0 = __builtin_bit_cast(u32x2, x0), y1 = __builtin_bit_cast(u32x2, x1);
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt)
+      o[rt][q % MT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4{y0.x, y0.y, y1.x, y1.y}),
+                                                              __builtin_bit_cast(bf16x8, pb[rt][q / MT]), o[rt][q % MT], 0, 0, 0);
+  }
+  __syncthreads();
+
+  // ---- outputs, through the wave's part of LDS into whole rows ----
+#pragma unroll
+  for (int rt = 0; rt < 2; ++rt) {
+    const float sum = lanes::add_xor<32>(l[rt]);
+    // (a pad token sees nothing)
+    const bool real = r0 + tw + 32 * rt + n >= 0;
+    const float inv = real ? 1.0f / sum : 0.0f;
+    char* ost = lds + w * (32 * RB);
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x16 x = o[rt][mt];
+        const int d0 = 32 * mt + 8 * i + 4 * h;
+        const u32x2 y = {pack2(x[4 * i] * inv, x[4 * i + 1] * inv), pack2(x[4 * i + 2] * inv, x[4 * i + 3] * inv)};
+        *reinterpret_cast<u32x2*>(ost + n * RB + ((d0 * 2) ^ (16 * swz_k<RB>(n)))) = real ? y : u32x2{0, 0};
+      }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int j = 0; j < 32 * CPR / 64; ++j) {
+      const int r = j * (64 / CPR) + lane / CPR, c = lane % CPR, t = tw + 32 * rt + r;
+      const u32x4 y = *reinterpret_cast<const u32x4*>(ost + r * RB + 16 * (c ^ swz_k<RB>(r)));
+      if (t < a.n_tok) *reinterpret_cast<u32x4*>(static_cast<char*>(a.o) + (head * a.seq_ld + t) * RB + c * 16) = y;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// ---- float32: one wave a query row ----
 template <typename E, int D>
-__global__ void __launch_bounds__(256) window_prompt_kernel(PromptArgs a) {
+__global__ void __launch_bounds__(256) window_rows_kernel(PromptArgs a) {
   constexpr int P = D / 64;
   const int group = a.n_heads / a.n_kv_heads;
   const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -86,21 +491,43 @@ __global__ void __launch_bounds__(256) window_store_kernel(PromptArgs a, int row
       *reinterpret_cast<const uint4*>(static_cast<const char*>(a.vin) + src);
 }
 
-template <typename E, int D>
-hipError_t launch_t(const PromptArgs& a, hipStream_t stream) {
-  const int group = a.n_heads / a.n_kv_heads;
-  const int64_t waves = (int64_t)a.units * group * a.n_tok;
-  hipLaunchKernelGGL((window_prompt_kernel<E, D>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0,
-                     stream, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+template <int RB>
+hipError_t launch_store(const PromptArgs& a, hipStream_t stream) {
   const int kept = a.n_tok < a.window ? a.n_tok : a.window;
   const int lead = a.sinks < a.n_tok - kept ? a.sinks : a.n_tok - kept;
-  constexpr int RB = D * (int)sizeof(E);
   const unsigned chunks = (unsigned)(((int64_t)(kept + lead) * (RB / 16) + 255) / 256);
   hipLaunchKernelGGL((window_store_kernel<RB>), dim3((unsigned)a.units, chunks), dim3(256), 0, stream, a,
                      kept + lead);
   return hipGetLastError();
+}
+
+template <int D, int G>
+hipError_t launch_bf16(const PromptArgs& a, hipStream_t stream) {
+  constexpr int PT = kPromptWaves * kPromptRows / G;
+  const int tiles = (a.n_tok + PT - 1) / PT;
+  hipLaunchKernelGGL((window_prompt_kernel<D, G>), dim3((unsigned)(a.units * tiles)), dim3(64 * kPromptWaves), 0,
+                     stream, a, tiles);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? launch_store<2 * D>(a, stream) : e;
+}
+
+template <int D>
+hipError_t launch_f32(const PromptArgs& a, hipStream_t stream) {
+  const int64_t waves = (int64_t)a.units * (a.n_heads / a.n_kv_heads) * a.n_tok;
+  hipLaunchKernelGGL((window_rows_kernel<float, D>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  return e == hipSuccess ? launch_store<4 * D>(a, stream) : e;
+}
+
+template <int D>
+hipError_t launch_d(const PromptArgs& a, int dtype, int group, hipStream_t stream) {
+  if (dtype == BM_F32) return launch_f32<D>(a, stream);
+  switch (group) {
+    case 1: return launch_bf16<D, 1>(a, stream);
+    case 2: return launch_bf16<D, 2>(a, stream);
+    case 4: return launch_bf16<D, 4>(a, stream);
+    default: return hipErrorInvalidValue;
+  }
 }
 
 }  // namespace
@@ -110,10 +537,7 @@ bool prompt_fits(int units, int group, int n_tok) {
 }
 
 hipError_t launch_prompt(const PromptArgs& a, int dtype, int head_dim, int group, hipStream_t stream) {
-  (void)group;
-  if (dtype == BM_BF16)
-    return head_dim == 128 ? launch_t<uint16_t, 128>(a, stream) : launch_t<uint16_t, 64>(a, stream);
-  return head_dim == 128 ? launch_t<float, 128>(a, stream) : launch_t<float, 64>(a, stream);
+  return head_dim == 128 ? launch_d<128>(a, dtype, group, stream) : launch_d<64>(a, dtype, group, stream);
 }
 
 }  // namespace bm
