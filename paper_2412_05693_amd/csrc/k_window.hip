@@ -74,6 +74,30 @@ __device__ __forceinline__ constexpr int key_of(int r, int h) {
   return 16 * (r >> 3) + 8 * h + 4 * ((r >> 2) & 1) + (r & 3);
 }
 
+// z = or += K Q^T of a 32 x 32 tile.  As assembly because z has to be in the registers that
+// vector instructions work on: for a kernel of more than 256 registers the compiler puts
+// every product's result into the accumulation registers, from which each of the
+// logits would have to be copied first (622 TFLOP/s like that).  Operands of a product
+// have arrived before it is issued (waits are the compiler's, for assembly too); what it
+// does not count are the 19 wait states until a vector instruction may read the result:
+// see z_settled and the steps' order.
+template <bool FIRST>
+__device__ __forceinline__ void mfma_z(f32x16& z, u32x4 k, u32x4 q) {
+  if constexpr (FIRST)
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, 0" : "=&v"(z) : "v"(k), "a"(q));
+  else
+    asm volatile("v_mfma_f32_32x32x16_bf16 %0, %1, %2, %0" : "+&v"(z) : "v"(k), "a"(q));
+}
+__device__ __forceinline__ void z_settled(f32x16 (&z)[2]) {
+  asm volatile("s_nop 15\n\ts_nop 3" : "+v"(z[0]), "+v"(z[1]));
+}
+
+// x = max(x, y, z): one instruction (of values that assembly made the compiler first makes
+// quiet numbers)
+__device__ __forceinline__ void max3(float& x, float y, float z) {
+  asm volatile("v_max3_f32 %0, %0, %1, %2" : "+v"(x) : "v"(y), "v"(z));
+}
+
 template <int D, int G>
 __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(PromptArgs a, int tiles_per_unit) {
   constexpr int RB = 2 * D, CPR = RB / 16, KK = D / 16, MT = D / 32;
@@ -81,8 +105,8 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   constexpr int NCOPY = kPromptTile * CPR / (64 * kPromptWaves);   // 16-byte chunks of a thread and tile
   constexpr int RPC = kPromptTile / NCOPY;                   // rows of a round of copies
   constexpr int PT = kPromptWaves * kPromptRows / G;         // tokens of a workgroup
-  __shared__ __attribute__((aligned(2 * TILE))) char lds[4 * TILE];
-  char* const kbuf = lds;
+  // two K tiles (t, t + 1) and three V tiles (t - 1, t, t + 1)
+  __shared__ __attribute__((aligned(2 * TILE))) char lds[5 * TILE];
   char* const vbuf = lds + 2 * TILE;
 
   // workgroups of a unit on one XCD (they share keys): ids go round-robin over the 8 XCDs
@@ -122,66 +146,64 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   const char* ki = static_cast<const char*>(a.kin) + (int64_t)u * a.seq_ld * RB;
   const char* vi = static_cast<const char*>(a.vin) + (int64_t)u * a.seq_ld * RB;
 
-  // ---- copies: thread's chunk of rows crow, crow + RPC, .. of a tile, through registers ----
+  // ---- copies: the thread's 16-byte chunk of rows crow, crow + RPC, .. of tile t's K and V,
+  //      through registers ----
   const int crow = threadIdx.x / CPR, cch = threadIdx.x % CPR;
+  const int coff = crow * RB + cch * 16;
   u32x4 ks[NCOPY], vs[NCOPY];
-  auto load_rows = [&](u32x4 (&x)[NCOPY], const char* cached, const char* input, int t) BM_LAMBDA {
+  auto load_tile = [&](int t) BM_LAMBDA {
     const int v0 = t * kPromptTile;
-    const int j0 = v0 + shift;
-    if (v0 >= lead && j0 >= r0 && v0 + kPromptTile <= nv) {
+    const int64_t row = (int64_t)v0 + shift - r0;
+    if (v0 >= lead && row >= 0 && v0 + kPromptTile <= nv) {
       // rows of the call alone: one run
-      const char* p = input + (int64_t)(j0 - r0) * RB;
+      const char *pk = ki + row * RB, *pv = vi + row * RB;
 #pragma unroll
-      for (int i = 0; i < NCOPY; ++i)
-        x[i] = *reinterpret_cast<const u32x4*>(p + (crow + i * RPC) * RB + cch * 16);
+      for (int i = 0; i < NCOPY; ++i) {
+        ks[i] = *reinterpret_cast<const u32x4*>(pk + (uint32_t)(coff + i * RPC * RB));
+        vs[i] = *reinterpret_cast<const u32x4*>(pv + (uint32_t)(coff + i * RPC * RB));
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < NCOPY; ++i) {
         const int v = min(v0 + crow + i * RPC, nv - 1);
         const int j = v < lead ? v : v + shift;
-        int slot = j;
-        if (j >= a.sinks) {
-          slot = place0 + v;
-          slot = a.sinks + (slot >= a.window ? slot - a.window : slot);
-        }
-        const char* p = j < r0 ? cached + (int64_t)slot * RB : input + (int64_t)(j - r0) * RB;
-        x[i] = *reinterpret_cast<const u32x4*>(p + cch * 16);
+        int slot = place0 + v;
+        slot = j < a.sinks ? j : a.sinks + (slot >= a.window ? slot - a.window : slot);
+        const bool old = j < r0;
+        const int64_t off = (int64_t)(old ? slot : j - r0) * RB + cch * 16;
+        ks[i] = *reinterpret_cast<const u32x4*>((old ? kc : ki) + off);
+        vs[i] = *reinterpret_cast<const u32x4*>((old ? vc : vi) + off);
       }
     }
   };
-  auto store_k = [&](int t) BM_LAMBDA {
+  // (rows RPC apart have the same order of bits and chunks)
+  const int kat = (crow & ~31) + kappa(crow & 31);
+  const int kst = kat * RB + (cch ^ swz_k<RB>(kat)) * 16, vst = crow * RB + (cch ^ swz_v<RB>(crow)) * 16;
+  auto store_tile = [&](int t, int v_at) BM_LAMBDA {
+    char *pk = lds + (t & 1) * TILE + kst, *pv = vbuf + v_at + vst;
 #pragma unroll
     for (int i = 0; i < NCOPY; ++i) {
-      const int r = crow + i * RPC, at = (r & ~31) + kappa(r & 31);
-      *reinterpret_cast<u32x4*>(kbuf + (t & 1) * TILE + at * RB + (cch ^ swz_k<RB>(at)) * 16) = ks[i];
+      *reinterpret_cast<u32x4*>(pk + i * RPC * RB) = ks[i];
+      *reinterpret_cast<u32x4*>(pv + i * RPC * RB) = vs[i];
     }
   };
-  auto store_v = [&](int t) BM_LAMBDA {
-#pragma unroll
-    for (int i = 0; i < NCOPY; ++i) {
-      const int r = crow + i * RPC;
-      *reinterpret_cast<u32x4*>(vbuf + (t & 1) * TILE + r * RB + (cch ^ swz_v<RB>(r)) * 16) = vs[i];
-    }
-  };
-  load_rows(ks, kc, ki, 0);
-  load_rows(vs, vc, vi, 0);
+  load_tile(0);
 
   // ---- queries: lane (n, h) holds row n, chunks 2 kk + h ----
-  bf16x8 qf[2][KK];
+  u32x4 qf[2][KK];
 #pragma unroll
   for (int rt = 0; rt < 2; ++rt) {
     const int t = min(tw + 32 * rt + n, a.n_tok - 1);
     const char* q = static_cast<const char*>(a.q) + (head * a.seq_ld + t) * RB;
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk)
-      qf[rt][kk] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(q + 16 * (2 * kk + h)));
+      qf[rt][kk] = *reinterpret_cast<const u32x4*>(q + 16 * (2 * kk + h));
   }
-  store_k(0);
-  store_v(0);
-  load_rows(ks, kc, ki, min(1, nt - 1));
-  store_k(1);
-  load_rows(ks, kc, ki, min(2, nt - 1));
-  load_rows(vs, vc, vi, min(1, nt - 1));
+#pragma nounroll
+  for (int t = 0; t < 2; ++t) {
+    store_tile(t, t * TILE);
+    load_tile(min(t + 1, nt - 1));
+  }
 
   // what a row sees, in key numbers (rows that are no tokens take the nearest one's)
   int vhi[2];
@@ -208,13 +230,13 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) o[rt][mt] = f32x16{};
 
-  // operand addresses in LDS: K of tile t + 1's or t's parity, V of the half before
+  // operand addresses in LDS: K of tile t + 1 or t, V of the half before
   uint32_t ka[KK], va[MT];
   const uint32_t lds0 = (uint32_t)(uintptr_t)(lds_void*)lds;
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) ka[kk] = lds0 + (uint32_t)(frag0 ^ (32 * kk));
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) va[mt] = lds0 + 3 * TILE + (uint32_t)(vbase ^ (64 * mt));
+  for (int mt = 0; mt < MT; ++mt) va[mt] = lds0 + (uint32_t)(vbase ^ (64 * mt));
 
   // hide what rows do not see of half t
   auto hide = [&](f32x16 (&z)[2], float (&top)[2], int t) BM_LAMBDA {
@@ -235,7 +257,7 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
 
   // One half: zo holds half t's logits (what nobody sees is hidden), top their maxima, po half
   // t - 1's weights.  KH, VH: which half of its tile t + 1, and t - 1, is.
-  auto step = [&](auto kh_tag, f32x16 (&zn)[2], f32x16 (&zo)[2], u32x4 (&pn)[2][2], const u32x4 (&po)[2][2],
+  auto step = [&](auto kh_tag, uint32_t v_at, f32x16 (&zn)[2], f32x16 (&zo)[2], u32x4 (&pn)[2][2], const u32x4 (&po)[2][2],
                   float (&top)[2], int t) BM_LAMBDA {
     constexpr int KH = decltype(kh_tag)::value;
     // the maximum a row's weights are taken against; O follows behind this step's product
@@ -257,13 +279,10 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
     // 2 KK logit products, then 4 MT value products; pairs of weights between them, in three
     // stages (argument, exp2, sum and packing) so that none waits for the one before
     constexpr int NQ = 2 * KK, NP = 4 * MT, NS = NQ + NP, kAhead = 2, NB = kAhead + 1;
-    bf16x8 kf[NB];
-    u32x4 vf[NB];
-    auto k_fetch = [&](int j) BM_LAMBDA {
-      kf[j % NB] = __builtin_bit_cast(bf16x8, *lds_at<lds_u32x4>(ka[j] + KH * 32 * RB));
-    };
+    u32x4 kf[NB], vf[NB];
+    auto k_fetch = [&](int j) BM_LAMBDA { kf[j % NB] = *lds_at<lds_u32x4>(ka[j] + KH * 32 * RB); };
     auto v_fetch = [&](int j) BM_LAMBDA {
-      const uint32_t x = va[j % MT] + (KH * 32 + 16 * (j / MT)) * RB;
+      const uint32_t x = va[j % MT] + v_at + (KH * 32 + 16 * (j / MT)) * RB;
       const bf16v4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_at<lds_bf16v4>(x));
       const bf16v4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_at<lds_bf16v4>(x + 4 * RB));
       const u32x2 y0 = __builtin_bit_cast(u32x2, x0), y1 = __builtin_bit_cast(u32x2, x1);
@@ -282,7 +301,9 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
     auto sums = [&](int p) BM_LAMBDA {
       sum[p / 8] += e[p & 1][0];
       sum[p / 8] += e[p & 1][1];
-      pn[p / 8][(p / 4) & 1][p & 3] = pack2(e[p & 1][0], e[p & 1][1]);
+      uint32_t y = pack2(e[p & 1][0], e[p & 1][1]);
+      asm volatile("" : "+v"(y), "+v"(sum[p / 8]));   // (made here, not where the next step uses it)
+      pn[p / 8][(p / 4) & 1][p & 3] = y;
     };
     auto pair = [&](int p) BM_LAMBDA {
       exps(p);
@@ -296,7 +317,8 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
     for (int j = 0; j < NQ; ++j) {
       const int kk = j / 2, rt = j % 2;
       __builtin_amdgcn_sched_barrier(0);
-      zn[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk % NB], qf[rt][kk], kk == 0 ? f32x16{} : zn[rt], 0, 0, 0);
+      if (kk == 0) mfma_z<true>(zn[rt], kf[kk % NB], qf[rt][kk]);
+      else mfma_z<false>(zn[rt], kf[kk % NB], qf[rt][kk]);
       __builtin_amdgcn_sched_barrier(0);
       if (rt == 0) {
         if (kk + kAhead < KK) k_fetch(kk + kAhead);
@@ -318,21 +340,28 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
 #pragma unroll
       for (int p = 0; p < 16; ++p)
         if (p * NS / 16 == NQ + j) pair(p);
+      // maxima of the new logits (the last of their products is kWait value products and the
+      // weights between them away)
+      constexpr int kWait = NP / 4, kPer = 16 / (NP - kWait) + (16 % (NP - kWait) != 0);
 #pragma unroll
-      for (int r = 0; r < 32 / NP; ++r) {
-        const int i = j * (32 / NP) + r;
-        nt0[i / 16] = fmaxf(nt0[i / 16], zn[i / 16][i % 16]);
+      for (int r = 0; r < kPer; ++r) {
+        const int i = (j - kWait) * kPer + r;
+        if (i >= 0 && i < 16) max3(nt0[i / 8], zn[i / 8][2 * (i % 8)], zn[i / 8][2 * (i % 8) + 1]);
       }
     }
     sums(15);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) l[rt] += sum[rt];
-    if (raised) {
+    if (__builtin_expect(raised, 0)) {
+      asm volatile("" : "+v"(f[0]), "+v"(f[1]));    // (not multiplied by 1 every time)
 #pragma unroll
       for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
-        for (int mt = 0; mt < MT; ++mt) o[rt][mt] *= f[rt];
+        for (int mt = 0; mt < MT; ++mt) {
+          o[rt][mt] *= f[rt];
+          asm volatile("" : "+a"(o[rt][mt]));       // (back in its registers on this path)
+        }
     }
     top[0] = nt0[0];
     top[1] = nt0[1];
@@ -348,41 +377,52 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
 #pragma unroll
     for (int s = 0; s < 2; ++s) pb[rt][s] = u32x4{0, 0, 0, 0};
   for (int c = threadIdx.x; c < 32 * CPR; c += 64 * kPromptWaves)
-    *reinterpret_cast<u32x4*>(vbuf + TILE + 32 * RB + c * 16) = u32x4{0, 0, 0, 0};
+    *reinterpret_cast<u32x4*>(vbuf + 2 * TILE + 32 * RB + c * 16) = u32x4{0, 0, 0, 0};
   __syncthreads();
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) {
-    const bf16x8 kf = __builtin_bit_cast(bf16x8, *lds_at<lds_u32x4>(ka[kk]));
+    const u32x4 kf = *lds_at<lds_u32x4>(ka[kk]);
 #pragma unroll
-    for (int rt = 0; rt < 2; ++rt)
-      za[rt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[rt][kk], kk == 0 ? f32x16{} : za[rt], 0, 0, 0);
+    for (int rt = 0; rt < 2; ++rt) {
+      if (kk == 0) mfma_z<true>(za[rt], kf, qf[rt][kk]);
+      else mfma_z<false>(za[rt], kf, qf[rt][kk]);
+    }
   }
+  z_settled(za);
 #pragma unroll
   for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) top[rt] = fmaxf(top[rt], za[rt][r]);
+    for (int r = 0; r < 16; r += 2) max3(top[rt], za[rt][r], za[rt][r + 1]);
   if (!plain(0)) hide(za, top, 0);
   // Tile t's halves: behind the first one K(t) and V(t - 1) are done with, and K(t + 2) and
-  // V(t + 1) take their places; the barrier behind the next tile's first half shows them.
+  // V(t + 2) take their places; the barrier behind the next tile's first half shows them.
+  uint32_t v_at = 4 * TILE;                    // V of tile t - 1
+  auto keep_o = [&]() BM_LAMBDA {
+    // (O stays in the accumulation registers over the loop)
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+a"(o[rt][mt]));
+  };
+  keep_o();
   for (int t = 0; t < nt; ++t) {
-    step(std::integral_constant<int, 1>{}, zb, za, pa, pb, top, 2 * t);
+    step(std::integral_constant<int, 1>{}, v_at, zb, za, pa, pb, top, 2 * t);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) ka[kk] ^= TILE;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt) va[mt] ^= TILE;
     __syncthreads();
-    if (t + 1 < nt) {
-      store_v(t + 1);
-      if (t + 2 < nt) store_k(t + 2);
-      load_rows(ks, kc, ki, min(t + 3, nt - 1));
-      load_rows(vs, vc, vi, min(t + 2, nt - 1));
+    if (t + 2 < nt) {
+      store_tile(t, v_at - 2 * TILE);
+      load_tile(min(t + 3, nt - 1));
     }
-    step(std::integral_constant<int, 0>{}, za, zb, pb, pa, top, 2 * t + 1);
+    v_at = v_at == 4 * TILE ? 2 * TILE : v_at + TILE;
+    keep_o();
+    step(std::integral_constant<int, 0>{}, v_at, za, zb, pb, pa, top, 2 * t + 1);
+    keep_o();
   }
   // the last half's values
 #pragma unroll
   for (int q = 0; q < 2 * MT; ++q) {
-    const uint32_t x = va[q % MT] + (32 + 16 * (q / MT)) * RB;
+    const uint32_t x = va[q % MT] + v_at + (32 + 16 * (q / MT)) * RB;
     const bf16v4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_at<lds_bf16v4>(x));
     const bf16v4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_at<lds_bf16v4>(x + 4 * RB));
     const u32x2 y0 = __builtin_bit_cast(u32x2, x0), y1 = __builtin_bit_cast(u32x2, x1);
