@@ -1,6 +1,7 @@
 // Tokens through a window cache (bm_window.h): a prompt's attention, and the storing of
 // its rows behind it.
 #include <type_traits>
+#include <utility>
 
 #include "bm_internal.h"
 #include "bm_lanes.h"
@@ -98,6 +99,12 @@ __device__ __forceinline__ void max3(float& x, float y, float z) {
   asm volatile("v_max3_f32 %0, %0, %1, %2" : "+v"(x) : "v"(y), "v"(z));
 }
 
+// f(0), f(1), .. with numbers that are constants
+template <typename F, int... I>
+__device__ __forceinline__ void each(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+
 template <int D, int G>
 __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(PromptArgs a, int tiles_per_unit) {
   constexpr int RB = 2 * D, CPR = RB / 16, KK = D / 16, MT = D / 32;
@@ -151,43 +158,47 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   const int crow = threadIdx.x / CPR, cch = threadIdx.x % CPR;
   const int coff = crow * RB + cch * 16;
   u32x4 ks[NCOPY], vs[NCOPY];
-  auto load_tile = [&](int t) BM_LAMBDA {
+  // a tile of the call's own rows alone is one run: no address arithmetic in vector registers
+  struct Run {
+    __amdgpu_buffer_rsrc_t k, v;
+    bool is;
+  };
+  auto run_of = [&](int t) BM_LAMBDA {
     const int v0 = t * kPromptTile;
     const int64_t row = (int64_t)v0 + shift - r0;
-    if (v0 >= lead && row >= 0 && v0 + kPromptTile <= nv) {
-      // rows of the call alone: one run
-      const char *pk = ki + row * RB, *pv = vi + row * RB;
+    Run r;
+    r.is = v0 >= lead && row >= 0 && v0 + kPromptTile <= nv;
+    r.k = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(ki + row * RB), 0, TILE, 0x00020000);
+    r.v = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(vi + row * RB), 0, TILE, 0x00020000);
+    return r;
+  };
+  auto load_k = [&](const Run& r, int i) BM_LAMBDA { ks[i] = __builtin_amdgcn_raw_buffer_load_b128(r.k, coff, i * RPC * RB, 0); };
+  auto load_v = [&](const Run& r, int i) BM_LAMBDA { vs[i] = __builtin_amdgcn_raw_buffer_load_b128(r.v, coff, i * RPC * RB, 0); };
+  auto load_mixed = [&](int t) BM_LAMBDA {
+    int v0 = t * kPromptTile + crow;
+    asm volatile("" : "+v"(v0));      // (nothing of it outside the branch that it is in)
 #pragma unroll
-      for (int i = 0; i < NCOPY; ++i) {
-        ks[i] = *reinterpret_cast<const u32x4*>(pk + (uint32_t)(coff + i * RPC * RB));
-        vs[i] = *reinterpret_cast<const u32x4*>(pv + (uint32_t)(coff + i * RPC * RB));
-      }
-    } else {
-#pragma unroll
-      for (int i = 0; i < NCOPY; ++i) {
-        const int v = min(v0 + crow + i * RPC, nv - 1);
-        const int j = v < lead ? v : v + shift;
-        int slot = place0 + v;
-        slot = j < a.sinks ? j : a.sinks + (slot >= a.window ? slot - a.window : slot);
-        const bool old = j < r0;
-        const int64_t off = (int64_t)(old ? slot : j - r0) * RB + cch * 16;
-        ks[i] = *reinterpret_cast<const u32x4*>((old ? kc : ki) + off);
-        vs[i] = *reinterpret_cast<const u32x4*>((old ? vc : vi) + off);
-      }
+    for (int i = 0; i < NCOPY; ++i) {
+      const int v = min(v0 + i * RPC, nv - 1);
+      const int j = v < lead ? v : v + shift;
+      int slot = place0 + v;
+      slot = j < a.sinks ? j : a.sinks + (slot >= a.window ? slot - a.window : slot);
+      const bool old = j < r0;
+      const int64_t off = (int64_t)(old ? slot : j - r0) * RB + cch * 16;
+      ks[i] = *reinterpret_cast<const u32x4*>((old ? kc : ki) + off);
+      vs[i] = *reinterpret_cast<const u32x4*>((old ? vc : vi) + off);
     }
   };
   // (rows RPC apart have the same order of bits and chunks)
   const int kat = (crow & ~31) + kappa(crow & 31);
   const int kst = kat * RB + (cch ^ swz_k<RB>(kat)) * 16, vst = crow * RB + (cch ^ swz_v<RB>(crow)) * 16;
-  auto store_tile = [&](int t, int v_at) BM_LAMBDA {
-    char *pk = lds + (t & 1) * TILE + kst, *pv = vbuf + v_at + vst;
-#pragma unroll
-    for (int i = 0; i < NCOPY; ++i) {
-      *reinterpret_cast<u32x4*>(pk + i * RPC * RB) = ks[i];
-      *reinterpret_cast<u32x4*>(pv + i * RPC * RB) = vs[i];
-    }
+  auto store_k = [&](int i, int t) BM_LAMBDA {
+    *reinterpret_cast<u32x4*>(lds + (t & 1) * TILE + kst + i * RPC * RB) = ks[i];
   };
-  load_tile(0);
+  auto store_v = [&](int i, int at) BM_LAMBDA {
+    *reinterpret_cast<u32x4*>(vbuf + at + vst + i * RPC * RB) = vs[i];
+  };
+  load_mixed(0);
 
   // ---- queries: lane (n, h) holds row n, chunks 2 kk + h ----
   u32x4 qf[2][KK];
@@ -201,8 +212,12 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   }
 #pragma nounroll
   for (int t = 0; t < 2; ++t) {
-    store_tile(t, t * TILE);
-    load_tile(min(t + 1, nt - 1));
+#pragma unroll
+    for (int i = 0; i < NCOPY; ++i) {
+      store_k(i, t);
+      store_v(i, t * TILE);
+    }
+    load_mixed(min(t + 1, nt - 1));
   }
 
   // what a row sees, in key numbers (rows that are no tokens take the nearest one's)
@@ -236,7 +251,7 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) ka[kk] = lds0 + (uint32_t)(frag0 ^ (32 * kk));
 #pragma unroll
-  for (int mt = 0; mt < MT; ++mt) va[mt] = lds0 + (uint32_t)(vbase ^ (64 * mt));
+  for (int mt = 0; mt < MT; ++mt) va[mt] = lds0 + 4 * TILE + (uint32_t)(vbase ^ (64 * mt));
 
   // hide what rows do not see of half t
   auto hide = [&](f32x16 (&z)[2], float (&top)[2], int t) BM_LAMBDA {
@@ -256,14 +271,22 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   };
 
   // One half: zo holds half t's logits (what nobody sees is hidden), top their maxima, po half
-  // t - 1's weights.  KH, VH: which half of its tile t + 1, and t - 1, is.
-  auto step = [&](auto kh_tag, uint32_t v_at, f32x16 (&zn)[2], f32x16 (&zo)[2], u32x4 (&pn)[2][2], const u32x4 (&po)[2][2],
-                  float (&top)[2], int t) BM_LAMBDA {
+  // t - 1's weights, kpre the first operands of half t + 1's logits, raised whether some row's
+  // maximum has to move.  KH: which half of its tile t + 1, and t - 1, is; side(j): what
+  // else goes behind product j.
+  u32x4 kpre[2];
+  bool raised;
+  float top[2] = {kNegInf, kNegInf};
+  auto exceeds = [&]() BM_LAMBDA {
+    return __ballot(top[0] * c2 > m[0] + kRescaleLog2 || top[1] * c2 > m[1] + kRescaleLog2) != 0;
+  };
+  auto step = [&](auto kh_tag, auto side, f32x16 (&zn)[2], f32x16 (&zo)[2], u32x4 (&pn)[2][2],
+                  const u32x4 (&po)[2][2], int t) BM_LAMBDA {
     constexpr int KH = decltype(kh_tag)::value;
     // the maximum a row's weights are taken against; O follows behind this step's product
     float f[2] = {1.0f, 1.0f};
-    const bool raised = __ballot(top[0] * c2 > m[0] + kRescaleLog2 || top[1] * c2 > m[1] + kRescaleLog2) != 0;
-    if (raised) {
+    const bool raise = raised;
+    if (__builtin_expect(raise, 0)) {
 #pragma unroll
       for (int rt = 0; rt < 2; ++rt) {
         const float mn = fmaxf(m[rt], xhalf_max(top[rt]) * c2);
@@ -276,84 +299,84 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) ref[rt] = m[rt] == kNegInf ? 0.0f : m[rt];
 
-    // 2 KK logit products, then 4 MT value products; pairs of weights between them, in three
-    // stages (argument, exp2, sum and packing) so that none waits for the one before
+    // 2 KK logit products, then 4 MT value products, each with its share of the weights behind
+    // it: about as many cycles as the product takes
     constexpr int NQ = 2 * KK, NP = 4 * MT, NS = NQ + NP, kAhead = 2, NB = kAhead + 1;
     u32x4 kf[NB], vf[NB];
+    kf[0] = kpre[0];
+    kf[1] = kpre[1];
     auto k_fetch = [&](int j) BM_LAMBDA { kf[j % NB] = *lds_at<lds_u32x4>(ka[j] + KH * 32 * RB); };
     auto v_fetch = [&](int j) BM_LAMBDA {
-      const uint32_t x = va[j % MT] + v_at + (KH * 32 + 16 * (j / MT)) * RB;
+      const uint32_t x = va[j % MT] + (KH * 32 + 16 * (j / MT)) * RB;
       const bf16v4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_at<lds_bf16v4>(x));
       const bf16v4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_at<lds_bf16v4>(x + 4 * RB));
       const u32x2 y0 = __builtin_bit_cast(u32x2, x0), y1 = __builtin_bit_cast(u32x2, x1);
       vf[j % NB] = u32x4{y0.x, y0.y, y1.x, y1.y};
     };
-    float x[2][2], e[2][2];
+    float x[2], e[2];
     float sum[2] = {0.0f, 0.0f};
-    auto args = [&](int p) BM_LAMBDA {   // pair p: logits 2 p, 2 p + 1 of the lane's 32
-#pragma unroll
-      for (int i = 0; i < 2; ++i) x[p & 1][i] = fmaf(zo[p / 8][2 * (p % 8) + i], c2, -ref[p / 8]);
+    // weight i of the lane's 32, in three stages (argument, exp2, sum and packing) so that
+    // none waits for the one before
+    auto args = [&](int i) BM_LAMBDA { x[i & 1] = fmaf(zo[i / 16][i % 16], c2, -ref[i / 16]); };
+    float even;
+    auto sums = [&](int i) BM_LAMBDA {
+      sum[i / 16] += e[i & 1];
+      if (i & 1) {
+        uint32_t y = pack2(even, e[1]);
+        asm volatile("" : "+v"(y), "+v"(sum[i / 16]));   // (made here, not where the next step uses it)
+        pn[i / 16][(i / 8) & 1][(i / 2) & 3] = y;
+      } else {
+        asm volatile("" : "+v"(sum[i / 16]));
+        even = e[0];
+      }
     };
-    auto exps = [&](int p) BM_LAMBDA {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) e[p & 1][i] = __builtin_amdgcn_exp2f(x[p & 1][i]);
+    auto weight = [&](int i) BM_LAMBDA {
+      const float y = __builtin_amdgcn_exp2f(x[i & 1]);
+      if (i > 0) sums(i - 1);
+      e[i & 1] = y;
+      if (i + 1 < 32) args(i + 1);
     };
-    auto sums = [&](int p) BM_LAMBDA {
-      sum[p / 8] += e[p & 1][0];
-      sum[p / 8] += e[p & 1][1];
-      uint32_t y = pack2(e[p & 1][0], e[p & 1][1]);
-      asm volatile("" : "+v"(y), "+v"(sum[p / 8]));   // (made here, not where the next step uses it)
-      pn[p / 8][(p / 4) & 1][p & 3] = y;
-    };
-    auto pair = [&](int p) BM_LAMBDA {
-      exps(p);
-      if (p > 0) sums(p - 1);
-      if (p + 1 < 16) args(p + 1);
-    };
-#pragma unroll
-    for (int j = 0; j < kAhead; ++j) k_fetch(j);
     args(0);
-#pragma unroll
-    for (int j = 0; j < NQ; ++j) {
-      const int kk = j / 2, rt = j % 2;
-      __builtin_amdgcn_sched_barrier(0);
-      if (kk == 0) mfma_z<true>(zn[rt], kf[kk % NB], qf[rt][kk]);
-      else mfma_z<false>(zn[rt], kf[kk % NB], qf[rt][kk]);
-      __builtin_amdgcn_sched_barrier(0);
-      if (rt == 0) {
-        if (kk + kAhead < KK) k_fetch(kk + kAhead);
-        else v_fetch(kk + kAhead - KK);
-      }
-#pragma unroll
-      for (int p = 0; p < 16; ++p)
-        if (p * NS / 16 == j) pair(p);
-    }
     float nt0[2] = {kNegInf, kNegInf};
-#pragma unroll
-    for (int j = 0; j < NP; ++j) {
-      const int q = j / 2, rt = j % 2, mt = q % MT, s = q / MT;
+    each([&](auto jc) BM_LAMBDA {
+      constexpr int j = decltype(jc)::value;
       __builtin_amdgcn_sched_barrier(0);
-      o[rt][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[q % NB]),
-                                                          __builtin_bit_cast(bf16x8, po[rt][s]), o[rt][mt], 0, 0, 0);
-      __builtin_amdgcn_sched_barrier(0);
-      if (rt == 0 && q + kAhead < NP / 2) v_fetch(q + kAhead);
-#pragma unroll
-      for (int p = 0; p < 16; ++p)
-        if (p * NS / 16 == NQ + j) pair(p);
-      // maxima of the new logits (the last of their products is kWait value products and the
-      // weights between them away)
-      constexpr int kWait = NP / 4, kPer = 16 / (NP - kWait) + (16 % (NP - kWait) != 0);
-#pragma unroll
-      for (int r = 0; r < kPer; ++r) {
-        const int i = (j - kWait) * kPer + r;
-        if (i >= 0 && i < 16) max3(nt0[i / 8], zn[i / 8][2 * (i % 8)], zn[i / 8][2 * (i % 8) + 1]);
+      if constexpr (j < NQ) {
+        constexpr int kk = j / 2, rt = j % 2;
+        if constexpr (kk == 0) mfma_z<true>(zn[rt], kf[kk % NB], qf[rt][kk]);
+        else mfma_z<false>(zn[rt], kf[kk % NB], qf[rt][kk]);
+      } else {
+        constexpr int q = (j - NQ) / 2, rt = j % 2, mt = q % MT, s = q / MT;
+        o[rt][mt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, vf[q % NB]),
+                                                            __builtin_bit_cast(bf16x8, po[rt][s]), o[rt][mt], 0, 0, 0);
       }
-    }
-    sums(15);
+      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (j % 2 == 0) {
+        constexpr int next = j / 2 + kAhead;         // the operand that comes kAhead pairs on
+        if constexpr (next < KK) k_fetch(next);
+        else if constexpr (next < NS / 2) v_fetch(next - KK);
+        else kpre[next - NS / 2] = *lds_at<lds_u32x4>(KH ? ka[next - NS / 2] ^ TILE : ka[next - NS / 2] + 32 * RB);
+      }
+#pragma unroll
+      for (int i = j * 32 / NS; i < (j + 1) * 32 / NS; ++i) weight(i);
+      // maxima of the new logits (the last of their products is kWait value products and the
+      // weights between them away), and whether they matter
+      constexpr int kWait = NP / 4, kMax = NP - kWait - 2;
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (NQ + kWait + i * kMax / 16 == j) max3(nt0[i / 8], zn[i / 8][2 * (i % 8)], zn[i / 8][2 * (i % 8) + 1]);
+      side(jc);
+      if constexpr (j == NS - 2) {
+        top[0] = nt0[0];
+        top[1] = nt0[1];
+        raised = exceeds();
+      }
+    }, std::make_integer_sequence<int, NS>{});
+    sums(31);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) l[rt] += sum[rt];
-    if (__builtin_expect(raised, 0)) {
+    if (__builtin_expect(raise, 0)) {
       asm volatile("" : "+v"(f[0]), "+v"(f[1]));    // (not multiplied by 1 every time)
 #pragma unroll
       for (int rt = 0; rt < 2; ++rt)
@@ -363,14 +386,14 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
           asm volatile("" : "+a"(o[rt][mt]));       // (back in its registers on this path)
         }
     }
-    top[0] = nt0[0];
-    top[1] = nt0[1];
-    if (!plain(t + 1)) hide(zn, top, t + 1);
+    if (!plain(t + 1)) {
+      hide(zn, top, t + 1);
+      raised = exceeds();
+    }
   };
 
   f32x16 za[2], zb[2];
   u32x4 pa[2][2], pb[2][2];
-  float top[2] = {kNegInf, kNegInf};
   // nothing comes before the first half: weights and values of zero
 #pragma unroll
   for (int rt = 0; rt < 2; ++rt)
@@ -394,8 +417,13 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
 #pragma unroll
     for (int r = 0; r < 16; r += 2) max3(top[rt], za[rt][r], za[rt][r + 1]);
   if (!plain(0)) hide(za, top, 0);
+  raised = exceeds();
+#pragma unroll
+  for (int i = 0; i < 2; ++i) kpre[i] = *lds_at<lds_u32x4>(ka[i] + 32 * RB);
   // Tile t's halves: behind the first one K(t) and V(t - 1) are done with, and K(t + 2) and
-  // V(t + 2) take their places; the barrier behind the next tile's first half shows them.
+  // V(t + 2) take their places, copy by copy between the second one's products; the barrier
+  // behind the next tile's first half shows them.  (Past the last tile they are copies of
+  // it into places that nobody reads any more.)
   uint32_t v_at = 4 * TILE;                    // V of tile t - 1
   auto keep_o = [&]() BM_LAMBDA {
     // (O stays in the accumulation registers over the loop)
@@ -406,23 +434,41 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   };
   keep_o();
   for (int t = 0; t < nt; ++t) {
-    step(std::integral_constant<int, 1>{}, v_at, zb, za, pa, pb, top, 2 * t);
+    step(std::integral_constant<int, 1>{}, [](auto) BM_LAMBDA {}, zb, za, pa, pb, 2 * t);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) ka[kk] ^= TILE;
     __syncthreads();
-    if (t + 2 < nt) {
-      store_tile(t, v_at - 2 * TILE);
-      load_tile(min(t + 3, nt - 1));
-    }
-    v_at = v_at == 4 * TILE ? 2 * TILE : v_at + TILE;
     keep_o();
-    step(std::integral_constant<int, 0>{}, v_at, za, zb, pb, pa, top, 2 * t + 1);
+    const uint32_t v_new = v_at - 2 * TILE;
+    const int next = v_at == 4 * TILE ? -2 * TILE : TILE;
+    v_at += next;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt) va[mt] += next;
+    const Run run = run_of(min(t + 3, nt - 1));
+    step(std::integral_constant<int, 0>{},
+         [&](auto jc) BM_LAMBDA {
+           constexpr int j = decltype(jc)::value, EVERY = (2 * KK + 4 * MT) / 16, c = j / EVERY;
+           if constexpr (j % EVERY == 0) {
+             if constexpr (c < NCOPY) store_k(c, t);
+             if constexpr (c >= NCOPY && c < 2 * NCOPY) store_v(c - NCOPY, v_new);
+             if constexpr (c == 2 * NCOPY) {
+               if (__builtin_expect(!run.is, 0)) load_mixed(min(t + 3, nt - 1));
+             }
+             if constexpr (c >= 2 * NCOPY && c < 4 * NCOPY) {
+               if (run.is) {
+                 if constexpr (c < 3 * NCOPY) load_k(run, c - 2 * NCOPY);
+                 else load_v(run, c - 3 * NCOPY);
+               }
+             }
+           }
+         },
+         za, zb, pb, pa, 2 * t + 1);
     keep_o();
   }
   // the last half's values
 #pragma unroll
   for (int q = 0; q < 2 * MT; ++q) {
-    const uint32_t x = va[q % MT] + v_at + (32 + 16 * (q / MT)) * RB;
+    const uint32_t x = va[q % MT] + (32 + 16 * (q / MT)) * RB;
     const bf16v4 x0 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_at<lds_bf16v4>(x));
     const bf16v4 x1 = __builtin_amdgcn_ds_read_tr16_b64_v4bf16(lds_at<lds_bf16v4>(x + 4 * RB));
     const u32x2 y0 = __builtin_bit_cast(u32x2, x0), y1 = __builtin_bit_cast(u32x2, x1);
