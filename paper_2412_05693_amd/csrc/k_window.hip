@@ -52,7 +52,10 @@ __device__ __forceinline__ void put(float* p, float x) { *p = x; }
 constexpr int kPromptRows = 64;              // of a wave
 constexpr int kPromptWaves = 4;
 constexpr int kPromptTile = 64;              // keys
-constexpr float kRescaleLog2 = 8.0f;         // the maximum moves once a logit is 2^8 beyond it
+// A row's weights are taken against a maximum that moves once a logit is 2^24 beyond it: they
+// stay below 2^24 and their sums below 2^40, which float32 and bfloat16 hold as exactly as
+// smaller ones, and O is rescaled next to never (2^8: 15% of the halves of random rows).
+constexpr float kRescaleLog2 = 24.0f;
 
 __device__ __forceinline__ int kappa(int m) { return (m & ~12) | ((m & 4) << 1) | ((m & 8) >> 1); }
 
@@ -98,6 +101,10 @@ __device__ __forceinline__ void z_settled(f32x16 (&z)[2]) {
 __device__ __forceinline__ void max3(float& x, float y, float z) {
   asm volatile("v_max3_f32 %0, %0, %1, %2" : "+v"(x) : "v"(y), "v"(z));
 }
+
+// a barrier for what the workgroup wrote to LDS (__syncthreads would also wait for the rows
+// on their way into registers)
+__device__ __forceinline__ void lds_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
 // f(0), f(1), .. with numbers that are constants
 template <typename F, int... I>
@@ -174,7 +181,7 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   };
   auto load_k = [&](const Run& r, int i) BM_LAMBDA { ks[i] = __builtin_amdgcn_raw_buffer_load_b128(r.k, coff, i * RPC * RB, 0); };
   auto load_v = [&](const Run& r, int i) BM_LAMBDA { vs[i] = __builtin_amdgcn_raw_buffer_load_b128(r.v, coff, i * RPC * RB, 0); };
-  auto load_mixed = [&](int t) BM_LAMBDA {
+  auto load_mixed = [&](u32x4 (&ks)[NCOPY], u32x4 (&vs)[NCOPY], int t) BM_LAMBDA {
     int v0 = t * kPromptTile + crow;
     asm volatile("" : "+v"(v0));      // (nothing of it outside the branch that it is in)
 #pragma unroll
@@ -198,7 +205,11 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   auto store_v = [&](int i, int at) BM_LAMBDA {
     *reinterpret_cast<u32x4*>(vbuf + at + vst + i * RPC * RB) = vs[i];
   };
-  load_mixed(0);
+  // (three tiles' rows and the queries on their way at once: one wait for memory)
+  u32x4 k1[NCOPY], v1[NCOPY], k2[NCOPY], v2[NCOPY];
+  load_mixed(ks, vs, 0);
+  load_mixed(k1, v1, min(1, nt - 1));
+  load_mixed(k2, v2, min(2, nt - 1));
 
   // ---- queries: lane (n, h) holds row n, chunks 2 kk + h ----
   u32x4 qf[2][KK];
@@ -210,14 +221,24 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
     for (int kk = 0; kk < KK; ++kk)
       qf[rt][kk] = *reinterpret_cast<const u32x4*>(q + 16 * (2 * kk + h));
   }
-#pragma nounroll
-  for (int t = 0; t < 2; ++t) {
+  auto store_tile = [&](int t) BM_LAMBDA {
 #pragma unroll
     for (int i = 0; i < NCOPY; ++i) {
       store_k(i, t);
       store_v(i, t * TILE);
     }
-    load_mixed(min(t + 1, nt - 1));
+  };
+  store_tile(0);
+#pragma unroll
+  for (int i = 0; i < NCOPY; ++i) {
+    ks[i] = k1[i];
+    vs[i] = v1[i];
+  }
+  store_tile(1);
+#pragma unroll
+  for (int i = 0; i < NCOPY; ++i) {
+    ks[i] = k2[i];
+    vs[i] = v2[i];
   }
 
   // what a row sees, in key numbers (rows that are no tokens take the nearest one's)
@@ -253,19 +274,22 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
 #pragma unroll
   for (int mt = 0; mt < MT; ++mt) va[mt] = lds0 + 4 * TILE + (uint32_t)(vbase ^ (64 * mt));
 
-  // hide what rows do not see of half t
+  // hide what rows do not see of half t: the row's keys as bits, then two instructions a logit
   auto hide = [&](f32x16 (&z)[2], float (&top)[2], int t) BM_LAMBDA {
-    const int v0 = 32 * t + 8 * h;
+    const int v0 = 32 * t;
+    auto below = [](int x) BM_LAMBDA { return x <= 0 ? 0u : x >= 32 ? ~0u : (1u << x) - 1; };   // keys < x
+    const uint32_t sinks = below(a.sinks - v0);
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) {
-      // (lane half h's keys all have 8 h: it comes off the limits)
-      const int hi = vhi[rt] - v0, low = vhi[rt] - a.window - v0, sk = a.sinks - v0;
+      const uint32_t in = below(vhi[rt] + 1 - v0), old = below(vhi[rt] + 1 - a.window - v0);
+      const uint32_t seen = in & (~old | sinks);
+      const int bits = (int)(seen >> (8 * h));       // lane half h's keys all have 8 h
       top[rt] = kNegInf;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        const int k = key_of(r, 0);
-        z[rt][r] = k <= hi && (k > low || k < sk) ? z[rt][r] : kNegInf;
-        top[rt] = fmaxf(top[rt], z[rt][r]);
+        const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe(bits, key_of(r, 0), 1);   // ~0 or 0
+        z[rt][r] = __uint_as_float((__float_as_uint(z[rt][r]) & keep) | (0xFF800000u & ~keep));
+        if (r & 1) max3(top[rt], z[rt][r - 1], z[rt][r]);
       }
     }
   };
@@ -437,7 +461,7 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
     step(std::integral_constant<int, 1>{}, [](auto) BM_LAMBDA {}, zb, za, pa, pb, 2 * t);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) ka[kk] ^= TILE;
-    __syncthreads();
+    lds_barrier();
     keep_o();
     const uint32_t v_new = v_at - 2 * TILE;
     const int next = v_at == 4 * TILE ? -2 * TILE : TILE;
@@ -452,7 +476,7 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
              if constexpr (c < NCOPY) store_k(c, t);
              if constexpr (c >= NCOPY && c < 2 * NCOPY) store_v(c - NCOPY, v_new);
              if constexpr (c == 2 * NCOPY) {
-               if (__builtin_expect(!run.is, 0)) load_mixed(min(t + 3, nt - 1));
+               if (__builtin_expect(!run.is, 0)) load_mixed(ks, vs, min(t + 3, nt - 1));
              }
              if constexpr (c >= 2 * NCOPY && c < 4 * NCOPY) {
                if (run.is) {
