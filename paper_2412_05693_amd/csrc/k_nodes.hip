@@ -600,14 +600,14 @@ __global__ void __launch_bounds__(256) nodes_join_kernel(NodesArgs a) {
     a.lse[head * a.n + node] = none ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// Workgroups over a unit's entries: as many as leave no compute unit without one, each
-// with at least kMinTiles tiles a wave.
+// Workgroups over a unit's entries: as many as there are compute units for, each with at
+// least kMinTiles tiles a wave (with fewer the joining launch costs more than it spares).
 constexpr int kNodeWorkgroups = 512;
-constexpr int kMinTiles = 4;
+constexpr int kMinTiles = 1;
 int most_splits(int units, const NodePlan& p) {
-  const int base = units * p.row_groups;
-  const int s = base > 0 ? kNodeWorkgroups / base : 1;
-  return s < 1 ? 1 : s > kMaxNodeSplits ? kMaxNodeSplits : s;
+  const int64_t base = (int64_t)units * p.row_groups;
+  const int64_t s = kNodeWorkgroups / base;
+  return s < 1 ? 1 : s > kMaxNodeSplits ? kMaxNodeSplits : (int)s;
 }
 
 template <bool BF16, int D, int RT>
