@@ -535,6 +535,7 @@ int win_prompt(bm_ctx* ctx, int32_t n_tok, const void* q, const void* k, const v
   a.kc = ctx->cache.k;
   a.vc = ctx->cache.v;
   a.pad = ctx->pad;
+  a.part = static_cast<float*>(ctx->cache.work);
   a.seq_ld = seq_ld;
   a.n_heads = ctx->dims.n_heads;
   a.n_kv_heads = ctx->dims.n_kv_heads;
@@ -579,6 +580,7 @@ bm::NodesArgs nodes_args(const bm_ctx* ctx, int32_t n, const int32_t* parent, co
   a.window = ctx->window;
   a.sinks = ctx->sinks;
   a.nsplit = 1;
+  a.chain = 0;
   a.store = 0;
   a.scale_log2 = ctx->sm_scale * 1.4426950408889634f;
   return a;
@@ -589,7 +591,8 @@ bm::NodesArgs nodes_args(const bm_ctx* ctx, int32_t n, const int32_t* parent, co
 BM_EXPORT size_t bm_win_workspace_bytes(const bm_dims* dims) {
   if (check_win(dims, 0) != BM_OK) return 0;
   return bm::nodes_work_bytes(dims->b * dims->n_kv_heads, dims->head_dim,
-                              dims->n_heads / dims->n_kv_heads, 1);
+                              dims->n_heads / dims->n_kv_heads,
+                              dims->block < bm::kShortPrompt ? dims->block : bm::kShortPrompt);
 }
 
 BM_EXPORT int bm_win_validate(const bm_dims* dims, int32_t sinks) {

@@ -185,9 +185,13 @@ struct PromptArgs {
   void* vc;
   const int32_t* pad; // [b] left pad tokens per sample, or null
   int64_t seq_ld;
+  float* part;        // scratch of nodes_work_bytes for up to kShortPrompt nodes
   int n_heads, n_kv_heads, units, window, sinks, t0, n_tok;
   float scale_log2;
 };
+
+// tokens of a prompt that can be taken as the nodes of a chain (BM_DRAFT_MAX at most)
+constexpr int kShortPrompt = 64;
 
 // The n nodes of a tree (one: a token) over a cache: a bounded one of len0 entries
 // (window 0) or a window cache.
@@ -206,6 +210,7 @@ struct NodesArgs {
   int64_t seq_ld;
   int n_heads, n_kv_heads, units, slots, len0, n, next_pos, window, sinks;
   int nsplit;         // workgroups over a unit's entries (set by launch_nodes)
+  int chain;          // each node hangs from the one before it (parent is null)
   int store;          // the node's rows go into the window cache (n == 1)
   float scale_log2;
 };

@@ -61,6 +61,15 @@ __device__ __forceinline__ float add_xor(float v) {
   }
 }
 
+// the largest of the values of the four lanes 16 apart
+__device__ __forceinline__ float max_xor16_32(float v) {
+  uint32_t x = __float_as_uint(v);
+  const auto a = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
+  const auto b = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
 // smallest 64-bit key of the wave (the same steps on both halves of the key)
 __device__ __forceinline__ uint64_t wave_min_u64(uint64_t k) {
   uint32_t lo = (uint32_t)k, hi = (uint32_t)(k >> 32);

@@ -40,10 +40,12 @@ typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 
 constexpr float kNegInf = -__builtin_huge_valf();
-constexpr float kRescaleLog2 = 8.0f;   // the maximum moves once a logit is 2^8 beyond it
+constexpr float kRescaleLog2 = 24.0f;  // the maximum moves once a logit is 2^24 beyond it
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kTile = 32;              // keys
-constexpr int kNodeWaves = 8;
+// Waves of a workgroup: two a SIMD where 256 registers hold one's tile, otherwise one.
+constexpr bool big_wave(bool bf16, int d, int rt) { return bf16 ? rt > 1 : d == 128; }
+constexpr int node_waves(bool bf16, int d, int rt) { return big_wave(bf16, d, rt) ? 4 : 8; }
 constexpr int kMaxNodeSplits = 64;     // a lane of the joining wave each
 constexpr int kNoWindow = 0x7FFFFFFF;
 
@@ -56,13 +58,6 @@ struct NodeCfg {
   static constexpr int VW = EPL * (int)sizeof(E) / 4;  // ... and words
 };
 
-__device__ __forceinline__ float xmax4(float x) {   // over the lanes 16 apart
-  uint32_t y = __float_as_uint(x);
-  const auto a = __builtin_amdgcn_permlane16_swap(y, y, false, false);
-  y = __float_as_uint(fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1])));
-  const auto b = __builtin_amdgcn_permlane32_swap(y, y, false, false);
-  return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-}
 __device__ __forceinline__ float xsum4(float x) { return lanes::add_xor<32>(lanes::add_xor<16>(x)); }
 
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
@@ -88,7 +83,7 @@ __device__ __forceinline__ uint64_t shfl64(uint64_t x, int lane) {
 
 // Ancestors by doubling the step up the tree; then the nodes that a window or a left pad
 // hides (r0: the index of a root, below 0 where the sample has not begun).
-__device__ __forceinline__ Tree make_tree(const int32_t* parent, int n, int r0, int sinks, int window) {
+__device__ __forceinline__ Tree make_tree(const int32_t* parent, bool chain, int n, int r0, int sinks, int window) {
   const int a = threadIdx.x & 63;
   int up = -1;
   if (parent && a < n) {
@@ -96,7 +91,7 @@ __device__ __forceinline__ Tree make_tree(const int32_t* parent, int n, int r0, 
     if (up < 0 || up >= a) up = -1;
   }
   Tree t;
-  t.sees = 1ull << a;
+  t.sees = chain ? (2ull << a) - 1 : 1ull << a;    // (2 << 63 is 0)
   while (__ballot(up >= 0) != 0) {
     const uint64_t more = shfl64(t.sees, max(up, 0));
     const int next = __shfl(up, max(up, 0));
@@ -117,32 +112,63 @@ __device__ __forceinline__ Tree make_tree(const int32_t* parent, int n, int r0, 
 
 // Work of a launch over the waves: rows of 16 RT, and what is left over the keys.
 struct NodePlan {
+  int waves;       // of a workgroup
   int rt;          // row tiles of a wave
   int row_waves;   // waves of a workgroup over different rows
   int row_groups;  // workgroups over different rows of a unit
-  int key_waves() const { return kNodeWaves / row_waves; }
+  int key_waves() const { return waves / row_waves; }
 };
 
-NodePlan plan_of(int rows, bool bf16) {
+// Waves of 64 rows read the keys from the caches half as often as those of 32, and are half as
+// many: they pay once the launch has work for all compute units.  us with 32 -> 64 rows, 8 KV
+// heads, four query heads each, d = 128:
+//   units rows entries  8 128 512    8 256 4096   64 128 512   64 128 4096  512 64 512   512 64 4096
+//                       21.8 -> 23.5 36.7 -> 43.6 27.6 -> 30.8 60.1 -> 51.4 41.0 -> 48.2 237 -> 199
+//                       512 128 512  512 128 4096 512 256 512  512 256 4096
+//                       61.0 -> 59.0 413 -> 291   128 -> 92    833 -> 506
+constexpr int64_t kBigWork = 1 << 25;       // units x rows x entries
+NodePlan plan_of(int rows, bool bf16, int d, bool big) {
   NodePlan p;
-  p.rt = bf16 && rows > 16 ? 2 : 1;
+  p.rt = !bf16 || rows <= 16 ? 1 : rows <= 32 || !big ? 2 : 4;
+  p.waves = node_waves(bf16, d, p.rt);
   const int blocks = (rows + 16 * p.rt - 1) / (16 * p.rt);
   p.row_waves = 1;
-  while (p.row_waves < blocks && p.row_waves < kNodeWaves) p.row_waves *= 2;
+  while (p.row_waves < blocks && p.row_waves < p.waves) p.row_waves *= 2;
   p.row_groups = (blocks + p.row_waves - 1) / p.row_waves;
   return p;
 }
 
+// z = or += K Q^T of a 16 x 16 tile of bfloat16, for waves of 32 and 64 rows.  As assembly: for a
+// kernel of more than 256 registers the compiler puts every product's result into the
+// accumulation registers, from which each logit would have to be copied before a vector
+// instruction could use it.  The compiler does not count the wait states until such an
+// instruction may read the result either: s_settled does.
+template <bool FIRST>
+__device__ __forceinline__ void mfma_s(f32x4& z, u32x4 k, u32x4 q) {
+  if constexpr (FIRST)
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, 0" : "=&v"(z) : "v"(k), "a"(q));
+  else
+    asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+&v"(z) : "v"(k), "a"(q));
+}
+template <int RT>
+__device__ __forceinline__ void s_settled(f32x4 (&s)[RT][2]) {
+  asm volatile("s_nop 15" ::: "memory");
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) asm volatile("" : "+v"(s[rt][0]), "+v"(s[rt][1]));
+}
+
 template <bool BF16, int D, int RT>
-__global__ void __launch_bounds__(64 * kNodeWaves, 1) nodes_kernel(NodesArgs a, int row_waves) {
+__global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(NodesArgs a, int row_waves) {
+  constexpr int kNodeWaves = node_waves(BF16, D, RT);
+  constexpr bool kBig = big_wave(BF16, D, RT);
   using C = NodeCfg<BF16, D>;
   using E = typename C::E;
   constexpr int RB = C::RB, KL = C::KL, EPL = C::EPL, VW = C::VW;
-  constexpr int OREGS = 4 * EPL;                       // output values of a lane and row tile
-  // joins: half of the waves hand over O, m and l; rows of a wave's weights (see patch)
-  constexpr int JOIN = RT * (OREGS + 2) * 64;
-  __shared__ float lds[(kNodeWaves / 2) * JOIN > kNodeWaves * 512 * RT ? (kNodeWaves / 2) * JOIN
-                                                                     : kNodeWaves * 512 * RT];
+  // a wave's part of LDS: O in quads of elements, m and l, for the join; the weights of a tile
+  // of 32 keys (see the end of a tile) for a moment before
+  constexpr int QUADS = EPL, PART = RT * (QUADS * 256 + 128);
+  static_assert(QUADS * 256 >= 512, "weights of 32 keys and 16 rows");
+  __shared__ __attribute__((aligned(16))) float lds[kNodeWaves * PART];
   const int group = a.n_heads / a.n_kv_heads, rows = group * a.n;
   const int u = blockIdx.x, split = blockIdx.y;
   const int bi = u / a.n_kv_heads, hk = u - bi * a.n_kv_heads;
@@ -155,11 +181,11 @@ __global__ void __launch_bounds__(64 * kNodeWaves, 1) nodes_kernel(NodesArgs a, 
   const Ring ring(r0, a.sinks, max(a.window, 1));
   const int entries = a.window ? ring.filled() : a.len0;
 
-  // ---- the workgroup's tiles: its share of the cached ones and, in the last share, the nodes' ----
-  const int tiles = (entries + kTile - 1) / kTile;
-  const int per = (tiles + a.nsplit - 1) / a.nsplit;
-  const int lo = min(split * per, tiles), cached = min(tiles - lo, per);
-  const int total = cached + (split == a.nsplit - 1 ? (a.n + kTile - 1) / kTile : 0);
+  // ---- the workgroup's tiles: its share of the cached ones with the nodes' behind them ----
+  const int tiles = (entries + kTile - 1) / kTile, all = tiles + (a.n + kTile - 1) / kTile;
+  const int per = (all + a.nsplit - 1) / a.nsplit;
+  const int lo = min(split * per, all), total = min(per, all - lo);
+  const int cached = min(max(tiles - lo, 0), total), node0 = tiles - lo;   // tile node0 is the first of the nodes
 
   const char* kc = static_cast<const char*>(a.kc) + (int64_t)u * a.slots * RB;
   const char* vc = static_cast<const char*>(a.vc) + (int64_t)u * a.slots * RB;
@@ -172,7 +198,7 @@ __global__ void __launch_bounds__(64 * kNodeWaves, 1) nodes_kernel(NodesArgs a, 
   int pk = 0;           // the position of key (lane & 31) of the tile (left padding)
   auto load_k = [&](int t) BM_LAMBDA {
     const bool node = t >= cached;
-    const int base = (node ? t - cached : lo + t) * kTile;
+    const int base = (node ? t - node0 : lo + t) * kTile;
     const auto r = rows_of(node ? kin : kc, (node ? a.n : entries) * RB);
 #pragma unroll
     for (int s = 0; s < 2; ++s)
@@ -183,7 +209,7 @@ __global__ void __launch_bounds__(64 * kNodeWaves, 1) nodes_kernel(NodesArgs a, 
   };
   auto load_v = [&](int t) BM_LAMBDA {
     const bool node = t >= cached;
-    const int base = (node ? t - cached : lo + t) * kTile;
+    const int base = (node ? t - node0 : lo + t) * kTile;
     const auto r = rows_of(node ? vin : vc, (node ? a.n : entries) * RB);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -220,7 +246,7 @@ __global__ void __launch_bounds__(64 * kNodeWaves, 1) nodes_kernel(NodesArgs a, 
     for (int kk = 0; kk < KL; ++kk)
       qf[rt][kk] = *reinterpret_cast<const u32x4*>(q + 16 * h + 64 * kk);
   }
-  const Tree tree = make_tree(a.parent ? a.parent + (int64_t)bi * a.n : nullptr, a.n, r0, a.sinks,
+  const Tree tree = make_tree(a.parent ? a.parent + (int64_t)bi * a.n : nullptr, a.chain != 0, a.n, r0, a.sinks,
                               a.window ? a.window : kNoWindow);
   uint64_t sees[RT];
   int depth[RT];
@@ -230,14 +256,27 @@ __global__ void __launch_bounds__(64 * kNodeWaves, 1) nodes_kernel(NodesArgs a, 
     sees[rt] = shfl64(tree.sees, node);
     depth[rt] = __shfl(tree.depth, node);
   }
-  // entries that the window hides from the deepest node: those of index <= edge
-  const bool nested = __ballot((threadIdx.x & 63) < a.n && tree.depth > 0) != 0;
-  int deepest = 0;
+  // The entries that the window hides from the deepest node: `old` slots from `oldest` on, going
+  // round behind the ring's last one.  Where all nodes are roots nobody sees them; otherwise
+  // the deeper ones do not.
+  const bool nested = __ballot(lane < a.n && tree.depth > 0) != 0;
+  int oldest = 0, old = 0;
   if (a.window) {
-    deepest = (threadIdx.x & 63) < a.n ? tree.depth : 0;
+    int deepest = lane < a.n ? tree.depth : 0;
 #pragma unroll
     for (int off = 32; off; off >>= 1) deepest = max(deepest, __shfl_xor(deepest, off));
+    deepest = __builtin_amdgcn_readfirstlane(deepest);
+    const bool full = r0 >= a.sinks + a.window;
+    oldest = a.sinks + (full ? (ring.last + 1) % a.window : 0);
+    old = min(full ? deepest + 1 : max(r0 - a.window + deepest - a.sinks + 1, 0), a.window);
   }
+  const int old_end = min(oldest + old, a.slots), wrapped = a.sinks + oldest + old - a.slots;   // slots behind the ring's start
+  auto has_old = [&](int base) BM_LAMBDA {
+    return old > 0 && ((base < old_end && base + kTile > oldest) || (base < wrapped && base + kTile > a.sinks));
+  };
+  auto is_old = [&](int slot) BM_LAMBDA {
+    return (slot >= oldest && slot < old_end) || (slot >= a.sinks && slot < wrapped);
+  };
 
   if (a.store && split == 0 && blockIdx.z == 0 && r0 >= 0) {
     // the token's own rows into its slot, which nobody sees in this call
@@ -262,22 +301,39 @@ __global__ void __launch_bounds__(64 * kNodeWaves, 1) nodes_kernel(NodesArgs a, 
   }
   const float c2 = a.scale_log2;
 
-  for (int t = kw; t < total; t += key_waves) {
-    const bool node = t >= cached;
-    const int base = (node ? t - cached : lo + t) * kTile;
+  auto keep_acc = [&]() BM_LAMBDA {
+    // (O stays in the accumulation registers over the loops)
+    if constexpr (kBig) {
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) asm volatile("" : "+a"(acc[rt][e]));
+    }
+  };
+  // Tile t.  MIXED: rows see different keys of it (the nodes, and entries at the window's edge);
+  // otherwise they all see the same ones.
+  auto tile = [&](auto mixed_tag, int t) BM_LAMBDA {
+    constexpr bool MIXED = decltype(mixed_tag)::value;
+    const bool node = MIXED && t >= cached;
+    const int base = (node ? t - node0 : lo + t) * kTile;
     // ---- logits ----
     f32x4 s[RT][2];
+    if constexpr (!(BF16 && kBig)) {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+      for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-      for (int x = 0; x < 2; ++x) s[rt][x] = f32x4{0, 0, 0, 0};
+        for (int x = 0; x < 2; ++x) s[rt][x] = f32x4{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int kk = 0; kk < KL; ++kk)
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-          if constexpr (BF16) {
+          if constexpr (BF16 && kBig) {
+            if (kk == 0) mfma_s<true>(s[rt][x], kf[x][kk], qf[rt][kk]);
+            else mfma_s<false>(s[rt][x], kf[x][kk], qf[rt][kk]);
+          } else if constexpr (BF16) {
             s[rt][x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, kf[x][kk]),
                                                                __builtin_bit_cast(bf16x8, qf[rt][kk]), s[rt][x], 0, 0, 0);
           } else {
@@ -287,112 +343,96 @@ __global__ void __launch_bounds__(64 * kNodeWaves, 1) nodes_kernel(NodesArgs a, 
                                                               __uint_as_float(qf[rt][kk][j]), s[rt][x], 0, 0, 0);
           }
         }
+    const int pk0 = pk;
+    load_k(t + key_waves);
+    if constexpr (BF16 && kBig) s_settled(s);
 
-    // ---- who sees what.  Keys that nobody sees: bit k of `gone`; keys that some rows see
-    //      and others do not (`mixed`): dist, their index less that of the oldest one a
-    //      root does not see, against the row's depth, or the tree's bits ----
+    // ---- keys that nobody sees: bit k of `gone`; V rows of theirs become zeros, so that a
+    //      NaN there does not count either ----
     uint32_t gone = 0;
-    bool mixed = node;
-    int dist[8];
-    if (!node) {
-      const int k32 = lane & 31, slot = base + k32;
-      bool out = slot >= entries;
-      if (pos && pad > 0) out = out || pk < pad;
-      if (a.window) {
-        const int j = ring.index(min(slot, a.slots - 1));
-        const bool old = slot >= a.sinks && j - (r0 - a.window) <= deepest;
-        if (nested)
-          mixed = __ballot(old && !out) != 0;
-        else
-          out = out || old;
-      }
-      gone = (uint32_t)__ballot(out);
-      if (mixed) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int sl = base + 16 * (i >> 2) + 4 * h + (i & 3);
-          dist[i] = sl < a.sinks ? kNoWindow : ring.index(min(sl, a.slots - 1)) - (r0 - a.window);
-        }
-      }
-    } else {
+    if (node) {
       gone = base + kTile > a.n ? ~0u << (a.n - base) : 0;
+    } else if (base + kTile > entries || (pos && pad > 0) || (!nested && has_old(base))) {
+      const int slot = base + (lane & 31);
+      gone = (uint32_t)__ballot(slot >= entries || (pos && pad > 0 && pk0 < pad) || (!nested && is_old(slot)));
     }
     const uint32_t hide = gone >> (4 * h);               // bit 16 t + r: this lane's key (t, r)
-    uint32_t mask[RT];                                   // ... as each row sees it
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      mask[rt] = hide;
-      if (mixed) {
-        if (node) {
-          mask[rt] |= (uint32_t)~(sees[rt] >> base) >> (4 * h);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (dist[i] <= depth[rt]) mask[rt] |= 1u << (16 * (i >> 2) + (i & 3));
-        }
-      }
-    }
-
-    // (float32 rows of 128: K and V together leave no registers to load ahead)
-    constexpr bool kAhead = BF16 || D == 64;
-    if constexpr (kAhead) load_k(t + key_waves);
-
-    // ---- softmax ----
-    uint32_t phi[RT][4], plo[RT][4];                     // bfloat16 weights, two parts
-    float pw[RT][8];
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      float z[8], top = kNegInf;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) z[i] = s[rt][i >> 2][i & 3];
-      if (gone != 0 || mixed) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          if ((mask[rt] >> (16 * (i >> 2) + (i & 3))) & 1) z[i] = kNegInf;
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, z[i]);
-      if (__ballot(top * c2 > m[rt] + kRescaleLog2) != 0) {
-        const float mn = fmaxf(m[rt], xmax4(top) * c2);
-        // (a row that has seen no key yet: nothing to scale)
-        const float f = mn == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - mn);
-        m[rt] = mn;
-        l[rt] *= f;
-#pragma unroll
-        for (int e = 0; e < EPL; ++e) acc[rt][e] *= f;
-      }
-      const float ref = m[rt] == kNegInf ? 0.0f : m[rt];
-      float sum = 0.0f;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        pw[rt][i] = __builtin_amdgcn_exp2f(fmaf(z[i], c2, -ref));
-        sum += pw[rt][i];
-      }
-      l[rt] += sum;
-      if constexpr (BF16) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t hi = pack2(pw[rt][2 * i], pw[rt][2 * i + 1]);
-          phi[rt][i] = hi;
-          plo[rt][i] = pack2(pw[rt][2 * i] - __uint_as_float(hi << 16),
-                             pw[rt][2 * i + 1] - __uint_as_float(hi & 0xFFFF0000u));
-        }
-      }
-    }
-
-    // ---- V rows that weigh nothing for a row must not reach it, NaN and infinities
-    //      included: those nobody sees become zeros; where rows differ, a row with such a
-    //      value becomes zeros too and is added to the rows that see it one by one ----
-    uint32_t bad = 0;
     if (gone != 0) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const bool z = (hide >> (16 * (i >> 2) + (i & 3))) & 1;
 #pragma unroll
         for (int w = 0; w < VW; ++w) vf[i][w] = z ? 0u : vf[i][w];
+        if constexpr (!MIXED) {
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) s[rt][i >> 2][i & 3] = z ? kNegInf : s[rt][i >> 2][i & 3];
+        }
       }
     }
-    if (mixed) {
+    // ... and what each row does not see: by the tree, or by the index of an entry less that
+    // of the oldest one a root does not see, against the row's depth
+    uint32_t mask[RT];
+    if constexpr (MIXED) {
+      int dist[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int slot = base + 16 * (i >> 2) + 4 * h + (i & 3);
+        dist[i] = node || slot < a.sinks ? kNoWindow : ring.index(min(slot, a.slots - 1)) - (r0 - a.window);
+      }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        mask[rt] = hide | (node ? (uint32_t)~(sees[rt] >> base) >> (4 * h) : 0u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (dist[i] <= depth[rt]) mask[rt] |= 1u << (16 * (i >> 2) + (i & 3));
+          if ((mask[rt] >> (16 * (i >> 2) + (i & 3))) & 1) s[rt][i >> 2][i & 3] = kNegInf;
+        }
+      }
+    }
+
+    // ---- softmax ----
+    uint32_t phi[RT][4], plo[RT][4];                     // bfloat16 weights, two parts
+    float pf[BF16 ? 1 : RT][8];                          // float32 weights
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      float top = kNegInf;
+      float(&pw)[8] = pf[BF16 ? 0 : rt];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) top = fmaxf(top, s[rt][i >> 2][i & 3]);
+      if (__builtin_expect(__ballot(top * c2 > m[rt] + kRescaleLog2) != 0, 0)) {
+        const float mn = fmaxf(m[rt], lanes::max_xor16_32(top) * c2);
+        // (a row that has seen no key yet: nothing to scale)
+        const float f = mn == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - mn);
+        m[rt] = mn;
+        l[rt] *= f;
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) {
+          acc[rt][e] *= f;
+          if constexpr (kBig) asm volatile("" : "+a"(acc[rt][e]));   // (back in its registers on this path)
+        }
+      }
+      const float ref = m[rt] == kNegInf ? 0.0f : m[rt];
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        pw[i] = __builtin_amdgcn_exp2f(fmaf(s[rt][i >> 2][i & 3], c2, -ref));
+        sum += pw[i];
+      }
+      l[rt] += sum;
+      if constexpr (BF16) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t hi = pack2(pw[2 * i], pw[2 * i + 1]);
+          phi[rt][i] = hi;
+          plo[rt][i] = pack2(pw[2 * i] - __uint_as_float(hi << 16), pw[2 * i + 1] - __uint_as_float(hi & 0xFFFF0000u));
+        }
+      }
+    }
+
+    // ---- MIXED: a V row with an infinity or a NaN becomes zeros too, and is added below to
+    //      the rows that see it, one by one ----
+    uint32_t bad = 0;
+    if constexpr (MIXED) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         bool b = false;
@@ -430,13 +470,14 @@ __global__ void __launch_bounds__(64 * kNodeWaves, 1) nodes_kernel(NodesArgs a, 
 #pragma unroll
       for (int e = 0; e < EPL; ++e)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          const bf16x8 v8 = __builtin_bit_cast(bf16x8, vt[e]);
-          const u32x4 ph = {phi[rt][0], phi[rt][1], phi[rt][2], phi[rt][3]};
-          const u32x4 pl = {plo[rt][0], plo[rt][1], plo[rt][2], plo[rt][3]};
-          acc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, __builtin_bit_cast(bf16x8, ph), acc[rt][e], 0, 0, 0);
-          acc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8, __builtin_bit_cast(bf16x8, pl), acc[rt][e], 0, 0, 0);
-        }
+        for (int part = 0; part < 2; ++part)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            const uint32_t(&p)[4] = part ? plo[rt] : phi[rt];
+            acc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt[e]),
+                                                                 __builtin_bit_cast(bf16x8, u32x4{p[0], p[1], p[2], p[3]}),
+                                                                 acc[rt][e], 0, 0, 0);
+          }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i)
@@ -444,118 +485,145 @@ __global__ void __launch_bounds__(64 * kNodeWaves, 1) nodes_kernel(NodesArgs a, 
         for (int e = 0; e < EPL; ++e)
 #pragma unroll
           for (int rt = 0; rt < RT; ++rt)
-            acc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[i][e]), pw[rt][i], acc[rt][e], 0, 0, 0);
+            acc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vf[i][e]), pf[rt][i], acc[rt][e], 0, 0, 0);
       load_v(t + key_waves);
     }
 
     // ---- the rows taken out above, for those that see them ----
-    if (bad != 0) {
-      float* w = lds + wave * 512 * RT;                  // weights [RT][32 keys][16 rows], < 0: hidden
+    if constexpr (MIXED) {
+      if (__builtin_expect(bad != 0, 0)) {
+        float* w = lds + wave * PART;                // weights [RT][32 keys][16 rows], < 0: hidden
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+        for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int key = 16 * (i >> 2) + 4 * h + (i & 3);
-          w[(rt * 32 + key) * 16 + i16] = (mask[rt] >> (16 * (i >> 2) + (i & 3))) & 1 ? -1.0f : pw[rt][i];
-        }
-      // (a wave's own LDS writes are in order with its reads)
-      __builtin_amdgcn_wave_barrier();
-      const E* src = reinterpret_cast<const E*>(node ? vin : vc);
-      for (uint32_t left = bad; left != 0; left &= left - 1) {
-        const int key = __builtin_ctz(left);
-        const E* v = src + (int64_t)(base + key) * D + 4 * EPL * h;
+          for (int i = 0; i < 8; ++i) {
+            const int key = 16 * (i >> 2) + 4 * h + (i & 3);
+            float p;
+            if constexpr (BF16) {
+              const uint32_t x = phi[rt][i >> 1], y = plo[rt][i >> 1];
+              p = i & 1 ? __uint_as_float(x & 0xFFFF0000u) + __uint_as_float(y & 0xFFFF0000u)
+                        : __uint_as_float(x << 16) + __uint_as_float(y << 16);
+            } else {
+              p = pf[rt][i];
+            }
+            w[(rt * 32 + key) * 16 + i16] = (mask[rt] >> (16 * (i >> 2) + (i & 3))) & 1 ? -1.0f : p;
+          }
+        // (a wave's own LDS writes are in order with its reads)
+        __builtin_amdgcn_wave_barrier();
+        const E* src = reinterpret_cast<const E*>(node ? vin : vc);
+        for (uint32_t left = bad; left != 0; left &= left - 1) {
+          const int key = __builtin_ctz(left);
+          const E* v = src + (int64_t)(base + key) * D + 4 * EPL * h;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          const float p = w[(rt * 32 + key) * 16 + i16];
-          if (p >= 0.0f) {
+          for (int rt = 0; rt < RT; ++rt) {
+            const float p = w[(rt * 32 + key) * 16 + i16];
+            if (p >= 0.0f) {
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
+              for (int x = 0; x < 4; ++x)
 #pragma unroll
-              for (int e = 0; e < EPL; ++e) {
-                float f;
-                if constexpr (BF16) f = __uint_as_float((uint32_t)v[EPL * x + e] << 16);
-                else f = v[EPL * x + e];
-                acc[rt][e][x] += p * f;
-              }
+                for (int e = 0; e < EPL; ++e) {
+                  float f;
+                  if constexpr (BF16) f = __uint_as_float((uint32_t)v[EPL * x + e] << 16);
+                  else f = v[EPL * x + e];
+                  acc[rt][e][x] += p * f;
+                }
+            }
           }
         }
+        __builtin_amdgcn_wave_barrier();
       }
-      __builtin_amdgcn_wave_barrier();
+      keep_acc();
     }
-    if constexpr (!kAhead) load_k(t + key_waves);
+  };
+  keep_acc();
+  for (int t = kw; t < total;) {
+    for (; t < cached && !(nested && has_old((lo + t) * kTile)); t += key_waves) {
+      tile(std::false_type{}, t);
+      keep_acc();
+    }
+    if (t < total) {
+      tile(std::true_type{}, t);
+      t += key_waves;
+    }
   }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) l[rt] = xsum4(l[rt]);
 
-  // ---- join the waves over the same rows, half of them handing over at a time ----
-  for (int half = key_waves >> 1; half > 0; half >>= 1) {
-    __syncthreads();
-    float* x = lds + (rw * half + (kw & (half - 1))) * JOIN + lane;
-    if (kw >= half && kw < 2 * half) {
+  // ---- join the waves over the same rows, and the results: lane (i16, h) holds elements
+  //      4 EPL h .. of row i16, EPL of them for each x; the waves take turns by (rt, x) ----
+  float* part = lds + (wave - kw) * PART;                // of the first wave over these rows
+  if (key_waves > 1) {
+    float* mine = lds + wave * PART;
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        float* y = x + rt * (OREGS + 2) * 64;
-#pragma unroll
-        for (int i = 0; i < OREGS; ++i) y[i * 64] = acc[rt][i >> 2][i & 3];
-        y[OREGS * 64] = m[rt];
-        y[(OREGS + 1) * 64] = l[rt];
-      }
-    }
-    __syncthreads();
-    if (kw < half) {
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const float* y = x + rt * (OREGS + 2) * 64;
-        const float mo = y[OREGS * 64], mn = fmaxf(m[rt], mo);
-        const float f = m[rt] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m[rt] - mn);
-        const float fo = mo == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(mo - mn);
-        m[rt] = mn;
-        l[rt] = l[rt] * f + y[(OREGS + 1) * 64] * fo;
-#pragma unroll
-        for (int i = 0; i < OREGS; ++i) acc[rt][i >> 2][i & 3] = acc[rt][i >> 2][i & 3] * f + y[i * 64] * fo;
-      }
-    }
-  }
-  if (kw != 0) return;
-
-  // ---- results: lane (i16, h) holds elements 4 EPL h .. of row i16 ----
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    if (row[rt] >= rows) continue;
-    if (a.nsplit > 1) {
-      const int64_t at = ((int64_t)u * a.nsplit + split) * rows + row[rt];
-      float* o = a.part + at * D + 4 * EPL * h;
+    for (int rt = 0; rt < RT; ++rt) {
+      float* y = mine + rt * (QUADS * 256 + 128);
 #pragma unroll
       for (int x = 0; x < 4; ++x)
 #pragma unroll
         for (int e = 0; e < EPL; e += 4)
-          *reinterpret_cast<f32x4*>(o + EPL * x + e) =
+          *reinterpret_cast<f32x4*>(y + ((x * EPL + e) / 4 * 64 + lane) * 4) =
               f32x4{acc[rt][e][x], acc[rt][e + 1][x], acc[rt][e + 2][x], acc[rt][e + 3][x]};
-      if (h == 0) {
-        float* ml = a.part + (int64_t)a.units * a.nsplit * rows * D + at * 2;
-        ml[0] = m[rt];
-        ml[1] = l[rt];
+      y[QUADS * 256 + lane] = m[rt];
+      y[QUADS * 256 + 64 + lane] = l[rt];
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    if (row[rt] >= rows) continue;
+    float f[kNodeWaves], mx = m[rt], sum = l[rt];
+    if (key_waves > 1) {
+      const float* y = part + rt * (QUADS * 256 + 128) + QUADS * 256 + lane;
+      mx = kNegInf;
+      for (int j = 0; j < key_waves; ++j) mx = fmaxf(mx, y[j * PART]);
+      sum = 0.0f;
+#pragma unroll
+      for (int j = 0; j < kNodeWaves; ++j) {
+        f[j] = 0.0f;
+        if (j < key_waves) {
+          const float mj = y[j * PART];
+          f[j] = mj == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(mj - mx);
+          sum = fmaf(f[j], y[j * PART + 64], sum);
+        }
       }
-      continue;
     }
     const int g = row[rt] / a.n, node = row[rt] - g * a.n;
     const int64_t head = (int64_t)bi * a.n_heads + hk * group + g;
+    const int64_t at = ((int64_t)u * a.nsplit + split) * rows + row[rt];
     const bool none = r0 + depth[rt] < 0;                // a pad token: it sees nothing
-    const float inv = none ? 0.0f : 1.0f / l[rt];
-    E* o = static_cast<E*>(a.o) + (head * a.seq_ld + node) * D + 4 * EPL * h;
+    const float inv = a.nsplit > 1 ? 1.0f : none ? 0.0f : 1.0f / sum;
 #pragma unroll
-    for (int x = 0; x < 4; ++x)
+    for (int x = 0; x < 4; ++x) {
+      if (((4 * rt + x) & (key_waves - 1)) != kw) continue;
 #pragma unroll
       for (int e = 0; e < EPL; e += 4) {
-        f32x4 y = {acc[rt][e][x], acc[rt][e + 1][x], acc[rt][e + 2][x], acc[rt][e + 3][x]};
-        y = none ? f32x4{0, 0, 0, 0} : y * inv;
-        if constexpr (BF16)
-          *reinterpret_cast<u32x2*>(o + EPL * x + e) = u32x2{pack2(y.x, y.y), pack2(y.z, y.w)};
-        else
-          *reinterpret_cast<f32x4*>(o + EPL * x + e) = y;
+        f32x4 o = {acc[rt][e][x], acc[rt][e + 1][x], acc[rt][e + 2][x], acc[rt][e + 3][x]};
+        if (key_waves > 1) {
+          o = f32x4{0, 0, 0, 0};
+          const float* y = part + rt * (QUADS * 256 + 128) + ((x * EPL + e) / 4 * 64 + lane) * 4;
+#pragma unroll
+          for (int j = 0; j < kNodeWaves; ++j)
+            if (j < key_waves) o += f[j] * *reinterpret_cast<const f32x4*>(y + j * PART);
+        }
+        if (a.nsplit > 1) {
+          *reinterpret_cast<f32x4*>(a.part + at * D + 4 * EPL * h + EPL * x + e) = o;
+          continue;
+        }
+        o = none ? f32x4{0, 0, 0, 0} : o * inv;
+        E* dst = static_cast<E*>(a.o) + (head * a.seq_ld + node) * D + 4 * EPL * h + EPL * x + e;
+        if constexpr (BF16) *reinterpret_cast<u32x2*>(dst) = u32x2{pack2(o.x, o.y), pack2(o.z, o.w)};
+        else *reinterpret_cast<f32x4*>(dst) = o;
       }
-    if (a.lse && h == 0)
-      a.lse[head * a.n + node] = none ? kNegInf : (m[rt] + __builtin_amdgcn_logf(l[rt])) * kLn2;
+    }
+    if (h == 0 && kw == 0) {
+      if (a.nsplit > 1) {
+        float* ml = a.part + (int64_t)a.units * a.nsplit * rows * D + at * 2;
+        ml[0] = mx;
+        ml[1] = sum;
+      } else if (a.lse) {
+        a.lse[head * a.n + node] = none ? kNegInf : (mx + __builtin_amdgcn_logf(sum)) * kLn2;
+      }
+    }
   }
 }
 
@@ -582,11 +650,21 @@ __global__ void __launch_bounds__(256) nodes_join_kernel(NodesArgs a) {
   const float f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
   const float sum = lanes::wave_sum(f * l);
   float o[P] = {};
-  for (int c = 0; c < a.nsplit; ++c) {
-    const float fc = __shfl(f, c);
-    const float* x = a.part + (first + (int64_t)c * rows) * D + lane * P;
+  // (eight parts on their way at a time; past the last one its own again, without weight)
+  for (int c0 = 0; c0 < a.nsplit; c0 += 8) {
+    float x[8][P];
 #pragma unroll
-    for (int e = 0; e < P; ++e) o[e] = fmaf(fc, x[e], o[e]);
+    for (int c = 0; c < 8; ++c) {
+      const float* y = a.part + (first + (int64_t)min(c0 + c, a.nsplit - 1) * rows) * D + lane * P;
+#pragma unroll
+      for (int e = 0; e < P; ++e) x[c][e] = y[e];
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const float fc = c0 + c < a.nsplit ? __shfl(f, c0 + c) : 0.0f;
+#pragma unroll
+      for (int e = 0; e < P; ++e) o[e] = fmaf(fc, x[c][e], o[e]);
+    }
   }
   const int64_t head = (int64_t)(u / a.n_kv_heads) * a.n_heads + (u % a.n_kv_heads) * group + g;
   E* dst = static_cast<E*>(a.o) + (head * a.seq_ld + node) * D + lane * P;
@@ -600,23 +678,25 @@ __global__ void __launch_bounds__(256) nodes_join_kernel(NodesArgs a) {
     a.lse[head * a.n + node] = none ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
-// Workgroups over a unit's entries: as many as there are compute units for, each with at
-// least kMinTiles tiles a wave (with fewer the joining launch costs more than it spares).
-constexpr int kNodeWorkgroups = 512;
-constexpr int kMinTiles = 1;
-int most_splits(int units, const NodePlan& p) {
-  const int64_t base = (int64_t)units * p.row_groups;
-  const int64_t s = kNodeWorkgroups / base;
+// Workgroups over a unit's entries: what fills the compute units, one workgroup each, with at
+// least one tile a wave, and as many rows of partial results as the joining launch reads
+// in a few microseconds.
+constexpr int kNodeWorkgroups = 256;
+constexpr int kMostPartialRows = 65536;
+int most_splits(int units, int rows, const NodePlan& p) {
+  const int64_t fill = kNodeWorkgroups / ((int64_t)units * p.row_groups);
+  const int64_t room = kMostPartialRows / ((int64_t)units * rows);
+  const int64_t s = fill < room ? fill : room;
   return s < 1 ? 1 : s > kMaxNodeSplits ? kMaxNodeSplits : (int)s;
 }
 
 template <bool BF16, int D, int RT>
 hipError_t launch_t(NodesArgs a, const NodePlan& p, hipStream_t stream) {
-  const int tiles = (a.len0 + kTile - 1) / kTile, least = kMinTiles * p.key_waves();
-  a.nsplit = most_splits(a.units, p);
-  if (a.nsplit > tiles / least) a.nsplit = tiles / least > 1 ? tiles / least : 1;
+  const int tiles = (a.len0 + kTile - 1) / kTile + (a.n + kTile - 1) / kTile, most = tiles / p.key_waves();
+  a.nsplit = most_splits(a.units, a.n_heads / a.n_kv_heads * a.n, p);
+  if (a.nsplit > most) a.nsplit = most > 1 ? most : 1;
   hipLaunchKernelGGL((nodes_kernel<BF16, D, RT>), dim3((unsigned)a.units, (unsigned)a.nsplit, (unsigned)p.row_groups),
-                     dim3(64 * kNodeWaves), 0, stream, a, p.row_waves);
+                     dim3(64 * p.waves), 0, stream, a, p.row_waves);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
   const int64_t rows = (int64_t)a.units * (a.n_heads / a.n_kv_heads) * a.n;
@@ -628,23 +708,27 @@ hipError_t launch_t(NodesArgs a, const NodePlan& p, hipStream_t stream) {
 }  // namespace
 
 size_t nodes_work_bytes(int units, int head_dim, int group, int n) {
-  const size_t rows = (size_t)units * group * n;
+  // (the most that any number of nodes up to n asks for)
   size_t most = 16;
-  for (int bf16 = 0; bf16 < 2; ++bf16) {
-    const int s = most_splits(units, plan_of(group * n, bf16 != 0));
-    const size_t bytes = s > 1 ? rows * s * (head_dim + 2) * sizeof(float) : 0;
-    if (bytes > most) most = bytes;
-  }
+  for (int x = 1; x <= n; ++x)
+    for (int kind = 0; kind < 3; ++kind) {
+      const int rows = group * x, s = most_splits(units, rows, plan_of(rows, kind != 0, head_dim, kind == 2));
+      const size_t bytes = s > 1 ? (size_t)units * rows * s * (head_dim + 2) * sizeof(float) : 0;
+      if (bytes > most) most = bytes;
+    }
   return most;
 }
 
 hipError_t launch_nodes(const NodesArgs& a, int dtype, int head_dim, int group, hipStream_t stream) {
-  const NodePlan p = plan_of(group * a.n, dtype == BM_BF16);
+  const int64_t work = (int64_t)a.units * group * a.n * a.len0;
+  const NodePlan p = plan_of(group * a.n, dtype == BM_BF16, head_dim, work >= kBigWork);
   if (dtype == BM_F32)
     return head_dim == 128 ? launch_t<false, 128, 1>(a, p, stream) : launch_t<false, 64, 1>(a, p, stream);
   if (head_dim == 128)
-    return p.rt == 1 ? launch_t<true, 128, 1>(a, p, stream) : launch_t<true, 128, 2>(a, p, stream);
-  return p.rt == 1 ? launch_t<true, 64, 1>(a, p, stream) : launch_t<true, 64, 2>(a, p, stream);
+    return p.rt == 1 ? launch_t<true, 128, 1>(a, p, stream)
+         : p.rt == 2 ? launch_t<true, 128, 2>(a, p, stream) : launch_t<true, 128, 4>(a, p, stream);
+  return p.rt == 1 ? launch_t<true, 64, 1>(a, p, stream)
+       : p.rt == 2 ? launch_t<true, 64, 2>(a, p, stream) : launch_t<true, 64, 4>(a, p, stream);
 }
 
 }  // namespace bm

@@ -16,6 +16,7 @@ namespace {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __bf16 __attribute__((vector_size(8))) bf16v4;   // operand type of the LDS transpose read
@@ -28,11 +29,6 @@ template <typename T>
 __device__ __forceinline__ T* lds_at(uint32_t off) { return (T*)(uintptr_t)off; }
 
 constexpr float kNegInf = -__builtin_huge_valf();
-
-__device__ __forceinline__ float as_float(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-__device__ __forceinline__ float as_float(float x) { return x; }
-__device__ __forceinline__ void put(uint16_t* p, float x) { *reinterpret_cast<__bf16*>(p) = (__bf16)x; }
-__device__ __forceinline__ void put(float* p, float x) { *p = x; }
 
 // ---- bfloat16: tiles of 64 keys in LDS, 256 query rows a workgroup ----
 //
@@ -531,47 +527,140 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   }
 }
 
-// ---- float32: one wave a query row ----
-template <typename E, int D>
-__global__ void __launch_bounds__(256) window_rows_kernel(PromptArgs a) {
-  constexpr int P = D / 64;
+// ---- float32: 16 query rows a wave, operands straight from the rows ----
+//
+// MFMA-bound (a sixteenth of bfloat16's rate: 4096 cycles a tile of 32 keys at d = 128, where
+// a wave loads 32 KB), so nothing is staged.  Lane (i, h) of a tile: S^T = K Q^T takes 16
+// bytes of key row 16 s + i a step, contracting their four elements one after the other; a
+// lane then holds 8 logits of row i, keys 16 t + 4 h + r, and O^T += V^T P^T takes the keys in
+// that order: elements EPL i .. of V rows 16 t + 4 h + r, M-tile e standing for EPL i + e.
+// Every wave has its own keys: its rows' sinks and window.
+constexpr int kF32Rows = 16, kF32Tile = 32;
+
+template <int D>
+__global__ void __launch_bounds__(256, 2) window_prompt_f32_kernel(PromptArgs a, int blocks) {
+  constexpr int RB = 4 * D, KL = D / 16, EPL = D / 16;
   const int group = a.n_heads / a.n_kv_heads;
-  const int64_t wave = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (wave >= (int64_t)a.units * group * a.n_tok) return;
-  const int t = (int)(wave % a.n_tok);
-  const int64_t head = wave / a.n_tok;                 // sample * n_heads + query head
-  const int bi = (int)(head / a.n_heads), u = (int)(head / group);
-  const int pad = a.pad ? max(0, a.pad[bi]) : 0;
-  const int r0 = a.t0 - pad, i = r0 + t;
-  const E* q = static_cast<const E*>(a.q) + (head * a.seq_ld + t) * D;
-  E* o = static_cast<E*>(a.o) + (head * a.seq_ld + t) * D;
-  float x[P], acc[P], m = kNegInf, l = 0.0f;
-#pragma unroll
-  for (int e = 0; e < P; ++e) {
-    x[e] = as_float(q[lane * P + e]) * a.scale_log2;
-    acc[e] = 0.0f;
+  const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, i16 = lane & 15, h = lane >> 4;
+  if (wave >= (int64_t)a.units * group * blocks) return;
+  // the heads of a unit next to each other: they share keys
+  const int g = (int)(wave % group), blk = (int)(wave / group % blocks), u = (int)(wave / group / blocks);
+  const int bi = u / a.n_kv_heads, hk = u - bi * a.n_kv_heads;
+  const int64_t head = (int64_t)bi * a.n_heads + hk * group + g;
+  const int pad = a.pad ? max(0, __builtin_amdgcn_readfirstlane(a.pad[bi])) : 0;
+  const int r0 = a.t0 - pad, tw = blk * kF32Rows, t_own = tw + i16;
+  const int p1 = min(tw + kF32Rows, a.n_tok);
+  float* o = static_cast<float*>(a.o) + (head * a.seq_ld + t_own) * D + 4 * EPL * h;
+  if (r0 + p1 - 1 < 0) {
+    // pad tokens alone
+    if (t_own < a.n_tok)
+      for (int e = 0; e < 4 * EPL; e += 4) *reinterpret_cast<f32x4*>(o + e) = f32x4{0, 0, 0, 0};
+    return;
   }
-  const int lo = max(0, i - a.window + 1), lead = min(a.sinks, lo);
-  for (int c = 0; c < lead + (i + 1 - lo) && i >= 0; ++c) {
-    const int j = c < lead ? c : lo + c - lead;
-    const bool old = j < r0;
-    const int64_t row = old ? (int64_t)u * (a.window + a.sinks) + window_slot(j, a.sinks, a.window)
-                            : (int64_t)u * a.seq_ld + (j - r0);
-    const E* k = static_cast<const E*>(old ? a.kc : a.kin) + row * D;
-    const E* v = static_cast<const E*>(old ? a.vc : a.vin) + row * D;
-    float z = 0.0f;
+  const int first = max(r0 + tw, 0), last = r0 + p1 - 1;
+  const int lo = max(0, first - a.window + 1), lead = min(a.sinks, lo), shift = lo - lead;
+  const int nv = lead + last - lo + 1, nt = (nv + kF32Tile - 1) / kF32Tile;
+  const int ring0 = max(lo, a.sinks) - a.sinks;
+  const int place0 = ring0 % a.window - (ring0 + a.sinks - shift);
+  const char* kc = static_cast<const char*>(a.kc) + (int64_t)u * (a.window + a.sinks) * RB;
+  const char* vc = static_cast<const char*>(a.vc) + (int64_t)u * (a.window + a.sinks) * RB;
+  const char* ki = static_cast<const char*>(a.kin) + (int64_t)u * a.seq_ld * RB;
+  const char* vi = static_cast<const char*>(a.vin) + (int64_t)u * a.seq_ld * RB;
+  // the row of key number v (past the last one: the last)
+  auto row_of = [&](int v, const char* cached, const char* input) BM_LAMBDA {
+    v = min(v, nv - 1);
+    const int j = v < lead ? v : v + shift;
+    int slot = place0 + v;
+    slot = j < a.sinks ? j : a.sinks + (slot >= a.window ? slot - a.window : slot);
+    return j < r0 ? cached + (int64_t)slot * RB : input + (int64_t)(j - r0) * RB;
+  };
+  f32x4 kf[2][KL], vf[8][EPL / 4], qf[KL];
+  auto load_k = [&](int t) BM_LAMBDA {
 #pragma unroll
-    for (int e = 0; e < P; ++e) z = fmaf(x[e], as_float(k[lane * P + e]), z);
-    z = lanes::wave_sum(z);
-    const float mn = fmaxf(m, z), f = __builtin_amdgcn_exp2f(m - mn), p = __builtin_amdgcn_exp2f(z - mn);
-    l = l * f + p;
+    for (int s = 0; s < 2; ++s) {
+      const char* p = row_of(t * kF32Tile + 16 * s + i16, kc, ki) + 16 * h;
 #pragma unroll
-    for (int e = 0; e < P; ++e) acc[e] = acc[e] * f + p * as_float(v[lane * P + e]);
-    m = mn;
+      for (int kk = 0; kk < KL; ++kk) kf[s][kk] = *reinterpret_cast<const f32x4*>(p + 64 * kk);
+    }
+  };
+  auto load_v = [&](int t) BM_LAMBDA {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const char* p = row_of(t * kF32Tile + 16 * (i >> 2) + 4 * h + (i & 3), vc, vi) + i16 * (4 * EPL);
+#pragma unroll
+      for (int e = 0; e < EPL / 4; ++e) vf[i][e] = *reinterpret_cast<const f32x4*>(p + 16 * e);
+    }
+  };
+  load_k(0);
+  load_v(0);
+  {
+    const char* q = static_cast<const char*>(a.q) + (head * a.seq_ld + min(t_own, a.n_tok - 1)) * RB + 16 * h;
+#pragma unroll
+    for (int kk = 0; kk < KL; ++kk) qf[kk] = *reinterpret_cast<const f32x4*>(q + 64 * kk);
   }
+  const int vhi = max(min(r0 + t_own, last), first) - shift;      // what the lane's row sees
+  const int wfirst = first - shift, wlast = last - shift;
+  f32x4 acc[EPL];
+  float m = kNegInf, l = 0.0f;
 #pragma unroll
-  for (int e = 0; e < P; ++e) put(o + lane * P + e, i >= 0 ? acc[e] / l : 0.0f);
+  for (int e = 0; e < EPL; ++e) acc[e] = f32x4{0, 0, 0, 0};
+  const float c2 = a.scale_log2;
+  for (int t = 0; t < nt; ++t) {
+    f32x4 s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+    for (int kk = 0; kk < KL; ++kk)
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+          s[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(kf[x][kk][j], qf[kk][j], s[x], 0, 0, 0);
+    load_k(t + 1);
+    const int v0 = t * kF32Tile;
+    if (!(v0 + 31 <= wfirst && (v0 + 31 < a.sinks || v0 > wlast - a.window))) {
+      auto below = [](int x) BM_LAMBDA { return x <= 0 ? 0u : x >= 32 ? ~0u : (1u << x) - 1; };   // keys < x
+      const uint32_t seen = below(vhi + 1 - v0) & (~below(vhi + 1 - a.window - v0) | below(a.sinks - v0));
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        s[i >> 2][i & 3] = (seen >> (16 * (i >> 2) + 4 * h + (i & 3))) & 1 ? s[i >> 2][i & 3] : kNegInf;
+    }
+    float top = kNegInf;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, s[i >> 2][i & 3]);
+    if (__ballot(top * c2 > m + kRescaleLog2) != 0) {
+      float x = lanes::max_xor16_32(top) * c2;
+      const float mn = fmaxf(m, x), f = mn == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) acc[e] *= f;
+    }
+    const float ref = m == kNegInf ? 0.0f : m;
+    float p[8], sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      p[i] = __builtin_amdgcn_exp2f(fmaf(s[i >> 2][i & 3], c2, -ref));
+      sum += p[i];
+    }
+    l += sum;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int e = 0; e < EPL; ++e)
+        acc[e] = __builtin_amdgcn_mfma_f32_16x16x4f32(vf[i][e / 4][e % 4], p[i], acc[e], 0, 0, 0);
+    load_v(t + 1);
+  }
+  if (t_own >= a.n_tok) return;
+  l = lanes::add_xor<32>(lanes::add_xor<16>(l));
+  const bool real = r0 + t_own >= 0;                              // (a pad token sees nothing)
+  const float inv = 1.0f / l;
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+#pragma unroll
+    for (int e = 0; e < EPL; e += 4) {
+      const f32x4 y = {acc[e][x] * inv, acc[e + 1][x] * inv, acc[e + 2][x] * inv, acc[e + 3][x] * inv};
+      *reinterpret_cast<f32x4*>(o + EPL * x + e) = real ? y : f32x4{0, 0, 0, 0};
+    }
 }
 
 // Rows of the tokens that the cache keeps, 16 bytes a thread: token t of the call's last
@@ -623,8 +712,9 @@ hipError_t launch_bf16(const PromptArgs& a, hipStream_t stream) {
 
 template <int D>
 hipError_t launch_f32(const PromptArgs& a, hipStream_t stream) {
-  const int64_t waves = (int64_t)a.units * (a.n_heads / a.n_kv_heads) * a.n_tok;
-  hipLaunchKernelGGL((window_rows_kernel<float, D>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, a);
+  const int blocks = (a.n_tok + kF32Rows - 1) / kF32Rows;
+  const int64_t waves = (int64_t)a.units * (a.n_heads / a.n_kv_heads) * blocks;
+  hipLaunchKernelGGL((window_prompt_f32_kernel<D>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, a, blocks);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? launch_store<4 * D>(a, stream) : e;
 }
@@ -642,11 +732,51 @@ hipError_t launch_d(const PromptArgs& a, int dtype, int group, hipStream_t strea
 
 }  // namespace
 
+namespace {
+
+// A few tokens are the nodes of a chain: the node kernel splits their keys over workgroups,
+// where a launch of the prompt kernels has one for 256 rows.
+constexpr int kShortWorkgroups = 128;
+bool is_short(const PromptArgs& a, int dtype, int group) {
+  (void)dtype;
+  return a.n_tok <= kShortPrompt && (a.n_tok * group <= 32 || a.units <= kShortWorkgroups);
+}
+
+}  // namespace
+
 bool prompt_fits(int units, int group, int n_tok) {
   return (int64_t)units * group * n_tok / 4 < 0x7FFFFFFF;
 }
 
 hipError_t launch_prompt(const PromptArgs& a, int dtype, int head_dim, int group, hipStream_t stream) {
+  if (is_short(a, dtype, group)) {
+    NodesArgs n{};
+    n.q = a.q;
+    n.kin = a.kin;
+    n.vin = a.vin;
+    n.o = a.o;
+    n.kc = a.kc;
+    n.vc = a.vc;
+    n.pad = a.pad;
+    n.part = a.part;
+    n.seq_ld = a.seq_ld;
+    n.n_heads = a.n_heads;
+    n.n_kv_heads = a.n_kv_heads;
+    n.units = a.units;
+    n.slots = a.window + a.sinks;
+    n.len0 = a.t0 < n.slots ? a.t0 : n.slots;
+    n.n = a.n_tok;
+    n.next_pos = a.t0;
+    n.window = a.window;
+    n.sinks = a.sinks;
+    n.chain = 1;
+    n.store = a.n_tok == 1;
+    n.scale_log2 = a.scale_log2;
+    const hipError_t e = launch_nodes(n, dtype, head_dim, group, stream);
+    if (e != hipSuccess || n.store) return e;
+    const int rb = head_dim * (dtype == BM_BF16 ? 2 : 4);
+    return rb == 128 ? launch_store<128>(a, stream) : rb == 256 ? launch_store<256>(a, stream) : launch_store<512>(a, stream);
+  }
   return head_dim == 128 ? launch_d<128>(a, dtype, group, stream) : launch_d<64>(a, dtype, group, stream);
 }
 
