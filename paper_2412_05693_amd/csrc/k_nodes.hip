@@ -22,6 +22,7 @@
 // over the same rows join through LDS, workgroups over the same unit through the workspace
 // and a second launch.
 #include <type_traits>
+#include <utility>
 
 #include "bm_internal.h"
 #include "bm_lanes.h"
@@ -68,6 +69,18 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 // a buffer of whole rows: reads behind its end give zeros
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_of(const void* p, int bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00020000);
+}
+
+// x = max(x, y, z) in one instruction (of values that assembly made the compiler first makes
+// quiet numbers)
+__device__ __forceinline__ void max3(float& x, float y, float z) {
+  asm volatile("v_max3_f32 %0, %0, %1, %2" : "+v"(x) : "v"(y), "v"(z));
+}
+
+// f(0), f(1), .. with numbers that are constants
+template <typename F, int... I>
+__device__ __forceinline__ void each(F f, std::integer_sequence<int, I...>) {
+  (f(std::integral_constant<int, I>{}), ...);
 }
 
 // What the tree is to one wave: lane a stands for node a.
@@ -231,7 +244,7 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
     }
   };
   load_k(kw);
-  load_v(kw);
+  if constexpr (!(BF16 && kBig)) load_v(kw);
 
   // ---- the rows' queries, and what the tree shows them ----
   u32x4 qf[RT][KL];
@@ -248,14 +261,11 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
   }
   const Tree tree = make_tree(a.parent ? a.parent + (int64_t)bi * a.n : nullptr, a.chain != 0, a.n, r0, a.sinks,
                               a.window ? a.window : kNoWindow);
-  uint64_t sees[RT];
-  int depth[RT];
+  // (what a row's node sees and its depth come from that node's lane where they are needed)
+  int own[RT];
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int node = min(row[rt], rows - 1) % a.n;
-    sees[rt] = shfl64(tree.sees, node);
-    depth[rt] = __shfl(tree.depth, node);
-  }
+  for (int rt = 0; rt < RT; ++rt) own[rt] = min(row[rt], rows - 1) % a.n;
+
   // The entries that the window hides from the deepest node: `old` slots from `oldest` on, going
   // round behind the ring's last one.  Where all nodes are roots nobody sees them; otherwise
   // the deeper ones do not.
@@ -344,7 +354,7 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
           }
         }
     const int pk0 = pk;
-    load_k(t + key_waves);
+    if constexpr (!kBig) load_k(t + key_waves);
     if constexpr (BF16 && kBig) s_settled(s);
 
     // ---- keys that nobody sees: bit k of `gone`; V rows of theirs become zeros, so that a
@@ -381,10 +391,12 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
       }
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        mask[rt] = hide | (node ? (uint32_t)~(sees[rt] >> base) >> (4 * h) : 0u);
+        const int depth = __shfl(tree.depth, own[rt]);
+        const uint64_t sees = shfl64(tree.sees, own[rt]);
+        mask[rt] = hide | (node ? (uint32_t)~(sees >> base) >> (4 * h) : 0u);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-          if (dist[i] <= depth[rt]) mask[rt] |= 1u << (16 * (i >> 2) + (i & 3));
+          if (dist[i] <= depth) mask[rt] |= 1u << (16 * (i >> 2) + (i & 3));
           if ((mask[rt] >> (16 * (i >> 2) + (i & 3))) & 1) s[rt][i >> 2][i & 3] = kNegInf;
         }
       }
@@ -466,7 +478,14 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
           vt[2 * w][j] = __builtin_amdgcn_perm(vf[2 * j + 1][w], vf[2 * j][w], 0x05040100);
           vt[2 * w + 1][j] = __builtin_amdgcn_perm(vf[2 * j + 1][w], vf[2 * j][w], 0x07060302);
         }
-      load_v(t + key_waves);
+      if constexpr (kBig) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+          for (int w = 0; w < VW; ++w) vf[i][w] = 0;
+      } else {
+        load_v(t + key_waves);
+      }
 #pragma unroll
       for (int e = 0; e < EPL; ++e)
 #pragma unroll
@@ -534,14 +553,185 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
       }
       keep_acc();
     }
+    if constexpr (kBig) load_k(t + key_waves);           // (before, there are no registers for it)
   };
-  keep_acc();
-  for (int t = kw; t < total;) {
-    for (; t < cached && !(nested && has_old((lo + t) * kTile)); t += key_waves) {
-      tile(std::false_type{}, t);
+
+  // Big waves, plain tiles: the values' product of tile t - 1 goes with the weights of tile t,
+  // product by product, so that the matrix and the vector unit work at the same time (one
+  // wave a SIMD: nobody else would use the one while the other works).  V is loaded a
+  // tile later than K: vf holds tile t - 1's rows, of which nobody sees `late`.
+  using weights_t = uint32_t[BF16 && kBig ? RT : 1][8];
+  weights_t po = {};                                     // tile t - 1's: four words, four of the rest
+  uint32_t late = 0;
+  auto turn = [&](u32x4 (&vt)[EPL]) BM_LAMBDA {
+    if (late != 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const bool z = ((late >> (4 * h)) >> (16 * (i >> 2) + (i & 3))) & 1;
+#pragma unroll
+        for (int w = 0; w < VW; ++w) vf[i][w] = z ? 0u : vf[i][w];
+      }
+    }
+#pragma unroll
+    for (int w = 0; w < VW; ++w)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        vt[2 * w][j] = __builtin_amdgcn_perm(vf[2 * j + 1][w], vf[2 * j][w], 0x05040100);
+        vt[2 * w + 1][j] = __builtin_amdgcn_perm(vf[2 * j + 1][w], vf[2 * j][w], 0x07060302);
+      }
+  };
+  auto product = [&](auto jc, const u32x4 (&vt)[EPL]) BM_LAMBDA {
+    constexpr int j = decltype(jc)::value, e = j / (2 * RT), part = j / RT % 2, rt = j % RT;
+    const uint32_t* p = po[rt] + 4 * part;
+    acc[rt][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, vt[e]),
+                                                         __builtin_bit_cast(bf16x8, u32x4{p[0], p[1], p[2], p[3]}),
+                                                         acc[rt][e], 0, 0, 0);
+  };
+  // what is left of the last plain tile
+  auto flush = [&]() BM_LAMBDA {
+    if constexpr (BF16 && kBig) {
+      u32x4 vt[EPL];
+      turn(vt);
+      each([&](auto jc) BM_LAMBDA { product(jc, vt); }, std::make_integer_sequence<int, 2 * RT * EPL>{});
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) po[rt][i] = 0;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int w = 0; w < VW; ++w) vf[i][w] = 0;
+      late = 0;
       keep_acc();
     }
+  };
+  auto plain_tile = [&](int t) BM_LAMBDA {
+    if constexpr (!(BF16 && kBig)) {
+      tile(std::false_type{}, t);
+    } else {
+      const int base = (lo + t) * kTile;
+      f32x4 s[RT][2];
+#pragma unroll
+      for (int kk = 0; kk < KL; ++kk)
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            if (kk == 0) mfma_s<true>(s[rt][x], kf[x][kk], qf[rt][kk]);
+            else mfma_s<false>(s[rt][x], kf[x][kk], qf[rt][kk]);
+          }
+      const int pk0 = pk;
+      load_k(t + key_waves);
+      u32x4 vt[EPL];
+      turn(vt);
+      load_v(t);
+      s_settled(s);
+      late = 0;
+      if (base + kTile > entries || (pos && pad > 0) || (!nested && has_old(base))) {
+        const int slot = base + (lane & 31);
+        late = (uint32_t)__ballot(slot >= entries || (pos && pad > 0 && pk0 < pad) || (!nested && is_old(slot)));
+        if (late != 0) {
+          const uint32_t hide = late >> (4 * h);
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              s[rt][i >> 2][i & 3] = (hide >> (16 * (i >> 2) + (i & 3))) & 1 ? kNegInf : s[rt][i >> 2][i & 3];
+        }
+      }
+      // the maxima; O follows behind the product of the tile before
+      float top[RT], f[RT];
+      bool over = false;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        top[rt] = kNegInf;
+        f[rt] = 1.0f;
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) max3(top[rt], s[rt][i >> 2][i & 3], s[rt][i >> 2][(i & 3) + 1]);
+        over = over || top[rt] * c2 > m[rt] + kRescaleLog2;
+      }
+      const bool raise = __ballot(over) != 0;
+      if (__builtin_expect(raise, 0)) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          const float mn = fmaxf(m[rt], lanes::max_xor16_32(top[rt]) * c2);
+          f[rt] = mn == kNegInf ? 1.0f : __builtin_amdgcn_exp2f(m[rt] - mn);
+          m[rt] = mn;
+          l[rt] *= f[rt];
+        }
+      }
+      float ref[RT], sum[RT];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        ref[rt] = m[rt] == kNegInf ? 0.0f : m[rt];
+        sum[rt] = 0.0f;
+      }
+      // weight i of the lane's 8 RT: its argument a weight before, its sum and packing one behind
+      weights_t pn;
+      float x[2], y[2];
+      auto args = [&](int i) BM_LAMBDA { x[i & 1] = fmaf(s[i / 8][(i >> 2) & 1][i & 3], c2, -ref[i / 8]); };
+      auto pack = [&](int i) BM_LAMBDA {
+        sum[i / 8] += y[i & 1];
+        if (i & 1) {
+          uint32_t hi = pack2(y[0], y[1]);
+          uint32_t rest = pack2(y[0] - __uint_as_float(hi << 16), y[1] - __uint_as_float(hi & 0xFFFF0000u));
+          asm volatile("" : "+v"(hi), "+v"(rest), "+v"(sum[i / 8]));   // (made here, not where they are used)
+          pn[i / 8][(i & 7) >> 1] = hi;
+          pn[i / 8][4 + ((i & 7) >> 1)] = rest;
+        }
+      };
+      constexpr int NS = 2 * RT * EPL, NW = 8 * RT, EVERY = NS / NW;
+      args(0);
+      each([&](auto jc) BM_LAMBDA {
+        constexpr int j = decltype(jc)::value, i = j / EVERY;
+        __builtin_amdgcn_sched_barrier(0);
+        product(jc, vt);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (j % EVERY == 0) {
+          // (an even weight's packing waits for the odd one's: y holds both)
+          const float e = __builtin_amdgcn_exp2f(x[i & 1]);
+          if constexpr (i > 0) pack(i - 1);
+          y[i & 1] = e;
+          if constexpr (i + 1 < NW) args(i + 1);
+        }
+      }, std::make_integer_sequence<int, NS>{});
+      pack(NW - 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        l[rt] += sum[rt];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) po[rt][i] = pn[rt][i];
+      }
+      if (__builtin_expect(raise, 0)) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          asm volatile("" : "+v"(f[rt]));              // (not multiplied by 1 every time)
+#pragma unroll
+          for (int e = 0; e < EPL; ++e) {
+            acc[rt][e] *= f[rt];
+            asm volatile("" : "+a"(acc[rt][e]));
+          }
+        }
+      }
+    }
+  };
+  keep_acc();
+  if constexpr (BF16 && kBig) {
+    // nothing comes before the first plain tile
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int w = 0; w < VW; ++w) vf[i][w] = 0;
+  }
+  for (int t = kw; t < total;) {
+    for (; t < cached && !(nested && has_old((lo + t) * kTile)); t += key_waves) {
+      plain_tile(t);
+      keep_acc();
+    }
+    flush();
     if (t < total) {
+      if constexpr (BF16 && kBig) load_v(t);
       tile(std::true_type{}, t);
       t += key_waves;
     }
@@ -570,6 +760,7 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
   }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
+    const bool none = r0 + __shfl(tree.depth, own[rt]) < 0;   // a pad token: it sees nothing
     if (row[rt] >= rows) continue;
     float f[kNodeWaves], mx = m[rt], sum = l[rt];
     if (key_waves > 1) {
@@ -587,10 +778,9 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
         }
       }
     }
-    const int g = row[rt] / a.n, node = row[rt] - g * a.n;
+    const int g = row[rt] / a.n, node = own[rt];
     const int64_t head = (int64_t)bi * a.n_heads + hk * group + g;
     const int64_t at = ((int64_t)u * a.nsplit + split) * rows + row[rt];
-    const bool none = r0 + depth[rt] < 0;                // a pad token: it sees nothing
     const float inv = a.nsplit > 1 ? 1.0f : none ? 0.0f : 1.0f / sum;
 #pragma unroll
     for (int x = 0; x < 4; ++x) {

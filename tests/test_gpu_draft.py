@@ -101,6 +101,35 @@ def test_cache_lengths_at_tile_borders(length, n, group):
     c.check_tree(parent, q, k, v, o, lse)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("n,group", [(64, 4), (40, 2), (12, 4), (64, 1), (5, 1)])
+@pytest.mark.parametrize("window", [0, 90])
+def test_launches_of_many_units(dtype, d, n, group, window):
+    """More units than compute units: one workgroup has all of a unit's tiles, the nodes' and
+    those at the window's edge one behind the other."""
+    b, kw = 260, dict(heads=group, kv_heads=1, d=d, dtype=dtype)
+    if window:
+        r = Run(window=window, sinks=3, s=200, b=b, **kw)
+        r.go(200, heads=(), samples=())
+        att = r.att
+    else:
+        c = Bound(b=b, s=150, **kw)
+        att = c.att
+    parent = random_tree(b, n, 3, span=3)
+    q, k, v = (rows(60 + i, b, hh, n, d, dtype).cuda() for i, hh in enumerate((group, 1, 1)))
+    o, lse = torch.zeros_like(q), torch.zeros((b, group, n), device="cuda")
+    att.draft_attend(parent.cuda(), q, k, v, o, lse=lse)
+    for j in (0, 131, b - 1):
+        if window:
+            exact = r.ref.tree(parent, q, k, v, heads=(group - 1,), samples=(j,))[j, group - 1]
+        else:
+            exact = tree_over(att.k[j, 0, :100], att.v[j, 0, :100], torch.ones(100, dtype=torch.bool), parent[j].tolist(),
+                              q[j, group - 1], k[j, 0], v[j, 0], d ** -0.5, DT[dtype])
+        check_rows(o[j, group - 1], exact, f"sample {j}")
+        for a, row in enumerate(exact):
+            assert abs(float(lse[j, group - 1, a]) - row.lse) <= row.lse_tol, (j, a)
+
+
 def test_an_empty_cache():
     c = Bound(b=1, s=10, kv_max=600)
     c.att.resume(0, 10)
