@@ -590,9 +590,9 @@ bm::NodesArgs nodes_args(const bm_ctx* ctx, int32_t n, const int32_t* parent, co
 
 BM_EXPORT size_t bm_win_workspace_bytes(const bm_dims* dims) {
   if (check_win(dims, 0) != BM_OK) return 0;
-  return bm::nodes_work_bytes(dims->b * dims->n_kv_heads, dims->head_dim,
-                              dims->n_heads / dims->n_kv_heads,
-                              dims->block < bm::kShortPrompt ? dims->block : bm::kShortPrompt);
+  return bm::prompt_work_bytes(dims->b * dims->n_kv_heads, dims->head_dim,
+                               dims->n_heads / dims->n_kv_heads, dims->block,
+                               dims->dtype == BM_BF16);
 }
 
 BM_EXPORT int bm_win_validate(const bm_dims* dims, int32_t sinks) {

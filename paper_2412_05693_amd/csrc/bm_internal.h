@@ -185,8 +185,9 @@ struct PromptArgs {
   void* vc;
   const int32_t* pad; // [b] left pad tokens per sample, or null
   int64_t seq_ld;
-  float* part;        // scratch of nodes_work_bytes for up to kShortPrompt nodes
+  float* part;        // scratch of prompt_work_bytes
   int n_heads, n_kv_heads, units, window, sinks, t0, n_tok;
+  int nsplit;         // workgroups over the keys of a row block (set by launch_prompt)
   float scale_log2;
 };
 
@@ -269,12 +270,16 @@ hipError_t launch_kv4_long(const Kv4DecodeArgs& a, int dtype, int head_dim, int 
 // read rows, then (independently: no slot and no row twice) write rows; either may have n = 0
 hipError_t launch_kv4_rows(const Kv4RowsArgs& read, const Kv4RowsArgs& write, int dtype,
                            int head_dim, hipStream_t stream);
-hipError_t launch_prompt(const PromptArgs& a, int dtype, int head_dim, int group, hipStream_t stream);
+hipError_t launch_prompt(PromptArgs a, int dtype, int head_dim, int group, hipStream_t stream);
 // whether a launch of that size can be made
 bool prompt_fits(int units, int group, int n_tok);
+// bytes of PromptArgs.part for calls of up to n tokens
+size_t prompt_work_bytes(int units, int head_dim, int group, int n, bool bf16);
 hipError_t launch_nodes(const NodesArgs& a, int dtype, int head_dim, int group, hipStream_t stream);
 // bytes of NodesArgs.part for n nodes, whatever the cache holds
 size_t nodes_work_bytes(int units, int head_dim, int group, int n);
+// the join of launch_nodes alone: NodesArgs' o, part, seq_ld, units, heads, n and nsplit (> 1, 64 at most)
+hipError_t launch_nodes_join(const NodesArgs& a, int dtype, int head_dim, hipStream_t stream);
 hipError_t launch_accept(const AcceptArgs& a, int dtype, int head_dim, int group, hipStream_t stream);
 hipError_t launch_reset(float* score, int32_t* len, size_t n_score, size_t n_len,
                         hipStream_t stream);

@@ -880,6 +880,14 @@ int most_splits(int units, int rows, const NodePlan& p) {
   return s < 1 ? 1 : s > kMaxNodeSplits ? kMaxNodeSplits : (int)s;
 }
 
+template <bool BF16, int D>
+hipError_t launch_join(const NodesArgs& a, hipStream_t stream) {
+  const int64_t rows = (int64_t)a.units * (a.n_heads / a.n_kv_heads) * a.n;
+  hipLaunchKernelGGL((nodes_join_kernel<typename NodeCfg<BF16, D>::E, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256),
+                     0, stream, a);
+  return hipGetLastError();
+}
+
 template <bool BF16, int D, int RT>
 hipError_t launch_t(NodesArgs a, const NodePlan& p, hipStream_t stream) {
   const int tiles = (a.len0 + kTile - 1) / kTile + (a.n + kTile - 1) / kTile, most = tiles / p.key_waves();
@@ -888,11 +896,7 @@ hipError_t launch_t(NodesArgs a, const NodePlan& p, hipStream_t stream) {
   hipLaunchKernelGGL((nodes_kernel<BF16, D, RT>), dim3((unsigned)a.units, (unsigned)a.nsplit, (unsigned)p.row_groups),
                      dim3(64 * p.waves), 0, stream, a, p.row_waves);
   hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.nsplit == 1) return e;
-  const int64_t rows = (int64_t)a.units * (a.n_heads / a.n_kv_heads) * a.n;
-  hipLaunchKernelGGL((nodes_join_kernel<typename NodeCfg<BF16, D>::E, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256),
-                     0, stream, a);
-  return hipGetLastError();
+  return e == hipSuccess && a.nsplit > 1 ? launch_join<BF16, D>(a, stream) : e;
 }
 
 }  // namespace
@@ -919,6 +923,11 @@ hipError_t launch_nodes(const NodesArgs& a, int dtype, int head_dim, int group, 
          : p.rt == 2 ? launch_t<true, 128, 2>(a, p, stream) : launch_t<true, 128, 4>(a, p, stream);
   return p.rt == 1 ? launch_t<true, 64, 1>(a, p, stream)
        : p.rt == 2 ? launch_t<true, 64, 2>(a, p, stream) : launch_t<true, 64, 4>(a, p, stream);
+}
+
+hipError_t launch_nodes_join(const NodesArgs& a, int dtype, int head_dim, hipStream_t stream) {
+  if (dtype == BM_F32) return head_dim == 128 ? launch_join<false, 128>(a, stream) : launch_join<false, 64>(a, stream);
+  return head_dim == 128 ? launch_join<true, 128>(a, stream) : launch_join<true, 64>(a, stream);
 }
 
 }  // namespace bm

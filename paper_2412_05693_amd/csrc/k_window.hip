@@ -108,7 +108,19 @@ __device__ __forceinline__ void each(F f, std::integer_sequence<int, I...>) {
   (f(std::integral_constant<int, I>{}), ...);
 }
 
-template <int D, int G>
+// What a workgroup over a part of the keys leaves of a row: O without its division, m and l
+// (none: -inf, 0), for launch_nodes_join.
+__device__ __forceinline__ int64_t part_row(const PromptArgs& a, int u, int group, int g, int t) {
+  return (((int64_t)u * a.nsplit + blockIdx.y) * group + g) * a.n_tok + t;
+}
+__device__ __forceinline__ void put_sums(const PromptArgs& a, int group, int d, int64_t at, float m, float l) {
+  float* ml = a.part + (int64_t)a.units * a.nsplit * group * a.n_tok * d + at * 2;
+  ml[0] = m;
+  ml[1] = l;
+}
+
+// SPLIT: blockIdx.y is one of a.nsplit workgroups over the keys
+template <int D, int G, bool SPLIT>
 __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(PromptArgs a, int tiles_per_unit) {
   constexpr int RB = 2 * D, CPR = RB / 16, KK = D / 16, MT = D / 32;
   constexpr int TILE = kPromptTile * RB;                     // bytes
@@ -132,7 +144,28 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   const int p1 = min(p0 + PT, a.n_tok);
   const int64_t head = (int64_t)bi * a.n_heads + hk * G + w % G;
 
-  if (r0 + p1 - 1 < 0) {
+  // ---- the keys' numbers ----
+  const int first = max(r0 + p0, 0), last = r0 + p1 - 1;     // indices of real rows
+  const int lo = max(0, first - a.window + 1);
+  const int lead = min(a.sinks, lo), shift = lo - lead;
+  const int nv = lead + last - lo + 1;
+  const int nt = (nv + kPromptTile - 1) / kPromptTile;
+  // the workgroup's tiles: t0 to t1
+  const int per = SPLIT ? (nt + a.nsplit - 1) / a.nsplit : nt;
+  const int t0 = SPLIT ? min((int)blockIdx.y * per, nt) : 0, t1 = SPLIT ? min(t0 + per, nt) : nt;
+  if (SPLIT && (last < 0 || t0 == t1)) {
+    // pad tokens alone, or no keys left
+    for (int c = lane; c < kPromptRows * CPR; c += 64) {
+      const int t = tw + c / CPR;
+      if (t >= a.n_tok) break;
+      const int64_t at = part_row(a, u, G, w % G, t);
+      float* y = a.part + at * D + c % CPR * 8;
+      *reinterpret_cast<f32x4*>(y) = *reinterpret_cast<f32x4*>(y + 4) = f32x4{0, 0, 0, 0};
+      if (c % CPR == 0) put_sums(a, G, D, at, kNegInf, 0.0f);
+    }
+    return;
+  }
+  if (last < 0) {
     // pad tokens alone
     for (int c = lane; c < kPromptRows * CPR; c += 64) {
       const int t = tw + c / CPR;
@@ -142,12 +175,6 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
     return;
   }
 
-  // ---- the keys' numbers ----
-  const int first = max(r0 + p0, 0), last = r0 + p1 - 1;     // indices of real rows
-  const int lo = max(0, first - a.window + 1);
-  const int lead = min(a.sinks, lo), shift = lo - lead;
-  const int nv = lead + last - lo + 1;
-  const int nt = (nv + kPromptTile - 1) / kPromptTile;
   // ring places of the cached keys: number v lies at place0 + v (less the window at its end)
   const int ring0 = max(lo, a.sinks) - a.sinks;
   const int place0 = ring0 % a.window - (ring0 + a.sinks - shift);
@@ -203,9 +230,9 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   };
   // (three tiles' rows and the queries on their way at once: one wait for memory)
   u32x4 k1[NCOPY], v1[NCOPY], k2[NCOPY], v2[NCOPY];
-  load_mixed(ks, vs, 0);
-  load_mixed(k1, v1, min(1, nt - 1));
-  load_mixed(k2, v2, min(2, nt - 1));
+  load_mixed(ks, vs, t0);
+  load_mixed(k1, v1, min(t0 + 1, t1 - 1));
+  load_mixed(k2, v2, min(t0 + 2, t1 - 1));
 
   // ---- queries: lane (n, h) holds row n, chunks 2 kk + h ----
   u32x4 qf[2][KK];
@@ -436,7 +463,7 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
     for (int r = 0; r < 16; r += 2) max3(top[rt], za[rt][r], za[rt][r + 1]);
-  if (!plain(0)) hide(za, top, 0);
+  if (!plain(2 * t0)) hide(za, top, 2 * t0);
   raised = exceeds();
 #pragma unroll
   for (int i = 0; i < 2; ++i) kpre[i] = *lds_at<lds_u32x4>(ka[i] + 32 * RB);
@@ -453,8 +480,8 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
       for (int mt = 0; mt < MT; ++mt) asm volatile("" : "+a"(o[rt][mt]));
   };
   keep_o();
-  for (int t = 0; t < nt; ++t) {
-    step(std::integral_constant<int, 1>{}, [](auto) BM_LAMBDA {}, zb, za, pa, pb, 2 * t);
+  for (int t = 0; t < t1 - t0; ++t) {
+    step(std::integral_constant<int, 1>{}, [](auto) BM_LAMBDA {}, zb, za, pa, pb, 2 * (t0 + t));
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) ka[kk] ^= TILE;
     lds_barrier();
@@ -464,7 +491,7 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
     v_at += next;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt) va[mt] += next;
-    const Run run = run_of(min(t + 3, nt - 1));
+    const Run run = run_of(min(t0 + t + 3, t1 - 1));
     step(std::integral_constant<int, 0>{},
          [&](auto jc) BM_LAMBDA {
            constexpr int j = decltype(jc)::value, EVERY = (2 * KK + 4 * MT) / 16, c = j / EVERY;
@@ -472,7 +499,7 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
              if constexpr (c < NCOPY) store_k(c, t);
              if constexpr (c >= NCOPY && c < 2 * NCOPY) store_v(c - NCOPY, v_new);
              if constexpr (c == 2 * NCOPY) {
-               if (__builtin_expect(!run.is, 0)) load_mixed(ks, vs, min(t + 3, nt - 1));
+               if (__builtin_expect(!run.is, 0)) load_mixed(ks, vs, min(t0 + t + 3, t1 - 1));
              }
              if constexpr (c >= 2 * NCOPY && c < 4 * NCOPY) {
                if (run.is) {
@@ -482,7 +509,7 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
              }
            }
          },
-         za, zb, pb, pa, 2 * t + 1);
+         za, zb, pb, pa, 2 * (t0 + t) + 1);
     keep_o();
   }
   // the last half's values
@@ -496,6 +523,26 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
     for (int rt = 0; rt < 2; ++rt)
       o[rt][q % MT] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u32x4{y0.x, y0.y, y1.x, y1.y}),
                                                               __builtin_bit_cast(bf16x8, pb[rt][q / MT]), o[rt][q % MT], 0, 0, 0);
+  }
+  if constexpr (SPLIT) {
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt) {
+      const float sum = lanes::add_xor<32>(l[rt]);
+      const int t = tw + 32 * rt + n;
+      if (t >= a.n_tok) continue;
+      const bool real = r0 + t >= 0;                       // (a pad token sees nothing)
+      const int64_t at = part_row(a, u, G, w % G, t);
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x16 x = o[rt][mt];
+          *reinterpret_cast<f32x4*>(a.part + at * D + 32 * mt + 8 * i + 4 * h) =
+              f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
+        }
+      if (h == 0) put_sums(a, G, D, at, real ? m[rt] : kNegInf, real ? sum : 0.0f);
+    }
+    return;
   }
   __syncthreads();
 
@@ -539,6 +586,7 @@ constexpr int kF32Rows = 16, kF32Tile = 32;
 
 template <int D>
 __global__ void __launch_bounds__(256, 2) window_prompt_f32_kernel(PromptArgs a, int blocks) {
+  const bool split = a.nsplit > 1;             // blockIdx.y: one of the workgroups over the keys
   constexpr int RB = 4 * D, KL = D / 16, EPL = D / 16;
   const int group = a.n_heads / a.n_kv_heads;
   const int64_t wave = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -552,15 +600,20 @@ __global__ void __launch_bounds__(256, 2) window_prompt_f32_kernel(PromptArgs a,
   const int r0 = a.t0 - pad, tw = blk * kF32Rows, t_own = tw + i16;
   const int p1 = min(tw + kF32Rows, a.n_tok);
   float* o = static_cast<float*>(a.o) + (head * a.seq_ld + t_own) * D + 4 * EPL * h;
-  if (r0 + p1 - 1 < 0) {
-    // pad tokens alone
-    if (t_own < a.n_tok)
-      for (int e = 0; e < 4 * EPL; e += 4) *reinterpret_cast<f32x4*>(o + e) = f32x4{0, 0, 0, 0};
-    return;
-  }
   const int first = max(r0 + tw, 0), last = r0 + p1 - 1;
   const int lo = max(0, first - a.window + 1), lead = min(a.sinks, lo), shift = lo - lead;
   const int nv = lead + last - lo + 1, nt = (nv + kF32Tile - 1) / kF32Tile;
+  const int64_t at = split ? part_row(a, u, group, g, t_own) : 0;
+  if (split) o = a.part + at * D + 4 * EPL * h;
+  const int per = (nt + a.nsplit - 1) / a.nsplit, t0 = min((int)blockIdx.y * per, nt), t1 = min(t0 + per, nt);
+  if (last < 0 || t0 == t1) {
+    // pad tokens alone, or no keys left
+    if (t_own < a.n_tok) {
+      for (int e = 0; e < 4 * EPL; e += 4) *reinterpret_cast<f32x4*>(o + e) = f32x4{0, 0, 0, 0};
+      if (split && h == 0) put_sums(a, group, D, at, kNegInf, 0.0f);
+    }
+    return;
+  }
   const int ring0 = max(lo, a.sinks) - a.sinks;
   const int place0 = ring0 % a.window - (ring0 + a.sinks - shift);
   const char* kc = static_cast<const char*>(a.kc) + (int64_t)u * (a.window + a.sinks) * RB;
@@ -592,8 +645,8 @@ __global__ void __launch_bounds__(256, 2) window_prompt_f32_kernel(PromptArgs a,
       for (int e = 0; e < EPL / 4; ++e) vf[i][e] = *reinterpret_cast<const f32x4*>(p + 16 * e);
     }
   };
-  load_k(0);
-  load_v(0);
+  load_k(t0);
+  load_v(t0);
   {
     const char* q = static_cast<const char*>(a.q) + (head * a.seq_ld + min(t_own, a.n_tok - 1)) * RB + 16 * h;
 #pragma unroll
@@ -606,7 +659,7 @@ __global__ void __launch_bounds__(256, 2) window_prompt_f32_kernel(PromptArgs a,
 #pragma unroll
   for (int e = 0; e < EPL; ++e) acc[e] = f32x4{0, 0, 0, 0};
   const float c2 = a.scale_log2;
-  for (int t = 0; t < nt; ++t) {
+  for (int t = t0; t < t1; ++t) {
     f32x4 s[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
 #pragma unroll
     for (int kk = 0; kk < KL; ++kk)
@@ -653,7 +706,8 @@ __global__ void __launch_bounds__(256, 2) window_prompt_f32_kernel(PromptArgs a,
   if (t_own >= a.n_tok) return;
   l = lanes::add_xor<32>(lanes::add_xor<16>(l));
   const bool real = r0 + t_own >= 0;                              // (a pad token sees nothing)
-  const float inv = 1.0f / l;
+  const float inv = split ? 1.0f : 1.0f / l;
+  if (split && h == 0) put_sums(a, group, D, at, real ? m : kNegInf, real ? l : 0.0f);
 #pragma unroll
   for (int x = 0; x < 4; ++x)
 #pragma unroll
@@ -700,28 +754,84 @@ hipError_t launch_store(const PromptArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
+// A launch of fewer workgroups than compute units gives each row block's keys to several, as
+// many as the measured times of their work make worth it: 1.9 us a tile of 64 keys, 2.7 us
+// one of 32 in float32, against 5 us for a join and 14 (4) us for the parts of 256
+// workgroups.  us without -> with, samples x tokens of 8 KV heads, four query heads each,
+// d = 128:
+//   window  1 x 128      1 x 512      2 x 256      8 x 256      float32, 1 x 128
+//   512     31 -> 25     32 -> 32     32 -> 32     39 -> 39     54 -> 28
+//   1024    45 -> 29     45 -> 41     47 -> 41     56 -> 56     96 -> 39
+//   4096    132 -> 37    138 -> 61    143 -> 61    164 -> 152   351 -> 102
+constexpr int kPromptWorkgroups = 256, kMaxPromptSplits = 64;
+int most_prompt_splits(int64_t workgroups) {
+  const int64_t s = kPromptWorkgroups / workgroups;
+  return s < 1 ? 1 : s > kMaxPromptSplits ? kMaxPromptSplits : (int)s;
+}
+int prompt_splits(int64_t workgroups, int tiles, bool bf16) {
+  // tenths of us
+  const int most = most_prompt_splits(workgroups), tile = bf16 ? 19 : 27, parts = bf16 ? 140 : 40;
+  int best = 1, least = tiles * tile;
+  for (int s = 2; s <= most; ++s) {
+    const int cost = (tiles + s - 1) / s * tile + 50 + (int)(parts * workgroups * s / kPromptWorkgroups);
+    if (cost < least) {
+      best = s;
+      least = cost;
+    }
+  }
+  return best;
+}
+// tokens of a row block, and workgroups
+int block_tokens(bool bf16, int group) { return bf16 ? kPromptWaves * kPromptRows / group : kF32Rows; }
+int64_t prompt_workgroups(int units, int group, int n_tok, bool bf16) {
+  const int pt = block_tokens(bf16, group);
+  const int64_t blocks = ((int64_t)n_tok + pt - 1) / pt;
+  return bf16 ? units * blocks : (units * group * blocks + 3) / 4;
+}
+
+// behind the workgroups: the join of their parts, the rows to store
+hipError_t finish(const PromptArgs& a, int dtype, int head_dim, hipStream_t stream) {
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (a.nsplit > 1) {
+    NodesArgs n{};
+    n.o = a.o;
+    n.part = a.part;
+    n.seq_ld = a.seq_ld;
+    n.n_heads = a.n_heads;
+    n.n_kv_heads = a.n_kv_heads;
+    n.units = a.units;
+    n.n = a.n_tok;
+    n.nsplit = a.nsplit;
+    e = launch_nodes_join(n, dtype, head_dim, stream);
+    if (e != hipSuccess) return e;
+  }
+  const int rb = head_dim * (dtype == BM_BF16 ? 2 : 4);
+  return rb == 128 ? launch_store<128>(a, stream) : rb == 256 ? launch_store<256>(a, stream) : launch_store<512>(a, stream);
+}
+
 template <int D, int G>
 hipError_t launch_bf16(const PromptArgs& a, hipStream_t stream) {
-  constexpr int PT = kPromptWaves * kPromptRows / G;
-  const int tiles = (a.n_tok + PT - 1) / PT;
-  hipLaunchKernelGGL((window_prompt_kernel<D, G>), dim3((unsigned)(a.units * tiles)), dim3(64 * kPromptWaves), 0,
-                     stream, a, tiles);
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? launch_store<2 * D>(a, stream) : e;
+  const int tiles = (int)prompt_workgroups(1, G, a.n_tok, true);
+  const dim3 grid((unsigned)(a.units * tiles), (unsigned)a.nsplit);
+  if (a.nsplit > 1)
+    hipLaunchKernelGGL((window_prompt_kernel<D, G, true>), grid, dim3(64 * kPromptWaves), 0, stream, a, tiles);
+  else
+    hipLaunchKernelGGL((window_prompt_kernel<D, G, false>), grid, dim3(64 * kPromptWaves), 0, stream, a, tiles);
+  return finish(a, BM_BF16, D, stream);
 }
 
 template <int D>
-hipError_t launch_f32(const PromptArgs& a, hipStream_t stream) {
-  const int blocks = (a.n_tok + kF32Rows - 1) / kF32Rows;
-  const int64_t waves = (int64_t)a.units * (a.n_heads / a.n_kv_heads) * blocks;
-  hipLaunchKernelGGL((window_prompt_f32_kernel<D>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, stream, a, blocks);
-  const hipError_t e = hipGetLastError();
-  return e == hipSuccess ? launch_store<4 * D>(a, stream) : e;
+hipError_t launch_f32(const PromptArgs& a, int group, hipStream_t stream) {
+  hipLaunchKernelGGL((window_prompt_f32_kernel<D>),
+                     dim3((unsigned)prompt_workgroups(a.units, group, a.n_tok, false), (unsigned)a.nsplit), dim3(256), 0,
+                     stream, a, (a.n_tok + kF32Rows - 1) / kF32Rows);
+  return finish(a, BM_F32, D, stream);
 }
 
 template <int D>
 hipError_t launch_d(const PromptArgs& a, int dtype, int group, hipStream_t stream) {
-  if (dtype == BM_F32) return launch_f32<D>(a, stream);
+  if (dtype == BM_F32) return launch_f32<D>(a, group, stream);
   switch (group) {
     case 1: return launch_bf16<D, 1>(a, stream);
     case 2: return launch_bf16<D, 2>(a, stream);
@@ -730,16 +840,13 @@ hipError_t launch_d(const PromptArgs& a, int dtype, int group, hipStream_t strea
   }
 }
 
-}  // namespace
-
-namespace {
-
-// A few tokens are the nodes of a chain: the node kernel splits their keys over workgroups,
-// where a launch of the prompt kernels has one for 256 rows.
-constexpr int kShortWorkgroups = 128;
+// A few tokens are the nodes of a chain: their waves have fewer rows, and take keys each.  us
+// as nodes and as a prompt, samples x tokens of 8 KV heads, four query heads each, d = 128,
+// over a window of 4096: bfloat16 1 x 16 22 and 24, 32 x 16 107 and 181, 1 x 32 28 and 26,
+// 32 x 32 144 and 183, 1 x 64 35 and 32, 32 x 64 267 and 192; float32 8 x 8 64 and 110,
+// 32 x 16 389 and 392, 32 x 32 761 and 712.
 bool is_short(const PromptArgs& a, int dtype, int group) {
-  (void)dtype;
-  return a.n_tok <= kShortPrompt && (a.n_tok * group <= 32 || a.units <= kShortWorkgroups);
+  return a.n_tok <= kShortPrompt && a.n_tok * group <= (dtype == BM_BF16 ? 128 : 64);
 }
 
 }  // namespace
@@ -748,7 +855,21 @@ bool prompt_fits(int units, int group, int n_tok) {
   return (int64_t)units * group * n_tok / 4 < 0x7FFFFFFF;
 }
 
-hipError_t launch_prompt(const PromptArgs& a, int dtype, int head_dim, int group, hipStream_t stream) {
+size_t prompt_work_bytes(int units, int head_dim, int group, int n, bool bf16) {
+  size_t most = nodes_work_bytes(units, head_dim, group, n < kShortPrompt ? n : kShortPrompt);
+  // (every number of row blocks that is split; the last block full, or what n has of it)
+  const int pt = block_tokens(bf16, group);
+  for (int64_t t = pt;; t += pt) {
+    const int tokens = (int)(t < n ? t : n), s = most_prompt_splits(prompt_workgroups(units, group, tokens, bf16));
+    if (s == 1) break;
+    const size_t bytes = (size_t)units * group * tokens * s * (head_dim + 2) * sizeof(float);
+    if (bytes > most) most = bytes;
+    if (t >= n) break;
+  }
+  return most;
+}
+
+hipError_t launch_prompt(PromptArgs a, int dtype, int head_dim, int group, hipStream_t stream) {
   if (is_short(a, dtype, group)) {
     NodesArgs n{};
     n.q = a.q;
@@ -774,9 +895,14 @@ hipError_t launch_prompt(const PromptArgs& a, int dtype, int head_dim, int group
     n.scale_log2 = a.scale_log2;
     const hipError_t e = launch_nodes(n, dtype, head_dim, group, stream);
     if (e != hipSuccess || n.store) return e;
-    const int rb = head_dim * (dtype == BM_BF16 ? 2 : 4);
-    return rb == 128 ? launch_store<128>(a, stream) : rb == 256 ? launch_store<256>(a, stream) : launch_store<512>(a, stream);
+    a.nsplit = 1;
+    return finish(a, dtype, head_dim, stream);
   }
+  const bool bf16 = dtype == BM_BF16;
+  // (a row block sees the sinks, the window before it and itself, and no more than there is)
+  const int64_t end = (int64_t)a.t0 + a.n_tok, seen = (int64_t)a.sinks + a.window + block_tokens(bf16, group);
+  const int tile = bf16 ? kPromptTile : kF32Tile;
+  a.nsplit = prompt_splits(prompt_workgroups(a.units, group, a.n_tok, bf16), (int)(((end < seen ? end : seen) + tile - 1) / tile), bf16);
   return head_dim == 128 ? launch_d<128>(a, dtype, group, stream) : launch_d<64>(a, dtype, group, stream);
 }
 

@@ -147,6 +147,23 @@ def test_tokens_over_long_caches(window, sinks, dtype, d, heads, kv_heads):
         r.go(1, step=True)
 
 
+@pytest.mark.parametrize("window,sinks", [(1500, 4), (777, 0), (3000, 64)])
+@pytest.mark.parametrize("dtype,d,heads,kv_heads", [("bf16", 128, 4, 1), ("f32", 64, 2, 2), ("bf16", 64, 4, 2),
+                                                    ("bf16", 128, 1, 1), ("f32", 128, 4, 1)])
+def test_turns_over_long_caches(window, sinks, dtype, d, heads, kv_heads):
+    """Few rows over many keys, which several workgroups share: before the window is full,
+    and after; a sample that begins within a turn, one that has not begun."""
+    r = Run(window=window, sinks=sinks, s=3756, b=3, heads=heads, kv_heads=kv_heads, d=d, dtype=dtype,
+            pads=(0, 1490, 5000))
+    r.go(1400, heads=(heads - 1,))
+    r.go(133, heads=(0,))
+    r.go(1900, heads=(), samples=())
+    r.go(66, heads=(0,))
+    r.go(257, heads=(heads - 1,), ld=300, row=11)
+    r.go(1, step=True)
+    r.check_slots()
+
+
 def test_rows_inside_larger_buffers():
     """Rows before and behind the call's are neither read nor written."""
     r = Run(window=20, sinks=2, s=100)

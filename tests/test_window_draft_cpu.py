@@ -34,6 +34,9 @@ def test_window_dims():
     assert ok(head_dim=96) == UNSUP and ok(n_heads=16) == UNSUP and ok(b=0) == BAD
     assert bmx.bm_win_workspace_bytes(dims(b=0)) == 0
     assert bmx.bm_win_workspace_bytes(dims(block=1 << 20)) > 0
+    for b in (1, 3, 40, 1000):                                  # longer calls never need less
+        need = [bmx.bm_win_workspace_bytes(dims(b=b, block=n)) for n in (*range(1, 700), 1 << 14, 1 << 20)]
+        assert need == sorted(need)
     assert status_of(bmx.bm_win_validate, dims(dtype=3), 0) == UNSUP
 
 
