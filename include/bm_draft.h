@@ -65,7 +65,8 @@ int bm_draft_attend(bm_ctx* ctx, int32_t n, const int32_t* parent, const void* q
  * entries grow by that much ON THE DEVICE, so that its next token again stands next to
  * its last, and in a bounded cache hidden entries of zeros, which leave at the next cut,
  * stand for the tokens that it did not take.  All that depends on ages or distances is
- * as if the sample had run by itself: its own next index is next_pos - pad[j]. */
+ * as if the sample had run by itself: its own next index is next_pos - pad[j].  So with
+ * count each context (each layer's) needs a pad array of its own. */
 int bm_draft_accept(bm_ctx* ctx, int32_t n, int32_t m, const int32_t* path, const int32_t* count,
                     const void* q, const void* k, const void* v, int32_t seq_ld, const float* lse,
                     hipStream_t stream);

@@ -697,7 +697,7 @@ class PDAttention:
         one's child) of the tree of n nodes (by default all rows from ``row`` on; ``lse``, if
         given, has n columns) and advance by m.  ``lse``: as draft_attend left it.  ``count``
         int32 ``[b]``: sample j takes only the first count[j]; the samples' left padding has to
-        be set, and that tensor grows by m - count."""
+        be set, and that tensor grows by m - count: caches (layers) must not share it."""
         if n is None:
             n = lse.shape[-1] if lse is not None else q.shape[2] - row
         m = path.shape[-1]

@@ -32,6 +32,11 @@ __device__ __forceinline__ int node_at(const AcceptArgs& a, int bi, int i) {
   return min(max(a.path[(int64_t)bi * a.m + i], 0), a.n - 1);
 }
 
+// a sample's pad behind the call; the largest stays (a sample that never begins)
+__device__ __forceinline__ int grown(int pad, int late) {
+  return pad > 0x7FFFFFFF - late ? 0x7FFFFFFF : pad + late;
+}
+
 template <bool BF16, int D>
 struct AcceptCfg {
   using E = typename std::conditional<BF16, uint16_t, float>::type;
@@ -158,7 +163,7 @@ __global__ void __launch_bounds__(256) accept_kernel(AcceptArgs a) {
 // the samples' pads behind the kernel that reads them
 __global__ void __launch_bounds__(256) pad_kernel(AcceptArgs a, int b) {
   const int bi = blockIdx.x * 256 + threadIdx.x;
-  if (bi < b) a.pad[bi] = max(0, a.pad[bi]) + a.m - taken(a, bi);
+  if (bi < b) a.pad[bi] = grown(max(0, a.pad[bi]), a.m - taken(a, bi));
 }
 
 // Window cache: a workgroup a sample, all KV heads' rows, and then the sample's pad.
@@ -182,7 +187,7 @@ __global__ void __launch_bounds__(256) window_accept_kernel(AcceptArgs a) {
         *reinterpret_cast<const u32x4*>(static_cast<const char*>(a.vin) + src);
   }
   __syncthreads();
-  if (a.count && threadIdx.x == 0) a.pad[bi] = pad + a.m - c;
+  if (a.count && threadIdx.x == 0) a.pad[bi] = grown(pad, a.m - c);
 }
 
 // Workgroups over a unit's cached tiles: a wave's tile costs what a workgroup's start does, so

@@ -1,5 +1,7 @@
 """Drafted tokens over bounded and window caches: a tree's attention against a 64-bit
 reference, and accepted paths against the calls that would have brought the same tokens."""
+import math
+
 import pytest
 import torch
 
@@ -381,6 +383,30 @@ def test_counts_and_path_numbers_outside_their_range():
         assert torch.equal(a[:, :, :63], b[:, :, :63])
         if y != "pos":
             assert torch.isnan(a[:, :, 63:]).all()
+
+
+@pytest.mark.parametrize("window", [0, 20])
+def test_a_sample_that_never_begins(window):
+    """The largest pad stays the largest, so that the sample goes on seeing nothing."""
+    largest = 2 ** 31 - 1
+    kw = dict(b=2, s=60, max_gen=20, n_heads=4, n_kv_heads=2, head_dim=64)
+    att = bmx.WindowAttention(window=window, **kw) if window else bmx.PDAttention(kv_max=64, block=16, **kw)
+    pads = torch.tensor([0, largest], dtype=torch.int32, device="cuda")
+    att.set_left_padding(pads)
+    q, k, v = (torch.ones((2, h, 60, 64), dtype=torch.bfloat16, device="cuda") for h in (4, 2, 2))
+    o = torch.zeros_like(q)
+    for t in range(0, 60, 15):
+        att.prefill_block(t, 15, q, k, v, o)
+    parent = torch.arange(-1, 3).expand(2, 4).int().contiguous().cuda()
+    path = torch.arange(3).expand(2, 3).int().contiguous().cuda()
+    for taken in ([1, 0], [3, 3]):
+        lse = torch.zeros((2, 4, 4), device="cuda")
+        att.draft_attend(parent, q[:, :, :4].contiguous(), k[:, :, :4].contiguous(), v[:, :, :4].contiguous(),
+                         o[:, :, :4].contiguous(), lse=lse)
+        assert torch.isfinite(lse[0]).all() and (lse[1] == -math.inf).all()
+        att.draft_accept(path, q[:, :, :4].contiguous(), k[:, :, :4].contiguous(), v[:, :, :4].contiguous(), lse=lse,
+                         count=torch.tensor(taken, dtype=torch.int32, device="cuda"))
+        assert pads.tolist() == [2, largest]
 
 
 def test_the_same_node_twice():
