@@ -272,10 +272,13 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
   const bool nested = __ballot(lane < a.n && tree.depth > 0) != 0;
   int oldest = 0, old = 0;
   if (a.window) {
-    int deepest = lane < a.n ? tree.depth : 0;
+    int deepest = 0;
+    if (nested) {
+      deepest = lane < a.n ? tree.depth : 0;
 #pragma unroll
-    for (int off = 32; off; off >>= 1) deepest = max(deepest, __shfl_xor(deepest, off));
-    deepest = __builtin_amdgcn_readfirstlane(deepest);
+      for (int off = 32; off; off >>= 1) deepest = max(deepest, __shfl_xor(deepest, off));
+      deepest = __builtin_amdgcn_readfirstlane(deepest);
+    }
     const bool full = r0 >= a.sinks + a.window;
     oldest = a.sinks + (full ? (ring.last + 1) % a.window : 0);
     old = min(full ? deepest + 1 : max(r0 - a.window + deepest - a.sinks + 1, 0), a.window);
@@ -758,63 +761,73 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
     }
     __syncthreads();
   }
+  // (their number is a constant here so that nothing waits for one LDS read after the other)
+  auto join = [&](auto kw_tag) BM_LAMBDA {
+    constexpr int KW = decltype(kw_tag)::value;
 #pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const bool none = r0 + __shfl(tree.depth, own[rt]) < 0;   // a pad token: it sees nothing
-    if (row[rt] >= rows) continue;
-    float f[kNodeWaves], mx = m[rt], sum = l[rt];
-    if (key_waves > 1) {
-      const float* y = part + rt * (QUADS * 256 + 128) + QUADS * 256 + lane;
-      mx = kNegInf;
-      for (int j = 0; j < key_waves; ++j) mx = fmaxf(mx, y[j * PART]);
-      sum = 0.0f;
+    for (int rt = 0; rt < RT; ++rt) {
+      const bool none = r0 + __shfl(tree.depth, own[rt]) < 0;   // a pad token: it sees nothing
+      if (row[rt] >= rows) continue;
+      float f[KW], mx = m[rt], sum = l[rt];
+      if constexpr (KW > 1) {
+        const float* y = part + rt * (QUADS * 256 + 128) + QUADS * 256 + lane;
+        float mj[KW], lj[KW];
 #pragma unroll
-      for (int j = 0; j < kNodeWaves; ++j) {
-        f[j] = 0.0f;
-        if (j < key_waves) {
-          const float mj = y[j * PART];
-          f[j] = mj == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(mj - mx);
-          sum = fmaf(f[j], y[j * PART + 64], sum);
+        for (int j = 0; j < KW; ++j) {
+          mj[j] = y[j * PART];
+          lj[j] = y[j * PART + 64];
+        }
+        mx = mj[0];
+#pragma unroll
+        for (int j = 1; j < KW; ++j) mx = fmaxf(mx, mj[j]);
+        sum = 0.0f;
+#pragma unroll
+        for (int j = 0; j < KW; ++j) {
+          f[j] = mj[j] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(mj[j] - mx);
+          sum = fmaf(f[j], lj[j], sum);
         }
       }
-    }
-    const int g = row[rt] / a.n, node = own[rt];
-    const int64_t head = (int64_t)bi * a.n_heads + hk * group + g;
-    const int64_t at = ((int64_t)u * a.nsplit + split) * rows + row[rt];
-    const float inv = a.nsplit > 1 ? 1.0f : none ? 0.0f : 1.0f / sum;
+      const int g = row[rt] / a.n, node = own[rt];
+      const int64_t head = (int64_t)bi * a.n_heads + hk * group + g;
+      const int64_t at = ((int64_t)u * a.nsplit + split) * rows + row[rt];
+      const float inv = a.nsplit > 1 ? 1.0f : none ? 0.0f : 1.0f / sum;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      if (((4 * rt + x) & (key_waves - 1)) != kw) continue;
+      for (int x = 0; x < 4; ++x) {
+        if (((4 * rt + x) & (KW - 1)) != kw) continue;
 #pragma unroll
-      for (int e = 0; e < EPL; e += 4) {
-        f32x4 o = {acc[rt][e][x], acc[rt][e + 1][x], acc[rt][e + 2][x], acc[rt][e + 3][x]};
-        if (key_waves > 1) {
-          o = f32x4{0, 0, 0, 0};
-          const float* y = part + rt * (QUADS * 256 + 128) + ((x * EPL + e) / 4 * 64 + lane) * 4;
+        for (int e = 0; e < EPL; e += 4) {
+          f32x4 o = {acc[rt][e][x], acc[rt][e + 1][x], acc[rt][e + 2][x], acc[rt][e + 3][x]};
+          if constexpr (KW > 1) {
+            o = f32x4{0, 0, 0, 0};
+            const float* y = part + rt * (QUADS * 256 + 128) + ((x * EPL + e) / 4 * 64 + lane) * 4;
 #pragma unroll
-          for (int j = 0; j < kNodeWaves; ++j)
-            if (j < key_waves) o += f[j] * *reinterpret_cast<const f32x4*>(y + j * PART);
+            for (int j = 0; j < KW; ++j) o += f[j] * *reinterpret_cast<const f32x4*>(y + j * PART);
+          }
+          if (a.nsplit > 1) {
+            *reinterpret_cast<f32x4*>(a.part + at * D + 4 * EPL * h + EPL * x + e) = o;
+            continue;
+          }
+          o = none ? f32x4{0, 0, 0, 0} : o * inv;
+          E* dst = static_cast<E*>(a.o) + (head * a.seq_ld + node) * D + 4 * EPL * h + EPL * x + e;
+          if constexpr (BF16) *reinterpret_cast<u32x2*>(dst) = u32x2{pack2(o.x, o.y), pack2(o.z, o.w)};
+          else *reinterpret_cast<f32x4*>(dst) = o;
         }
+      }
+      if (h == 0 && kw == 0) {
         if (a.nsplit > 1) {
-          *reinterpret_cast<f32x4*>(a.part + at * D + 4 * EPL * h + EPL * x + e) = o;
-          continue;
+          float* ml = a.part + (int64_t)a.units * a.nsplit * rows * D + at * 2;
+          ml[0] = mx;
+          ml[1] = sum;
+        } else if (a.lse) {
+          a.lse[head * a.n + node] = none ? kNegInf : (mx + __builtin_amdgcn_logf(sum)) * kLn2;
         }
-        o = none ? f32x4{0, 0, 0, 0} : o * inv;
-        E* dst = static_cast<E*>(a.o) + (head * a.seq_ld + node) * D + 4 * EPL * h + EPL * x + e;
-        if constexpr (BF16) *reinterpret_cast<u32x2*>(dst) = u32x2{pack2(o.x, o.y), pack2(o.z, o.w)};
-        else *reinterpret_cast<f32x4*>(dst) = o;
       }
     }
-    if (h == 0 && kw == 0) {
-      if (a.nsplit > 1) {
-        float* ml = a.part + (int64_t)a.units * a.nsplit * rows * D + at * 2;
-        ml[0] = mx;
-        ml[1] = sum;
-      } else if (a.lse) {
-        a.lse[head * a.n + node] = none ? kNegInf : (mx + __builtin_amdgcn_logf(sum)) * kLn2;
-      }
-    }
-  }
+  };
+  if (key_waves == 1) join(std::integral_constant<int, 1>{});
+  else if (key_waves == 2) join(std::integral_constant<int, 2>{});
+  else if (key_waves == 4) join(std::integral_constant<int, 4>{});
+  else if constexpr (kNodeWaves == 8) join(std::integral_constant<int, 8>{});
 }
 
 // Join the parts of a unit's keys: a wave a row, lane c holding part c's m and l.
