@@ -830,55 +830,91 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
   else if constexpr (kNodeWaves == 8) join(std::integral_constant<int, 8>{});
 }
 
-// Join the parts of a unit's keys: a wave a row, lane c holding part c's m and l.
-template <typename E, int D>
+// Join the parts of a unit's keys: lane c holds part c's m and l of a row, C parts are on their
+// way at a time (past the last one its own again, without weight), the first ones before
+// their weights are known.  Latency-bound: a wave has one row, four where two parts say
+// that there are many (32768 rows take 12.0 us, 14.5 with one a wave; one token's 32 rows
+// of four parts the other way round: 10.0 us a step, 10.9 with two a wave).
+template <int C>
+constexpr int join_rows() { return C == 2 ? 4 : 1; }
+template <typename E, int D, int C>
 __global__ void __launch_bounds__(256) nodes_join_kernel(NodesArgs a) {
-  constexpr int P = D / 64;
-  const int group = a.n_heads / a.n_kv_heads, rows = group * a.n;
-  const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int P = D / 64, R = join_rows<C>();
+  const int group = a.n_heads / a.n_kv_heads, rows = group * a.n, all = a.units * rows;
+  const int w0 = ((int)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * R;
   const int lane = threadIdx.x & 63;
-  if (w >= (int64_t)a.units * rows) return;
-  const int u = (int)(w / rows), row = (int)(w - (int64_t)u * rows);
-  const int g = row / a.n, node = row - g * a.n;
-  const int64_t first = (int64_t)u * a.nsplit * rows + row;
-  const float* ml = a.part + (int64_t)a.units * a.nsplit * rows * D;
-  float m = kNegInf, l = 0.0f;
-  if (lane < a.nsplit) {
-    const float* x = ml + (first + (int64_t)lane * rows) * 2;
-    m = x[0];
-    l = x[1];
-  }
-  const float top = lanes::wave_max(m);
-  const bool none = top == kNegInf;                      // a pad token: it sees nothing
-  const float f = m == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m - top);
-  const float sum = lanes::wave_sum(f * l);
-  float o[P] = {};
-  // (eight parts on their way at a time; past the last one its own again, without weight)
-  for (int c0 = 0; c0 < a.nsplit; c0 += 8) {
-    float x[8][P];
+  if (w0 >= all) return;
+  const float* ml = a.part + (int64_t)a.nsplit * all * D;
+  int u[R], row[R];
+  int64_t first[R];
+  float x[R][C][P], m[R], l[R], o[R][P];
+  auto load = [&](int c0) BM_LAMBDA {
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const float* y = a.part + (first + (int64_t)min(c0 + c, a.nsplit - 1) * rows) * D + lane * P;
+    for (int r = 0; r < R; ++r)
 #pragma unroll
-      for (int e = 0; e < P; ++e) x[c][e] = y[e];
+      for (int c = 0; c < C; ++c) {
+        const float* y = a.part + (first[r] + (int64_t)min(c0 + c, a.nsplit - 1) * rows) * D + lane * P;
+#pragma unroll
+        for (int e = 0; e < P; ++e) x[r][c][e] = y[e];
+      }
+  };
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    const int w = min(w0 + r, all - 1);
+    u[r] = w / rows;
+    row[r] = w - u[r] * rows;
+    first[r] = (int64_t)u[r] * a.nsplit * rows + row[r];
+    m[r] = kNegInf;
+    l[r] = 0.0f;
+    if (lane < a.nsplit) {
+      const float* y = ml + (first[r] + (int64_t)lane * rows) * 2;
+      m[r] = y[0];
+      l[r] = y[1];
     }
 #pragma unroll
-    for (int c = 0; c < 8; ++c) {
-      const float fc = c0 + c < a.nsplit ? __shfl(f, c0 + c) : 0.0f;
+    for (int e = 0; e < P; ++e) o[r][e] = 0.0f;
+  }
+  load(0);
+  float top[R], f[R], sum[R];
 #pragma unroll
-      for (int e = 0; e < P; ++e) o[e] = fmaf(fc, x[c][e], o[e]);
+  for (int r = 0; r < R; ++r) {
+    top[r] = lanes::wave_max(m[r]);
+    f[r] = m[r] == kNegInf ? 0.0f : __builtin_amdgcn_exp2f(m[r] - top[r]);
+    sum[r] = lanes::wave_sum(f[r] * l[r]);
+  }
+  for (int c0 = 0;;) {
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        const float fc = c0 + c < a.nsplit ? __shfl(f[r], c0 + c) : 0.0f;
+#pragma unroll
+        for (int e = 0; e < P; ++e) o[r][e] = fmaf(fc, x[r][c][e], o[r][e]);
+      }
+    c0 += C;
+    if (c0 >= a.nsplit) break;
+    load(c0);
+  }
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    if (w0 + r >= all) break;
+    const bool none = top[r] == kNegInf;                 // a pad token: it sees nothing
+    const int g = row[r] / a.n, node = row[r] - g * a.n;
+    const int64_t head = (int64_t)(u[r] / a.n_kv_heads) * a.n_heads + (u[r] % a.n_kv_heads) * group + g;
+    E* dst = static_cast<E*>(a.o) + (head * a.seq_ld + node) * D + lane * P;
+#pragma unroll
+    for (int e = 0; e < P; ++e) o[r][e] = none ? 0.0f : o[r][e] / sum[r];
+    if constexpr (sizeof(E) == 4) {
+#pragma unroll
+      for (int e = 0; e < P; ++e) dst[e] = o[r][e];
+    } else if constexpr (P == 2) {
+      *reinterpret_cast<uint32_t*>(dst) = pack2(o[r][0], o[r][1]);
+    } else {
+      *reinterpret_cast<__bf16*>(dst) = (__bf16)o[r][0];
     }
+    if (a.lse && lane == 0)
+      a.lse[head * a.n + node] = none ? kNegInf : (top[r] + __builtin_amdgcn_logf(sum[r])) * kLn2;
   }
-  const int64_t head = (int64_t)(u / a.n_kv_heads) * a.n_heads + (u % a.n_kv_heads) * group + g;
-  E* dst = static_cast<E*>(a.o) + (head * a.seq_ld + node) * D + lane * P;
-#pragma unroll
-  for (int e = 0; e < P; ++e) {
-    const float y = none ? 0.0f : o[e] / sum;
-    if constexpr (sizeof(E) == 2) *reinterpret_cast<__bf16*>(dst + e) = (__bf16)y;
-    else dst[e] = y;
-  }
-  if (a.lse && lane == 0)
-    a.lse[head * a.n + node] = none ? kNegInf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 // Workgroups over a unit's entries: what fills the compute units, one workgroup each, with at
@@ -893,11 +929,18 @@ int most_splits(int units, int rows, const NodePlan& p) {
   return s < 1 ? 1 : s > kMaxNodeSplits ? kMaxNodeSplits : (int)s;
 }
 
+// (split launches have at most kMostPartialRows rows: numbers of 32 bits)
 template <bool BF16, int D>
 hipError_t launch_join(const NodesArgs& a, hipStream_t stream) {
-  const int64_t rows = (int64_t)a.units * (a.n_heads / a.n_kv_heads) * a.n;
-  hipLaunchKernelGGL((nodes_join_kernel<typename NodeCfg<BF16, D>::E, D>), dim3((unsigned)((rows + 3) / 4)), dim3(256),
-                     0, stream, a);
+  using E = typename NodeCfg<BF16, D>::E;
+  const int rows = a.units * (a.n_heads / a.n_kv_heads) * a.n;
+  auto launch = [&](auto c) {
+    constexpr int C = decltype(c)::value, in_block = 4 * join_rows<C>();
+    hipLaunchKernelGGL((nodes_join_kernel<E, D, C>), dim3((unsigned)((rows + in_block - 1) / in_block)), dim3(256), 0, stream, a);
+  };
+  if (a.nsplit <= 2) launch(std::integral_constant<int, 2>{});
+  else if (a.nsplit <= 4) launch(std::integral_constant<int, 4>{});
+  else launch(std::integral_constant<int, 8>{});
   return hipGetLastError();
 }
 
