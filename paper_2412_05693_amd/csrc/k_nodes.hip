@@ -18,6 +18,13 @@
 // bfloat16 weights go in two parts, the nearest bfloat16 and that of the rest (2^-16 in
 // all), so the outputs carry little more than their own rounding.
 //
+// A token is HBM-bound: 64 samples' over windows of 4096 entries (8 KV heads, d = 128) take
+// 175 us, 6.1 TB/s.  A tree of 64 nodes with four heads each (256 rows a unit) is bound by its
+// waves' own instructions, one wave a SIMD: 512 units of 4096 entries take 505 us, 375 without
+// their loads, of which the products are 186 (545 TFLOP/s; with the second parts 820).
+// Short launches are a chain of latencies: 8 units of 64 rows and 512 entries take 11 us,
+// of which arguments 1, queries and tree 2, tiles 3, the join 2.
+//
 // The workgroup's waves share the rows (up to 8 blocks of them) and then the key tiles; waves
 // over the same rows join through LDS, workgroups over the same unit through the workspace
 // and a second launch.
