@@ -147,9 +147,16 @@ struct NodePlan {
 //                       512 128 512  512 128 4096 512 256 512  512 256 4096
 //                       61.0 -> 59.0 413 -> 291   128 -> 92    833 -> 506
 constexpr int64_t kBigWork = 1 << 25;       // units x rows x entries
-NodePlan plan_of(int rows, bool bf16, int d, bool big) {
+// Waves of 16 rows have the shorter chain where there is next to nothing to read; us with
+// 32 -> 16 rows:
+//   units rows entries  8 32 512      8 64 512      8 256 512     32 64 512     32 128 512
+//                       12.5 -> 11.8  14.4 -> 13.8  24.6 -> 23.2  18.1 -> 17.5  24.4 -> 25.5
+//                       8 32 4096     8 64 4096     64 64 512     64 128 4096
+//                       15.5 -> 15.2  19.3 -> 19.8  18.9 -> 20.1  40.1 -> 55.3
+constexpr int64_t kSmallWork = 1 << 20;
+NodePlan plan_of(int rows, bool bf16, int d, int64_t work) {
   NodePlan p;
-  p.rt = !bf16 || rows <= 16 ? 1 : rows <= 32 || !big ? 2 : 4;
+  p.rt = !bf16 || rows <= 16 || work <= kSmallWork ? 1 : rows <= 32 || work < kBigWork ? 2 : 4;
   p.waves = node_waves(bf16, d, p.rt);
   const int blocks = (rows + 16 * p.rt - 1) / (16 * p.rt);
   p.row_waves = 1;
@@ -968,17 +975,19 @@ size_t nodes_work_bytes(int units, int head_dim, int group, int n) {
   // (the most that any number of nodes up to n asks for)
   size_t most = 16;
   for (int x = 1; x <= n; ++x)
-    for (int kind = 0; kind < 3; ++kind) {
-      const int rows = group * x, s = most_splits(units, rows, plan_of(rows, kind != 0, head_dim, kind == 2));
-      const size_t bytes = s > 1 ? (size_t)units * rows * s * (head_dim + 2) * sizeof(float) : 0;
-      if (bytes > most) most = bytes;
+    for (const int64_t work : {(int64_t)0, kSmallWork + 1, kBigWork}) {
+      for (const bool bf16 : {true, false}) {
+        const int rows = group * x, s = most_splits(units, rows, plan_of(rows, bf16, head_dim, work));
+        const size_t bytes = s > 1 ? (size_t)units * rows * s * (head_dim + 2) * sizeof(float) : 0;
+        if (bytes > most) most = bytes;
+      }
     }
   return most;
 }
 
 hipError_t launch_nodes(const NodesArgs& a, int dtype, int head_dim, int group, hipStream_t stream) {
   const int64_t work = (int64_t)a.units * group * a.n * a.len0;
-  const NodePlan p = plan_of(group * a.n, dtype == BM_BF16, head_dim, work >= kBigWork);
+  const NodePlan p = plan_of(group * a.n, dtype == BM_BF16, head_dim, work);
   if (dtype == BM_F32)
     return head_dim == 128 ? launch_t<false, 128, 1>(a, p, stream) : launch_t<false, 64, 1>(a, p, stream);
   if (head_dim == 128)
