@@ -446,7 +446,7 @@ class PDAttention:
         self._bhd = (b, n_heads, n_kv_heads, head_dim)
         self._row_bytes = head_dim * (4 if self.dims.dtype == BM_F32 else 2)
         self.ctx = None
-        self._draft_works = []
+        self._draft_works, self._draft_nodes = [], 0
         # schedule settings (bm_set_*): kept here and applied again to every new
         # context, so they survive reset() and resume()
         self._settings = {}
@@ -642,18 +642,17 @@ class PDAttention:
 
     # -- drafted tokens (include/bm_draft.h) -----------------------------------------
     def _ints(self, x, shape, name):
-        t = self.torch
-        if x.dtype != t.int32 or x.device != self.device or not x.is_contiguous() or \
-                tuple(x.shape) != shape:
+        if x.dtype is not self.torch.int32 or x.get_device() != self._dev_index or x.shape != shape or \
+                not x.is_contiguous():
             raise ValueError(f"{name}: need a contiguous int32 {list(shape)} tensor on {self.device}")
         return x.data_ptr()
 
     def _lse_ptr(self, lse, n):
         if lse is None:
             return None
-        t, shape = self.torch, (self.dims.b, self.dims.n_heads, n)
-        if lse.dtype != t.float32 or lse.device != self.device or not lse.is_contiguous() or \
-                tuple(lse.shape) != shape:
+        shape = (*self._bhd[:2], n)
+        if lse.dtype is not self.torch.float32 or lse.get_device() != self._dev_index or lse.shape != shape or \
+                not lse.is_contiguous():
             raise ValueError(f"lse: need a contiguous float32 {list(shape)} tensor on {self.device}")
         return lse.data_ptr()
 
@@ -679,14 +678,17 @@ class PDAttention:
         n = parent.shape[-1]
         tree = self._ints(parent, (self.dims.b, n), "parent")
         rows = self._tree_rows(n, q, k, v, o, row)
-        need = bm_draft_workspace_bytes(self.dims, n)
-        if self._draft_work is None or self._draft_work.numel() < need:
-            # (kept for later calls; of another size for a larger tree.  The old one stays
-            # with graphs that were captured over it)
-            self._draft_works.append(self.torch.empty(max(need, 16), dtype=self.torch.uint8, device=self.device))
+        if n > self._draft_nodes:
+            # (kept for later calls; another one for a larger tree, which needs no less.  The old
+            # one stays with graphs that were captured over it)
+            need = bm_draft_workspace_bytes(self.dims, n)
+            if need:                                   # (none: the call below says what is wrong)
+                self._draft_works.append(self.torch.empty(need, dtype=self.torch.uint8, device=self.device))
+                self._draft_nodes = n
         work = self._draft_work
-        bm_draft_attend(self.ctx, n, tree, *rows, q.shape[2], self._lse_ptr(lse, n), work.data_ptr(),
-                        work.numel(), self._stream())
+        bm_draft_attend(self.ctx, n, tree, *rows, q.shape[2], self._lse_ptr(lse, n),
+                        work.data_ptr() if work is not None else None,
+                        work.numel() if work is not None else 0, self._stream())
 
     @property
     def _draft_work(self):

@@ -972,17 +972,11 @@ hipError_t launch_t(NodesArgs a, const NodePlan& p, hipStream_t stream) {
 }  // namespace
 
 size_t nodes_work_bytes(int units, int head_dim, int group, int n) {
-  // (the most that any number of nodes up to n asks for)
-  size_t most = 16;
-  for (int x = 1; x <= n; ++x)
-    for (const int64_t work : {(int64_t)0, kSmallWork + 1, kBigWork}) {
-      for (const bool bf16 : {true, false}) {
-        const int rows = group * x, s = most_splits(units, rows, plan_of(rows, bf16, head_dim, work));
-        const size_t bytes = s > 1 ? (size_t)units * rows * s * (head_dim + 2) * sizeof(float) : 0;
-        if (bytes > most) most = bytes;
-      }
-    }
-  return most;
+  // (no plan has more splits than one of a single row group; never less for more nodes)
+  const int64_t fill = kNodeWorkgroups / units, s = fill > kMaxNodeSplits ? kMaxNodeSplits : fill;
+  if (s < 2) return 16;
+  const int64_t rows = (int64_t)units * group * n * s;
+  return (size_t)(rows < kMostPartialRows ? rows : kMostPartialRows) * (head_dim + 2) * sizeof(float);
 }
 
 hipError_t launch_nodes(const NodesArgs& a, int dtype, int head_dim, int group, hipStream_t stream) {

@@ -497,6 +497,20 @@ def test_count_needs_left_padding():
     assert err.value.status == bmx.BM_ERR_ORDER and c.att.length == 60 and c.att.next_pos == 60
 
 
+def test_trees_after_one_that_is_too_large():
+    c = Bound(b=1, s=60)
+    for n in (66, 1, 64, 65, 3):
+        q, k, v = c.qkv(n)
+        o, parent = torch.zeros_like(q), torch.full((1, n), -1, dtype=torch.int32, device="cuda")
+        if n > bmx.BM_DRAFT_MAX:
+            with pytest.raises(bmx.BatchMaxError) as err:
+                c.att.draft_attend(parent, q, k, v, o)
+            assert err.value.status == bmx.BM_ERR_UNSUPPORTED and not o.any()
+        else:
+            c.att.draft_attend(parent, q, k, v, o)
+            assert torch.isfinite(o).all() and o.any()
+
+
 def test_a_workspace_full_of_nan_changes_no_bit():
     c = Bound(b=1, s=5000, kv_max=5000, block=1000, accumulate=False)
     parent = random_tree(1, 20, 3).cuda()
