@@ -282,6 +282,37 @@ def test_captured_steps_replay():
         assert torch.equal(o, eager) and torch.equal(r.att.k.nan_to_num(), k1.nan_to_num())
 
 
+@pytest.mark.parametrize("dtype,t", [("bf16", 200), ("bf16", 20), ("f32", 150)])
+def test_a_captured_turn_replays(dtype, t):
+    """Turns whose keys several workgroups share, replayed from the same state; another cache
+    uses the same workspace in between."""
+    r, other = (Run(window=2000, sinks=4, s=3000, b=2, dtype=dtype, seed=x) for x in (1, 50))
+    for x in (r, other):
+        x.go(2600, heads=(), samples=())
+    other.att.work = r.att.work
+    other.att.cache = other.att._cache()
+    other.att.resume(2600)
+    q, k, v = (x.cuda() for x in r.qkv(t))
+    oq, ok, ov = (x.cuda() for x in other.qkv(t))
+    k0, v0 = r.att.k.clone(), r.att.v.clone()
+    eager = torch.zeros_like(q)
+    r.att.prefill_block(2600, t, q, k, v, eager, row=0)
+    k1, v1 = r.att.k.clone(), r.att.v.clone()
+    r.att.resume(2600)
+    o, g = torch.zeros_like(q), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        r.att.prefill_block(2600, t, q, k, v, o, row=0)
+    for i in range(3):
+        r.att.k.copy_(k0)
+        r.att.v.copy_(v0)
+        o.zero_()
+        g.replay()
+        if i < 2:
+            other.att.prefill_block(2600 + i * t, t, oq, ok, ov, torch.zeros_like(oq), row=0)
+        torch.cuda.synchronize()
+        assert torch.equal(o, eager) and torch.equal(r.att.k, k1) and torch.equal(r.att.v, v1)
+
+
 def test_streams_and_two_caches_at_once():
     a, b = Run(window=300, sinks=4, s=900, b=2, seed=3), Run(window=300, sinks=4, s=900, b=2, seed=40)
     streams = [torch.cuda.Stream(), torch.cuda.Stream()]
