@@ -19,7 +19,7 @@
 // all), so the outputs carry little more than their own rounding.
 //
 // A token is HBM-bound: 64 samples' over windows of 4096 entries (8 KV heads, d = 128) take
-// 175 us, 6.1 TB/s.  A tree of 64 nodes with four heads each (256 rows a unit) is bound by its
+// 161 us, 6.7 TB/s.  A tree of 64 nodes with four heads each (256 rows a unit) is bound by its
 // waves' own instructions, one wave a SIMD: 512 units of 4096 entries take 505 us, 375 without
 // their loads, of which the products are 186 (545 TFLOP/s; with the second parts 820).
 // Short launches are a chain of latencies: 8 units of 64 rows and 512 entries take 11 us,
@@ -184,13 +184,15 @@ __device__ __forceinline__ void s_settled(f32x4 (&s)[RT][2]) {
   for (int rt = 0; rt < RT; ++rt) asm volatile("" : "+v"(s[rt][0]), "+v"(s[rt][1]));
 }
 
-template <bool BF16, int D, int RT>
+// NT: the cached rows are read past the last-level cache
+template <bool BF16, int D, int RT, bool NT>
 __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(NodesArgs a, int row_waves) {
   constexpr int kNodeWaves = node_waves(BF16, D, RT);
   constexpr bool kBig = big_wave(BF16, D, RT);
   using C = NodeCfg<BF16, D>;
   using E = typename C::E;
   constexpr int RB = C::RB, KL = C::KL, EPL = C::EPL, VW = C::VW;
+  constexpr int kAux = NT ? 2 : 0;                     // a load's non-temporal bit
   // a wave's part of LDS: O in quads of elements, m and l, for the join; the weights of a tile
   // of 32 keys (see the end of a tile) for a moment before
   constexpr int QUADS = EPL, PART = RT * (QUADS * 256 + 128);
@@ -231,7 +233,7 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
     for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int kk = 0; kk < KL; ++kk)
-        kf[s][kk] = __builtin_amdgcn_raw_buffer_load_b128(r, (base + 16 * s + i16) * RB + 16 * h + 64 * kk, 0, 0);
+        kf[s][kk] = __builtin_amdgcn_raw_buffer_load_b128(r, (base + 16 * s + i16) * RB + 16 * h + 64 * kk, 0, kAux);
     if (pos && pad > 0 && !node) pk = pos[min(base + (lane & 31), entries - 1)];
   };
   auto load_v = [&](int t) BM_LAMBDA {
@@ -242,13 +244,13 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
     for (int i = 0; i < 8; ++i) {
       const int off = (base + 16 * (i >> 2) + 4 * h + (i & 3)) * RB + i16 * (4 * VW);
       if constexpr (VW == 2) {
-        const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+        const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, kAux);
         vf[i][0] = x.x;
         vf[i][1] = x.y;
       } else {
 #pragma unroll
         for (int w = 0; w < VW; w += 4) {
-          const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, off + 4 * w, 0, 0);
+          const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(r, off + 4 * w, 0, kAux);
           vf[i][w] = x.x;
           vf[i][w + 1] = x.y;
           vf[i][w + 2] = x.z;
@@ -963,8 +965,16 @@ hipError_t launch_t(NodesArgs a, const NodePlan& p, hipStream_t stream) {
   const int tiles = (a.len0 + kTile - 1) / kTile + (a.n + kTile - 1) / kTile, most = tiles / p.key_waves();
   a.nsplit = most_splits(a.units, a.n_heads / a.n_kv_heads * a.n, p);
   if (a.nsplit > most) a.nsplit = most > 1 ? most : 1;
-  hipLaunchKernelGGL((nodes_kernel<BF16, D, RT>), dim3((unsigned)a.units, (unsigned)a.nsplit, (unsigned)p.row_groups),
-                     dim3(64 * p.waves), 0, stream, a, p.row_waves);
+  const dim3 grid((unsigned)a.units, (unsigned)a.nsplit, (unsigned)p.row_groups), block(64 * p.waves);
+  // Rows that one wave alone reads, once a step, stream past the last-level cache where it holds
+  // less than half of them: 1.07 GB take 161 us instead of 176, while of 269 MB the next
+  // step still finds enough there (45.7 us past it, 42.6 through it).
+  const size_t bytes = (size_t)a.units * a.len0 * 2 * NodeCfg<BF16, D>::RB;
+  const bool past = RT == 1 && p.row_waves == 1 && p.row_groups == 1 && bytes > 2 * kLastLevelCacheBytes;
+  if (past)
+    hipLaunchKernelGGL((nodes_kernel<BF16, D, RT, RT == 1>), grid, block, 0, stream, a, p.row_waves);
+  else
+    hipLaunchKernelGGL((nodes_kernel<BF16, D, RT, false>), grid, block, 0, stream, a, p.row_waves);
   hipError_t e = hipGetLastError();
   return e == hipSuccess && a.nsplit > 1 ? launch_join<BF16, D>(a, stream) : e;
 }

@@ -370,6 +370,39 @@ def test_offsets_past_32_bits():
     assert torch.equal(r.k[last][at], k[last][0]) and torch.equal(r.v[last][at], v[last][0])
 
 
+@pytest.mark.parametrize("dtype,d,heads", [("bf16", 64, 8), ("bf16", 128, 32), ("f32", 64, 16), ("f32", 128, 8)])
+def test_tokens_over_caches_beyond_the_last_level_one(dtype, d, heads):
+    """Launches that stream their rows: the first and the last unit, one sample with padding."""
+    from window_reference import Row
+    b, hk, window, sinks, end, group = 128, 8, 2100, 4, 5000, heads // 8       # 0.55 GB and more
+    r = bmx.WindowAttention(b=b, s=end, max_gen=8, window=window, sinks=sinks, n_heads=heads, n_kv_heads=hk,
+                            head_dim=d, dtype=dtype, block=4)
+    pads = torch.zeros(b, dtype=torch.int32)
+    pads[-1] = 1001
+    r.set_left_padding(pads.cuda())
+    g = torch.Generator(device="cuda").manual_seed(5)
+    r.k.normal_(generator=g)
+    r.v.normal_(generator=g)
+    r.resume(end)
+    q, k, v = (torch.randn((b, h, 1, d), device="cuda", generator=g).to(DT[dtype]) for h in (heads, hk, hk))
+    old_k, old_v = {}, {}
+    for j, u in ((0, 0), (b - 1, hk - 1)):
+        old_k[j, u], old_v[j, u] = r.k[j, u].cpu().double(), r.v[j, u].cpu().double()
+    o = torch.zeros_like(q)
+    r.decode_step(end, q, k, v, o)
+    for (j, u), kk in old_k.items():
+        now = end - int(pads[j])                                                # the token's index
+        index = torch.tensor([*range(sinks), *range(now - window, now)])
+        slot = torch.where(index < sinks, index, sinks + (index - sinks) % window)
+        keys = torch.cat([kk[slot], k[j, u].cpu().double()])
+        values = torch.cat([old_v[j, u][slot], v[j, u].cpu().double()])
+        seen = torch.cat([(index < sinks) | (now - index < window), torch.ones(1, dtype=torch.bool)])
+        for head in range(group * u, group * (u + 1)):
+            check_rows(o[j, head], [Row(q[j, head, 0].cpu().double(), keys, values, seen, d ** -0.5, DT[dtype], False)])
+        at = sinks + (now - sinks) % window
+        assert torch.equal(r.k[j, u, at], k[j, u, 0]) and torch.equal(r.v[j, u, at], v[j, u, 0])
+
+
 def test_another_current_device_is_refused():
     r = Run(window=8, sinks=0, s=10, b=1)
     q, k, v = (x.cuda() for x in r.qkv(10))
