@@ -142,10 +142,12 @@ struct NodePlan {
 // Waves of 64 rows read the keys from the caches half as often as those of 32, and are half as
 // many: they pay once the launch has work for all compute units.  us with 32 -> 64 rows, 8 KV
 // heads, four query heads each, d = 128:
-//   units rows entries  8 128 512    8 256 4096   64 128 512   64 128 4096  512 64 512   512 64 4096
-//                       21.8 -> 23.5 36.7 -> 43.6 27.6 -> 30.8 60.1 -> 51.4 41.0 -> 48.2 237 -> 199
-//                       512 128 512  512 128 4096 512 256 512  512 256 4096
-//                       61.0 -> 59.0 413 -> 291   128 -> 92    833 -> 506
+//   units rows entries  8 128 512     8 256 4096    64 128 512    64 128 4096   128 256 1024
+//                       21.8 -> 23.5  36.7 -> 43.6  27.6 -> 30.8  60.1 -> 51.4  51.4 -> 60.9
+//                       512 128 512   256 256 512   512 256 512   256 128 1024  128 256 2048
+//                       59.8 -> 61.3  65.6 -> 53.0  129 -> 102    48.7 -> 45.6  86.6 -> 89.4
+//                       512 64 2048   256 128 2048  512 128 2048  512 256 2048
+//                       120 -> 113    91.5 -> 75    186 -> 157    373 -> 270
 constexpr int64_t kBigWork = 1 << 25;       // units x rows x entries
 // Waves of 16 rows have the shorter chain where there is next to nothing to read; us with
 // 32 -> 16 rows:
