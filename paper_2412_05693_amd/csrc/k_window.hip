@@ -412,7 +412,12 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
         constexpr int next = j / 2 + kAhead;         // the operand that comes kAhead pairs on
         if constexpr (next < KK) k_fetch(next);
         else if constexpr (next < NS / 2) v_fetch(next - KK);
-        else kpre[next - NS / 2] = *lds_at<lds_u32x4>(KH ? ka[next - NS / 2] ^ TILE : ka[next - NS / 2] + 32 * RB);
+        else {
+          // (the next tile's first rows, which all waves wrote: behind the barrier, when this
+          // step's own operands have been read)
+          if constexpr (KH == 1 && next == NS / 2) lds_barrier();
+          kpre[next - NS / 2] = *lds_at<lds_u32x4>(KH ? ka[next - NS / 2] ^ TILE : ka[next - NS / 2] + 32 * RB);
+        }
       }
 #pragma unroll
       for (int i = j * 32 / NS; i < (j + 1) * 32 / NS; ++i) weight(i);
@@ -477,10 +482,12 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   raised = exceeds();
 #pragma unroll
   for (int i = 0; i < 2; ++i) kpre[i] = *lds_at<lds_u32x4>(ka[i] + 32 * RB);
-  // Tile t's halves: behind the first one K(t) and V(t - 1) are done with, and K(t + 2) and
-  // V(t + 2) take their places, copy by copy between the second one's products; the barrier
-  // behind the next tile's first half shows them.  (Past the last tile they are copies of
-  // it into places that nobody reads any more.)
+  // Tile t's halves: once the first one has read its operands K(t) and V(t - 1) are done with,
+  // and K(t + 2) and V(t + 2) take their places, copy by copy between the second one's
+  // products.  The barrier in every tile's first half, behind its last operands and before
+  // the first ones of the next tile, keeps both apart: it lets no wave overwrite what
+  // another one still reads, and shows what all of them wrote a tile before.  (Past the
+  // last tile the copies are of it, into places that nobody reads any more.)
   uint32_t v_at = 4 * TILE;                    // V of tile t - 1
   auto keep_o = [&]() BM_LAMBDA {
     // (O stays in the accumulation registers over the loop)
@@ -494,7 +501,6 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
     step(std::integral_constant<int, 1>{}, [](auto) BM_LAMBDA {}, zb, za, pa, pb, 2 * (t0 + t));
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) ka[kk] ^= TILE;
-    lds_barrier();
     keep_o();
     const uint32_t v_new = v_at - 2 * TILE;
     const int next = v_at == 4 * TILE ? -2 * TILE : TILE;
