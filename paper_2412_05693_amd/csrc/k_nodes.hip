@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(64 * node_waves(BF16, D, RT), 1) nodes_kernel(
   const int key_waves = kNodeWaves / row_waves, rw = wave / key_waves, kw = wave - rw * key_waves;
   const int row0 = ((int)blockIdx.z * row_waves + rw) * 16 * RT;     // the wave's first row
   const int pad = a.pad ? max(0, __builtin_amdgcn_readfirstlane(a.pad[bi])) : 0;
-  const int r0 = a.next_pos - pad;                                   // a root's index
+  const int r0 = index_of(a.next_pos, pad);                          // a root's index
   const Ring ring(r0, a.sinks, max(a.window, 1));
   const int entries = a.window ? ring.filled() : a.len0;
 

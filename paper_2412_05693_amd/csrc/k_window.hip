@@ -149,7 +149,7 @@ __global__ void __launch_bounds__(64 * kPromptWaves, 1) window_prompt_kernel(Pro
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int n = lane & 31, h = lane >> 5;
   const int pad = a.pad ? max(0, __builtin_amdgcn_readfirstlane(a.pad[bi])) : 0;
-  const int r0 = a.t0 - pad;                                 // the index of the call's first token
+  const int r0 = index_of(a.t0, pad);                        // the index of the call's first token
   const int p0 = pt * PT, tw = p0 + (w / G) * kPromptRows;   // first token of the workgroup, the wave
   const int p1 = min(p0 + PT, a.n_tok);
   const int64_t head = (int64_t)bi * a.n_heads + hk * G + w % G;
@@ -614,7 +614,7 @@ __global__ void __launch_bounds__(256, 2) window_prompt_f32_kernel(PromptArgs a,
   const int bi = u / a.n_kv_heads, hk = u - bi * a.n_kv_heads;
   const int64_t head = (int64_t)bi * a.n_heads + hk * group + g;
   const int pad = a.pad ? max(0, __builtin_amdgcn_readfirstlane(a.pad[bi])) : 0;
-  const int r0 = a.t0 - pad, tw = blk * kF32Rows, t_own = tw + i16;
+  const int r0 = index_of(a.t0, pad), tw = blk * kF32Rows, t_own = tw + i16;
   const int p1 = min(tw + kF32Rows, a.n_tok);
   float* o = static_cast<float*>(a.o) + (head * a.seq_ld + t_own) * D + 4 * EPL * h;
   const int first = max(r0 + tw, 0), last = r0 + p1 - 1;
@@ -742,16 +742,12 @@ __global__ void __launch_bounds__(256) window_store_kernel(PromptArgs a, int row
   const int u = blockIdx.x;
   const int pad = a.pad ? max(0, a.pad[u / a.n_kv_heads]) : 0;
   const int c = blockIdx.y * 256 + threadIdx.x;
-  // the first `lead` rows are those of possible sinks, then the call's last ones
   const int r = c / CPR, ch = c % CPR;
   if (r >= rows) return;
-  const int first = a.n_tok - min(a.n_tok, a.window);      // the first token kept for the window
-  const int r0 = a.t0 - pad;
-  // sinks of the call that lie before `first`: tokens max(0, -r0) on
-  const int lead = rows - (a.n_tok - first);
-  const int t = r < lead ? max(0, -r0) + r : first + r - lead;
+  const int kept = min(a.n_tok, a.window), r0 = index_of(a.t0, pad);
+  const int t = kept_token(r, rows - kept, a.n_tok, a.window, a.sinks, r0);
+  if (t < 0) return;
   const int i = r0 + t;
-  if (i < 0 || (r < lead && (i >= a.sinks || t >= first))) return;
   const int64_t src = ((int64_t)u * a.seq_ld + t) * RB + ch * 16;
   const int64_t dst =
       ((int64_t)u * (a.window + a.sinks) + window_slot(i, a.sinks, a.window)) * RB + ch * 16;

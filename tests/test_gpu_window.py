@@ -411,3 +411,18 @@ def test_another_current_device_is_refused():
         with pytest.raises(ValueError):
             r.att.prefill_block(0, 10, q, k, v, torch.zeros_like(q))
     assert r.att.next_pos == 0
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("window,sinks,calls", [(50, 4, (200, 70, 1)), (8, 4, (12, 13, 1)), (700, 6, (900, 90, 3))])
+def test_samples_that_never_begin(dtype, window, sinks, calls):
+    """The largest pads, in calls longer than the window: those samples see nothing, give zeros
+    and store nothing, whichever kernel takes the call (a prompt, the nodes of a chain, keys
+    over several workgroups), while the others go on."""
+    top = 2 ** 31 - 1
+    r = Run(dtype=dtype, window=window, sinks=sinks, s=sum(calls), b=5, d=64, pads=[0, top, top - 1, 2 ** 30, 3])
+    for t in calls:
+        r.go(t, heads=(3,) if t > 500 else None)
+        r.check_slots()
+    r.go(1, step=True)
+    r.check_slots()
