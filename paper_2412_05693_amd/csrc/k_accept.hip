@@ -155,7 +155,8 @@ __global__ void __launch_bounds__(256) accept_kernel(AcceptArgs a) {
         if (a.lse) a.score[slot] += all;
         if (late > 0) a.pos[slot] = pos + late;
       }
-      if (a.lastw) a.lastw[slot] = end;
+      // (of a sample that takes none the last query stays the one before)
+      if (a.lastw && (fresh || c > 0)) a.lastw[slot] = end;
     }
   }
 }

@@ -647,3 +647,38 @@ def test_speculation_gives_what_steps_give():
             out.append(o)
         assert (out[0] - out[1]).abs().max() <= 1e-5, kind
     assert lineage([-1, -1, 1, 1, 3, 0, 4])[6] == [1, 3, 4, 6]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("taken", [(0, 2), (2, 0), (0, 0)])
+def test_a_sample_that_takes_none_keeps_its_last_query(dtype, taken):
+    """The weights that rank by the last processed query are still those of the sample's own last
+    token when a call took none of its tokens and a lowered bound then cuts."""
+    kw = dict(dtype=dtype, heads=4, kv_heads=2, d=64, rule="tova", block=30, s=90)
+    c = Bound(b=2, pads=[0, 0], **kw)
+    alone = [Bound(b=1, pads=[0], **kw) for _ in range(2)]
+    for j, x in enumerate(alone):
+        x.att.reset()
+        mine = [y[j:j + 1].contiguous() for y in c.prompt]
+        x.att.run_prefill(*mine, torch.zeros_like(mine[0]), fused_cut=True)
+    n, m = 5, 2
+    parent = random_tree(2, n, 1)
+    path = pick_path(parent, m, 1)
+    q, k, v = c.qkv(n)
+    o, lse = torch.zeros_like(q), torch.zeros((2, 4, n), device="cuda")
+    c.att.draft_attend(parent.cuda(), q, k, v, o, lse=lse)
+    c.att.draft_accept(path.cuda(), q, k, v, lse=lse, count=torch.tensor(taken, dtype=torch.int32, device="cuda"))
+    step = c.qkv(1)
+    c.att.set_decode_bound(64)
+    c.att.decode_step(c.att.next_pos, *step, torch.zeros_like(step[0]))
+    for j, x in enumerate(alone):
+        mine = [y[j:j + 1].contiguous() for y in (q, k, v)]
+        oj, lj = torch.zeros_like(mine[0]), torch.zeros((1, 4, n), device="cuda")
+        x.att.draft_attend(parent[j:j + 1].contiguous().cuda(), *mine, oj, lse=lj)
+        if taken[j]:
+            x.att.draft_accept(path[j:j + 1, :taken[j]].contiguous().cuda(), *mine, lse=lj)
+        mine = [y[j:j + 1].contiguous() for y in step]
+        x.att.set_decode_bound(64)
+        x.att.decode_step(x.att.next_pos, *mine, torch.zeros_like(mine[0]))
+        for u in range(2):
+            same_entries(c.entries(j, u, int(c.pads[j])), x.entries(0, u))
