@@ -446,7 +446,7 @@ class PDAttention:
         self._bhd = (b, n_heads, n_kv_heads, head_dim)
         self._row_bytes = head_dim * (4 if self.dims.dtype == BM_F32 else 2)
         self.ctx = None
-        self._draft_works, self._draft_nodes = [], 0
+        self._draft_works = []      # the buffer of trees, once there is one (a stack's layers share the list)
         # schedule settings (bm_set_*): kept here and applied again to every new
         # context, so they survive reset() and resume()
         self._settings = {}
@@ -670,29 +670,40 @@ class PDAttention:
             raise ValueError(f"make {self.device} the current device")
         return self._row_ptrs(q, k, v, o, row)
 
-    def draft_attend(self, parent, q, k, v, o, lse=None, row=0) -> None:
-        """The attention of a tree's n nodes over the cache, their ancestors and themselves:
-        rows row .. row + n - 1 of q, k, v into o.  ``parent`` int32 ``[b, n]`` (-1: a root);
-        ``lse`` float32 ``[b, n_heads, n]`` or None takes their log-sum-exps.  The cache
-        is left as it is (one above the decode bound is cut to it)."""
-        n = parent.shape[-1]
-        tree = self._ints(parent, (self.dims.b, n), "parent")
-        rows = self._tree_rows(n, q, k, v, o, row)
-        if n > self._draft_nodes:
-            # (kept for later calls; another one for a larger tree, which needs no less.  The old
-            # one stays with graphs that were captured over it)
-            need = bm_draft_workspace_bytes(self.dims, n)
-            if need:                                   # (none: the call below says what is wrong)
-                self._draft_works.append(self.torch.empty(need, dtype=self.torch.uint8, device=self.device))
-                self._draft_nodes = n
-        work = self._draft_work
-        bm_draft_attend(self.ctx, n, tree, *rows, q.shape[2], self._lse_ptr(lse, n),
-                        work.data_ptr() if work is not None else None,
-                        work.numel() if work is not None else 0, self._stream())
+    def draft_work_bytes(self, n=BM_DRAFT_MAX) -> int:
+        """Bytes of scratch of a tree of n nodes (``draft_attend``'s work)."""
+        return bm_draft_workspace_bytes(self.dims, n)
 
     @property
     def _draft_work(self):
         return self._draft_works[-1] if self._draft_works else None
+
+    def _draft_scratch(self, work):
+        """Pointer and bytes of the caller's scratch, or of this object's own."""
+        if work is None:
+            work = self._draft_work
+            if work is None:
+                # (once, for the largest tree: a buffer that stays is what captured graphs need)
+                work = self.torch.empty(self.draft_work_bytes(), dtype=self.torch.uint8, device=self.device)
+                self._draft_works.append(work)
+        elif work.device != self.device or not work.is_contiguous():
+            raise ValueError(f"work: need a contiguous tensor on {self.device}")
+        return work.data_ptr(), work.numel() * work.element_size()
+
+    def draft_attend(self, parent, q, k, v, o, lse=None, row=0, work=None) -> None:
+        """The attention of a tree's n nodes over the cache, their ancestors and themselves:
+        rows row .. row + n - 1 of q, k, v into o.  ``parent`` int32 ``[b, n]`` (-1: a root);
+        ``lse`` float32 ``[b, n_heads, n]`` or None takes their log-sum-exps.  The cache
+        is left as it is (one above the decode bound is cut to it).  ``work``: scratch of at
+        least ``draft_work_bytes(n)`` bytes whose contents need not survive the call, so that
+        caches whose calls run one after another can share it; without it the object (a
+        ``PDStack``: its layers together) makes one of ``draft_work_bytes()`` at its first
+        tree and keeps it."""
+        n = parent.shape[-1]
+        tree = self._ints(parent, (self.dims.b, n), "parent")
+        rows = self._tree_rows(n, q, k, v, o, row)
+        bm_draft_attend(self.ctx, n, tree, *rows, q.shape[2], self._lse_ptr(lse, n),
+                        *self._draft_scratch(work), self._stream())
 
     def draft_accept(self, path, q, k, v, lse=None, count=None, row=0, n=None) -> None:
         """Append the m tokens ``path`` (int32 ``[b, m]``: node numbers, a root and then each
@@ -969,9 +980,10 @@ def stack_layer_bytes(*, b, kv_max, block, n_kv_heads, head_dim, dtype, kv_bits=
 class PDStack:
     """``n_layers`` independent bounded caches (the attention layers of one
     model, each with its own scores and evictions) carved from one device
-    arena, sharing one workspace (its contents never outlive a call).  Layer
-    ``l`` is driven through ``self.layers[l]``, a ``PDAttention`` (``kv_bits`` 4: a
-    ``PDAttentionKV4``)."""
+    arena, sharing one workspace (its contents never outlive a call) and, once
+    a layer has drafted tokens, one buffer of ``draft_work_bytes()`` for them
+    besides the arena.  Layer ``l`` is driven through ``self.layers[l]``, a
+    ``PDAttention`` (``kv_bits`` 4: a ``PDAttentionKV4``)."""
 
     def __init__(self, *, n_layers, b, s, kv_max, block, max_gen, n_heads, n_kv_heads, head_dim,
                  dtype="bf16", sm_scale=0.0, device="cuda", kv_bits=16):
@@ -1017,6 +1029,8 @@ class PDStack:
                                           head_dim=head_dim, dtype=dtype, sm_scale=sm_scale,
                                           device=dev, init=False,
                                           buffers=(*kv, sc, ps, ln, work)))
+            # (scratch of drafted tokens' trees, made at the first one)
+            self.layers[-1]._draft_works = self.layers[0]._draft_works
         self.n_layers = n_layers
         self.device = dev
 
@@ -1030,16 +1044,19 @@ class PDStack:
 
 
 def stack_bytes(*, b, n_layers, s, kv_max, block, max_gen, n_heads, n_kv_heads, head_dim,
-                dtype, kv_bits=16) -> int:
+                dtype, kv_bits=16, drafts=False) -> int:
     """Device bytes a P&D run of the layer stack needs at batch b: every layer's
-    bounded cache, the shared workspace, and the reusable input/output buffers
-    of one prefill block and one decode row."""
+    bounded cache, the shared workspace (with ``drafts`` also that of drafted
+    tokens), and the reusable input/output buffers of one prefill block and one
+    decode row."""
     es = 4 if dtype in ("f32", BM_F32) else 2
     dims = make_dims(b=b, s=s, kv_max=kv_max, block=block, max_gen=max_gen, n_heads=n_heads,
                      n_kv_heads=n_kv_heads, head_dim=head_dim, dtype=dtype)
     caches = n_layers * stack_layer_bytes(b=b, kv_max=kv_max, block=block, n_kv_heads=n_kv_heads,
                                           head_dim=head_dim, dtype=dtype, kv_bits=kv_bits)
     work = _align(bm_kv4_workspace_bytes(dims) if kv_bits == 4 else bm_workspace_bytes(dims))
+    if drafts:
+        work += _align(bm_draft_workspace_bytes(dims, BM_DRAFT_MAX))
     rows = block + 1
     io = rows * b * (2 * n_heads + 2 * n_kv_heads) * head_dim * es
     return caches + work + io

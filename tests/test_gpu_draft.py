@@ -682,3 +682,61 @@ def test_a_sample_that_takes_none_keeps_its_last_query(dtype, taken):
         x.att.decode_step(x.att.next_pos, *mine, torch.zeros_like(mine[0]))
         for u in range(2):
             same_entries(c.entries(j, u, int(c.pads[j])), x.entries(0, u))
+
+
+def test_trees_of_all_sizes_share_one_scratch():
+    """Trees that grow node by node keep one buffer, of the size that the object names."""
+    c = Bound(b=1, s=400, kv_max=400, block=400)
+    q, k, v = c.qkv(64)
+    o = torch.zeros_like(q)
+    trees_ = [random_tree(1, n, n).cuda() for n in range(1, 65)]
+    before = torch.cuda.memory_allocated()
+    for parent in trees_:
+        c.att.draft_attend(parent, q, k, v, o)
+    torch.cuda.synchronize()
+    assert torch.cuda.memory_allocated() - before <= (c.att.draft_work_bytes() + (2 << 20))
+    assert c.att.draft_work_bytes() == max(c.att.draft_work_bytes(n) for n in range(1, 65))
+
+
+def test_caches_share_a_callers_scratch():
+    """One buffer for caches whose calls follow one another: the same bits as with their own."""
+    a, b = Bound(seed=1, b=1, s=500, kv_max=500, block=500), Bound(seed=9, b=1, s=90, dtype="f32")
+    work = torch.full((max(x.att.draft_work_bytes(20) for x in (a, b)),), 255, dtype=torch.uint8, device="cuda")
+    parent = random_tree(1, 20, 3).cuda()
+    data = [x.qkv(20) for x in (a, b)]
+    outs = []
+    for w in (work, None):
+        for c, x in zip((a, b), data):
+            o, lse = torch.zeros_like(x[0]), torch.zeros((1, 4, 20), device="cuda")
+            c.att.draft_attend(parent, *x, o, lse=lse, work=w)
+            assert (w is None) == (len(c.att._draft_works) == 1)
+            outs.append((o, lse))
+    for (o1, l1), (o2, l2) in zip(outs[:2], outs[2:]):
+        assert torch.equal(o1, o2) and torch.equal(l1, l2)
+    x = data[0]
+    with pytest.raises(bmx.BatchMaxError):
+        a.att.draft_attend(parent, *x, torch.zeros_like(x[0]), work=work[:a.att.draft_work_bytes(20) - 16])
+    with pytest.raises(bmx.BatchMaxError):
+        a.att.draft_attend(parent, *x, torch.zeros_like(x[0]), work=work[8:])     # (not 16-byte aligned)
+    for bad in (work.cpu(), work[::2]):
+        with pytest.raises(ValueError):
+            a.att.draft_attend(parent, *x, torch.zeros_like(x[0]), work=bad)
+
+
+def test_layers_of_a_stack_share_one_scratch():
+    kw = dict(b=1, s=60, kv_max=100, block=60, max_gen=20, n_heads=4, n_kv_heads=1, head_dim=64)
+    stack = bmx.PDStack(n_layers=3, **kw)
+    stack.reset()
+    q, k, v = (rows(i, 1, h, 60, 64, "bf16").cuda() for i, h in enumerate((4, 1, 1)))
+    parent = random_tree(1, 8, 3)
+    tree, x = parent.cuda(), [y[:, :, :8].contiguous() for y in (q, k, v)]
+    for layer in stack.layers:
+        layer.run_prefill(q, k, v, torch.zeros_like(q))
+    for layer in stack.layers:
+        o = torch.zeros_like(x[0])
+        layer.draft_attend(tree, *x, o)
+        want = tree_over(layer.k[0, 0, :60], layer.v[0, 0, :60], torch.ones(60, dtype=torch.bool), parent[0].tolist(),
+                         x[0][0, 3], x[1][0, 0], x[2][0, 0], 64 ** -0.5, torch.bfloat16)
+        check_rows(o[0, 3], want)
+    assert len({layer._draft_work.data_ptr() for layer in stack.layers}) == 1
+    stack.close()

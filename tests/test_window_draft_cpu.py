@@ -252,3 +252,21 @@ def test_draft_tensors_are_checked():
             att.draft_accept(path, q, k, k, **kw2)
     with pytest.raises(ValueError):
         att.draft_accept(path.long(), q, k, k)
+
+
+def test_scratch_of_trees_is_counted():
+    kw = dict(b=2, s=64, kv_max=32, block=16, max_gen=8, n_heads=8, n_kv_heads=2, head_dim=64, dtype="bf16")
+    stack = bmx.PDStack(n_layers=3, device="cpu", **kw)
+    need = stack.layers[0].draft_work_bytes()
+    assert need == bmx.bm_draft_workspace_bytes(stack.layers[0].dims, bmx.BM_DRAFT_MAX)
+    assert stack.layers[0].draft_work_bytes(5) == bmx.bm_draft_workspace_bytes(stack.layers[0].dims, 5) < need
+    one = [layer._draft_scratch(None) for layer in stack.layers]
+    assert one[0] == one[1] == one[2] and one[0][1] == need
+    extra = bmx.stack_bytes(n_layers=3, drafts=True, **kw) - bmx.stack_bytes(n_layers=3, **kw)
+    assert need <= extra < need + 256
+    own = torch.empty(need // 4, dtype=torch.float32)
+    assert stack.layers[1]._draft_scratch(own) == (own.data_ptr(), own.numel() * 4)
+    with pytest.raises(ValueError):
+        stack.layers[0]._draft_scratch(own[::2])
+    with pytest.raises(ValueError):
+        stack.layers[0]._draft_scratch(own.to("meta"))
