@@ -375,6 +375,11 @@ def make_dims(*, b, s, kv_max, block, max_gen, n_heads, n_kv_heads, head_dim, dt
 # ---------------------------------------------------------------------------
 # tensor-owning convenience wrapper
 # ---------------------------------------------------------------------------
+# Pad arrays that acceptances have grown, by device and address: how often, and the K plane of
+# the cache that the last time was for.  An array that grows for one cache is no other cache's.
+_grown_pads: dict = {}
+
+
 class PDAttention:
     """Owns one layer's bounded cache (torch tensors on a GPU) and drives the ABI.
 
@@ -446,6 +451,7 @@ class PDAttention:
         self._bhd = (b, n_heads, n_kv_heads, head_dim)
         self._row_bytes = head_dim * (4 if self.dims.dtype == BM_F32 else 2)
         self.ctx = None
+        self._pads, self._pads_grown = None, 0
         self._draft_works = []      # the buffer of trees, once there is one (a stack's layers share the list)
         # schedule settings (bm_set_*): kept here and applied again to every new
         # context, so they survive reset() and resume()
@@ -548,6 +554,7 @@ class PDAttention:
         if old is not None:
             bm_destroy(old)
         self._apply_settings()
+        self._pads_grown = self._grown()[0]
 
     def reset(self) -> None:
         self._replace_context(self._new_context())
@@ -610,8 +617,23 @@ class PDAttention:
         if pads.dtype != t.int32 or pads.device != self.device or not pads.is_contiguous() or \
                 tuple(pads.shape) != (self.dims.b,):
             raise ValueError(f"pads: need a contiguous int32 [{self.dims.b}] tensor on {self.device}")
-        self._pads = pads
         self._set("pad", pads.data_ptr())
+        self._pads = pads
+        self._pads_grown = self._grown()[0]
+
+    def _grown(self) -> tuple:
+        """How often the pad array has grown, and for which cache last."""
+        if self._pads is None:
+            return 0, None
+        return _grown_pads.get((self._dev_index, self._pads.data_ptr()), (0, None))
+
+    def _own_pads(self) -> int:
+        """How often the pad array has grown; refuses one that grew for another cache."""
+        times, cache = self._grown()
+        if times != self._pads_grown and cache != self.k.data_ptr():
+            raise ValueError("the left padding has grown with another cache's accepted tokens: each cache "
+                             "(layer) needs a tensor of its own")
+        return times
 
     def set_split_event(self, event) -> None:
         """Record ``event`` (a torch.cuda.Event, or None to stop) between each
@@ -702,6 +724,7 @@ class PDAttention:
         n = parent.shape[-1]
         tree = self._ints(parent, (self.dims.b, n), "parent")
         rows = self._tree_rows(n, q, k, v, o, row)
+        self._own_pads()
         bm_draft_attend(self.ctx, n, tree, *rows, q.shape[2], self._lse_ptr(lse, n),
                         *self._draft_scratch(work), self._stream())
 
@@ -710,15 +733,21 @@ class PDAttention:
         one's child) of the tree of n nodes (by default all rows from ``row`` on; ``lse``, if
         given, has n columns) and advance by m.  ``lse``: as draft_attend left it.  ``count``
         int32 ``[b]``: sample j takes only the first count[j]; the samples' left padding has to
-        be set, and that tensor grows by m - count: caches (layers) must not share it."""
+        be set, and that tensor grows by m - count: caches (layers) must not share it (a draft
+        over another cache with the same tensor is then refused, until its padding is set
+        anew or it begins again)."""
         if n is None:
             n = lse.shape[-1] if lse is not None else q.shape[2] - row
         m = path.shape[-1]
         tree = self._ints(path, (self.dims.b, m), "path")
         taken = None if count is None else self._ints(count, (self.dims.b,), "count")
         rows = self._tree_rows(n, q, k, v, q, row)
+        times = self._own_pads()
         bm_draft_accept(self.ctx, n, m, tree, taken, *rows[:3], q.shape[2], self._lse_ptr(lse, n),
                         self._stream())
+        if count is not None:
+            self._pads_grown = times + 1
+            _grown_pads[self._dev_index, self._pads.data_ptr()] = times + 1, self.k.data_ptr()
 
     def run_prefill(self, q, k, v, o, fused_cut=False) -> None:
         """Algorithm 1 prefill under the block loop: every block, then a cut

@@ -740,3 +740,44 @@ def test_layers_of_a_stack_share_one_scratch():
         check_rows(o[0, 3], want)
     assert len({layer._draft_work.data_ptr() for layer in stack.layers}) == 1
     stack.close()
+
+
+def test_caches_that_share_a_pad_tensor():
+    """An acceptance grows the pads of one cache: drafts over another one with the same tensor
+    are refused, those of another object over the same cache are not."""
+    kw = dict(b=2, s=60, block=30, d=64)
+    a, b = Bound(pads=[0, 3], seed=1, **kw), Bound(pads=[0, 3], seed=2, **kw)
+    same = bmx.PDAttention(b=2, s=60, kv_max=100, block=30, max_gen=256, n_heads=4, n_kv_heads=1, head_dim=64,
+                           buffers=[getattr(a.att, x) for x in ("k", "v", "score", "pos", "len", "work")], init=False)
+    same.set_left_padding(a.pads)
+    same.resume(60, 60)
+    b.att.set_left_padding(a.pads)                       # as a program would that has one tensor for its layers
+    parent, path = torch.tensor([[-1, 0, 1]] * 2, dtype=torch.int32, device="cuda"), torch.tensor([[0, 1]] * 2, dtype=torch.int32, device="cuda")
+    count = torch.tensor([2, 1], dtype=torch.int32, device="cuda")
+    x, lses = [c.qkv(3) for c in (a, b)], [torch.zeros((2, 4, 3), device="cuda") for _ in range(2)]
+    for c, y, lse in zip((a, b), x, lses):
+        c.att.draft_attend(parent, *y, torch.zeros_like(y[0]), lse=lse)
+    a.att.draft_accept(path, *x[0], lse=lses[0], count=count)
+    assert a.pads.tolist() == [0, 4]
+    before = [getattr(b.att, n).clone() for n in ("k", "v", "score", "pos", "len")]
+    for call in (lambda: b.att.draft_accept(path, *x[1], lse=lses[1], count=count),
+                 lambda: b.att.draft_accept(path, *x[1], lse=lses[1]),
+                 lambda: b.att.draft_attend(parent, *x[1], torch.zeros_like(x[1][0]))):
+        with pytest.raises(ValueError, match="another cache"):
+            call()
+    assert a.pads.tolist() == [0, 4] and b.att.length == 60
+    assert all(torch.equal(p.nan_to_num(), getattr(b.att, n).nan_to_num())
+               for p, n in zip(before, ("k", "v", "score", "pos", "len")))
+    # the same cache through another object, and the first one again
+    same.resume(62, 62)
+    for att, m in ((same, 2), (a.att, 2)):
+        if att is a.att:
+            att.resume(64, 64)
+        att.draft_attend(parent, *x[0], torch.zeros_like(x[0][0]), lse=lses[0])
+        att.draft_accept(path, *x[0], lse=lses[0], count=count)
+    assert a.pads.tolist() == [0, 6]
+    # a tensor of its own
+    b.pads = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+    b.att.set_left_padding(b.pads)
+    b.att.draft_accept(path, *x[1], lse=lses[1], count=count)
+    assert b.pads.tolist() == [0, 4]
