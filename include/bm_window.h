@@ -58,7 +58,10 @@ int bm_win_validate(const bm_dims* dims, int32_t sinks);
 /* A context over an empty window cache; no device work. */
 int bm_win_init(const bm_dims* dims, int32_t sinks, const bm_win_cache* cache, bm_ctx** out);
 
-/* A context over a cache that holds the rows of the tokens before next_pos. */
+/* A context over a cache that holds the rows of the tokens before next_pos.  Also how a turn
+ * of several tokens follows generated ones, since a context prefills while its next
+ * position is below dims.s and generates from there on: a new context over the same cache
+ * at the same position, with dims.s past the turn (the other one is then destroyed). */
 int bm_win_resume(const bm_dims* dims, int32_t sinks, const bm_win_cache* cache,
                   int32_t next_pos, bm_ctx** out);
 

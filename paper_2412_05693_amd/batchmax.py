@@ -943,11 +943,22 @@ class WindowAttention(PDAttention):
     def _new_context(self) -> int:
         return bm_win_init(self.dims, self.sinks, self.cache)
 
-    def resume(self, next_pos: int) -> None:
-        """A context over the rows of the tokens before ``next_pos`` as they lie in k and v."""
-        if not -_INT32_MAX <= next_pos <= _INT32_MAX:
-            raise ValueError(f"next_pos {next_pos}: beyond 32 bits")
-        self._replace_context(bm_win_resume(self.dims, self.sinks, self.cache, next_pos))
+    def resume(self, next_pos: int, s: int | None = None) -> None:
+        """A context over the rows of the tokens before ``next_pos`` as they lie in k and v.  ``s``:
+        another prompt length, for a turn behind generated tokens: after ``resume(p, s=p + n)``
+        with p = ``next_pos``, n more tokens go through ``prefill_block`` (at most ``block`` a call)
+        and steps follow from p + n on.  (``reset`` keeps it; ``resume(0, s=..)`` begins anew
+        with another.)"""
+        s = self.dims.s if s is None else s
+        if not (-_INT32_MAX <= next_pos <= _INT32_MAX and -_INT32_MAX <= s <= _INT32_MAX):
+            raise ValueError(f"next_pos {next_pos}, s {s}: beyond 32 bits")
+        old, self.dims.s = self.dims.s, s
+        try:
+            new = bm_win_resume(self.dims, self.sinks, self.cache, next_pos)
+        except BatchMaxError:
+            self.dims.s = old
+            raise
+        self._replace_context(new)
 
 
 # ---------------------------------------------------------------------------

@@ -426,3 +426,21 @@ def test_samples_that_never_begin(dtype, window, sinks, calls):
         r.check_slots()
     r.go(1, step=True)
     r.check_slots()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_turns_behind_generated_tokens(dtype):
+    """A conversation: a prompt, tokens, a turn of several calls, tokens, a short turn, a token."""
+    r = Run(dtype=dtype, window=50, sinks=3, s=70, b=3, d=64, pads=[0, 60, 73])
+    r.go(70)
+    for turn in ((40, 21), (5,), (1,)):
+        for _ in range(3):
+            r.go(1, step=True)
+        p = r.att.next_pos
+        r.att.resume(p, s=p + sum(turn))
+        for t in turn:
+            r.go(t)
+        assert r.att.next_pos == r.att.dims.s
+        r.check_slots()
+    r.go(1, step=True)
+    r.check_slots()

@@ -270,3 +270,19 @@ def test_scratch_of_trees_is_counted():
         stack.layers[0]._draft_scratch(own[::2])
     with pytest.raises(ValueError):
         stack.layers[0]._draft_scratch(own.to("meta"))
+
+
+def test_a_refused_resume_keeps_the_prompt_length():
+    att = bmx.WindowAttention(window=8, sinks=2, b=2, s=64, max_gen=8, n_heads=8, n_kv_heads=2, head_dim=64,
+                              device="cpu")
+    att.resume(70, s=90)
+    assert (att.dims.s, att.next_pos, att.length) == (90, 70, 10)
+    for bad in (dict(next_pos=70, s=0), dict(next_pos=70, s=61), dict(next_pos=-1, s=80), dict(next_pos=70, s=2 ** 30)):
+        with pytest.raises(bmx.BatchMaxError):
+            att.resume(**bad)
+        assert (att.dims.s, att.next_pos) == (90, 70)
+    with pytest.raises(ValueError):
+        att.resume(70, s=2 ** 40)
+    assert (att.dims.s, att.next_pos) == (90, 70)
+    att.resume(64)
+    assert (att.dims.s, att.next_pos) == (90, 64)
