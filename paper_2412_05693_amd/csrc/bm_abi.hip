@@ -728,10 +728,6 @@ BM_EXPORT int bm_prefill_block_cut(bm_ctx* ctx, int32_t t0, int32_t n_tok, const
     const int ws = check_block(ctx, t0, n_tok, q, k, v, o, seq_ld);
     return ws == BM_OK ? win_prompt(ctx, n_tok, q, k, v, o, seq_ld, stream) : ws;
   }
-  if (ctx && ctx->window) {
-    const int ws = check_block(ctx, t0, n_tok, q, k, v, o, seq_ld);
-    return ws == BM_OK ? win_prompt(ctx, n_tok, q, k, v, o, seq_ld, stream) : ws;
-  }
   bm::PrefillArgs a;
   int st = prefill_args(ctx, t0, n_tok, q, k, v, o, seq_ld, &a);
   if (st != BM_OK) return st;

@@ -46,9 +46,4 @@ struct Ring {
   }
 };
 
-// whether the token at index i >= 0 sees the one at index j
-__device__ __forceinline__ bool window_sees(int i, int j, int sinks, int window) {
-  return j >= 0 && j <= i && (j < sinks || i - j < window);
-}
-
 }  // namespace bm
