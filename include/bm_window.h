@@ -21,6 +21,15 @@
  * bm_set_score_accumulation) return BM_ERR_UNSUPPORTED.  bm_ctx_len is the number of
  * slots that a sample without padding has filled.
  *
+ * bfloat16: a prefill call of more than 64 tokens, or of more than 128 query rows a KV head
+ * (tokens times query heads), rounds each softmax weight to bfloat16 before its product
+ * with V, as bm_prefill_block over a bounded cache does; shorter calls, single tokens and
+ * drafted ones carry weights to 2^-16.  So the last bits of an output depend on how its
+ * prompt was cut into calls: 2.3e-3 and 1.6e-3 (relative, root mean square) from the exact
+ * one, of which 1.6e-3 are the output's own rounding.  Float32 calls have no such step.
+ *
+ * bm_set_split_event's event is recorded behind a prefill call's launches.
+ *
  * What a slot without a token holds is of no weight, NaN included, and so is what a
  * pad token's rows hold.  Rows of real tokens have to be finite: in a call's result a
  * NaN or infinity of a V row also reaches queries of the same call that do not see it.

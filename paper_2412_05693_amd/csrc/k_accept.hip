@@ -167,7 +167,9 @@ __global__ void __launch_bounds__(256) pad_kernel(AcceptArgs a, int b) {
   if (bi < b) a.pad[bi] = grown(max(0, a.pad[bi]), a.m - taken(a, bi));
 }
 
-// Window cache: a workgroup a sample, all KV heads' rows, and then the sample's pad.
+// Window cache: a workgroup a sample, all KV heads' rows, and then the sample's pad.  Latency-bound
+// for short paths (8 KV heads, d = 128, a call within a graph: 64 samples that take 4 tokens 3.3 us,
+// 512 4.4); 64 samples that take 64 29 us, 2.3 TB/s, with 64 compute units at work.
 template <int RB>
 __global__ void __launch_bounds__(256) window_accept_kernel(AcceptArgs a) {
   constexpr int CPR = RB / 16;

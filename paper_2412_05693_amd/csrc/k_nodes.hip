@@ -19,11 +19,11 @@
 // all), so the outputs carry little more than their own rounding.
 //
 // A token is HBM-bound: 64 samples' over windows of 4096 entries (8 KV heads, d = 128) take
-// 161 us, 6.7 TB/s.  A tree of 64 nodes with four heads each (256 rows a unit) is bound by its
+// 162 us, 6.6 TB/s (d = 64 85, 6.3; float32 over 1024 entries 109, 4.9).  A tree of 64 nodes with four heads each (256 rows a unit) is bound by its
 // waves' own instructions, one wave a SIMD: 512 units of 4096 entries take 505 us, 375 without
 // their loads, of which the products are 186 (545 TFLOP/s; with the second parts 820).
-// Short launches are a chain of latencies: 8 units of 64 rows and 512 entries take 11 us,
-// of which arguments 1, queries and tree 2, tiles 3, the join 2.
+// Short launches are a chain of latencies: 8 units of 64 rows and 512 entries take 10.5 us
+// (11 with waves of 32 rows, of which arguments 1, queries and tree 2, tiles 3, the join 2).
 //
 // The workgroup's waves share the rows (up to 8 blocks of them) and then the key tiles; waves
 // over the same rows join through LDS, workgroups over the same unit through the workspace
@@ -140,14 +140,20 @@ struct NodePlan {
 };
 
 // Waves of 64 rows read the keys from the caches half as often as those of 32, and are half as
-// many: they pay once the launch has work for all compute units.  us with 32 -> 64 rows, 8 KV
-// heads, four query heads each, d = 128:
-//   units rows entries  8 128 512     8 256 4096    64 128 512    64 128 4096   128 256 1024
-//                       21.8 -> 23.5  36.7 -> 43.6  27.6 -> 30.8  60.1 -> 51.4  51.4 -> 60.9
-//                       512 128 512   256 256 512   512 256 512   256 128 1024  128 256 2048
-//                       59.8 -> 61.3  65.6 -> 53.0  129 -> 102    48.7 -> 45.6  86.6 -> 89.4
-//                       512 64 2048   256 128 2048  512 128 2048  512 256 2048
-//                       120 -> 113    91.5 -> 75    186 -> 157    373 -> 270
+// many: they pay once the launch has work for all compute units.  us with 32 -> 64 rows,
+// 64 nodes of one, two or four query heads a KV head:
+//   units rows entries   d = 128         d = 64         units rows entries   d = 128         d = 64
+//   64 256 512           32.3 -> 42.2    26.9 -> 32.8   256 128 512          34.3 -> 32.0    25.3 -> 22.3
+//   128 256 1024         51.5 -> 60.3    39.7 -> 45.7   256 128 2048         93.6 -> 75.6    59.8 -> 55.3
+//   64 256 4096          92.4 -> 84.2    74.1 -> 65.8   512 128 512          65.4 -> 60.5    33.8 -> 42.7
+//   256 256 512          65.7 -> 52.5    33.7 -> 36.1   512 128 2048         190 -> 159      102 -> 109
+//   256 256 2048         177 -> 137      96.6 -> 101    64 64 4096           33.6 -> 35.4    26.3 -> 24.6
+//   512 256 2048         369 -> 272      194 -> 203     256 64 512           21.4 -> 24.3    16.4 -> 16.5
+//   64 128 512           26.4 -> 30.3    20.3 -> 21.0   256 64 2048          55.0 -> 52.4    35.8 -> 33.2
+//   64 128 4096          55.4 -> 51.2    39.7 -> 37.9   512 64 2048          123 -> 116      57.1 -> 65.0
+// One number for all of them (2^25) is up to 17% off at d = 128 (128 units of 256 rows, whose
+// half as many workgroups split the keys instead) and up to 26% at d = 64, where two
+// workgroups of the smaller waves fit a compute unit.
 constexpr int64_t kBigWork = 1 << 25;       // units x rows x entries
 // Waves of 16 rows have the shorter chain where there is next to nothing to read; us with
 // 32 -> 16 rows:

@@ -52,8 +52,9 @@ constexpr float kNegInf = -__builtin_huge_valf();
 //
 // MFMA-bound in principle; measured, the vector unit and the matrix unit take turns (39% of
 // the waves' cycles are products, 9 vector instructions each).  32 heads, 8 KV heads,
-// d = 128: 8 x 4096 tokens over a window of 1024 take 646 us (747 TFLOP/s, at 16 tiles a
-// workgroup 9 of 42 us are its beginning and end), 2 x 32768 over 4096 4.1 ms (1.0 PFLOP/s).
+// d = 128: 8 x 4096 tokens over a window of 1024 take 660 us (731 TFLOP/s, at 16 tiles a
+// workgroup 9 of 42 us are its beginning and end), 2 x 32768 over 4096 4.1 ms (1.0 PFLOP/s);
+// at d = 64 512 us and 3.0 ms (539 and 728 TFLOP/s).
 // The loop's products alone run at 1.5 PFLOP/s.
 constexpr int kPromptRows = 64;              // of a wave
 constexpr int kPromptWaves = 4;
