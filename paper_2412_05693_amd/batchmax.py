@@ -566,6 +566,8 @@ class PDAttention:
 
     def _block_args(self, t0, n_tok, q, k, v, o, row):
         row = t0 if row is None else row
+        if t0 == 0 and self._pads is not None:
+            self._pads_grown = self._grown()[0]         # (a new prompt takes the pads as they are)
         if self._args_ok(q, k, v, o) and 0 <= row < q.shape[2] and row + n_tok <= q.shape[2]:
             return (self.ctx, t0, n_tok, *self._row_ptrs(q, k, v, o, row), q.shape[2],
                     self._stream())

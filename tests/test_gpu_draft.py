@@ -781,3 +781,24 @@ def test_caches_that_share_a_pad_tensor():
     b.att.set_left_padding(b.pads)
     b.att.draft_accept(path, *x[1], lse=lses[1], count=count)
     assert b.pads.tolist() == [0, 4]
+
+
+def test_caches_that_use_a_pad_tensor_one_after_another():
+    """A tensor that holds its first values again serves the next cache's prompt and drafts."""
+    pads = torch.tensor([0, 3], dtype=torch.int32, device="cuda")
+    kw = dict(b=2, s=60, max_gen=20, n_heads=4, n_kv_heads=1, head_dim=64)
+    atts = [bmx.PDAttention(kv_max=100, block=30, **kw), bmx.WindowAttention(window=40, sinks=2, block=30, **kw)]
+    for att in atts:
+        att.set_left_padding(pads)
+    q, k, v = (rows(i, 2, h, 60, 64, "bf16").cuda() for i, h in enumerate((4, 1, 1)))
+    x = [y[:, :, :3].contiguous() for y in (q, k, v)]
+    parent, path = (torch.tensor([r] * 2, dtype=torch.int32, device="cuda") for r in ([-1, 0, 1], [0, 1]))
+    count = torch.tensor([2, 1], dtype=torch.int32, device="cuda")
+    for att in atts:
+        pads.copy_(torch.tensor([0, 3]))
+        att.run_prefill(q, k, v, torch.zeros_like(q), fused_cut=True)
+        for grown in (4, 5):
+            lse = torch.zeros((2, 4, 3), device="cuda")
+            att.draft_attend(parent, *x, torch.zeros_like(x[0]), lse=lse)
+            att.draft_accept(path, *x, lse=lse, count=count)
+            assert pads.tolist() == [0, grown]
